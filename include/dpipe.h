@@ -462,6 +462,47 @@ int dp_op_attention_bwd(int dtype, int B, int H, int Nq, int Nk, int d_head, flo
                         int ldk, const void* v, int ldv, const void* o, int ldo, const float* lse, const void* d_o, int lddo,
                         float* delta, void* dq, int lddq, void* dk, int lddk, void* dv, int lddv, void* hip_stream);
 
+/* Dropout, and LayerNorm behind a dropout and a residual sum, for training: the end of a transformer sub-layer.
+ *
+ * No mask is stored.  Whether an element is kept follows from its position alone: the Philox4x32-10 generator, called with the counter
+ * (column / 8, row, site, step) and the key seed, gives 128 bits for eight neighbouring columns, sixteen for each (column 8 g + j: bits
+ * 16 (j % 2) .. of word j / 2), and the element is kept where this number is at least t = p * 65536 rounded to the nearest whole number.  What is
+ * kept is multiplied by 65536 / (65536 - t): the probability is the multiple of 2^-16 next to p, and the expectation is that of the input.  A dropped
+ * element contributes zero whatever it holds (infinities and NaN too); p = 1 drops everything.
+ *   rng        [device] two uint64, {seed, step}; the low 32 bits of step count.  Read by the kernel: a captured graph draws a new mask at each
+ *              replay if the caller has changed step in between, and the backward of a pass has to find the values of its forward.  NULL where p
+ *              rounds to no drop at all.
+ *   site       tells the dropouts of a step apart (one number for each place in the model)
+ *   first_row  the number of row 0: a slice of a batch drops what the whole batch would (rows counted modulo 2^32)
+ *
+ * dp_op_dropout: y = residual + dropout(x), residual NULL: y = dropout(x).  The backward is the same call on the gradient (residual: a gradient
+ * to add it to).  x, residual, y [rows, cols] in the storage dtype, row strides ldx, ldr, ldy; any width and stride, less than 2^34 elements; y may be x or
+ * residual itself (same stride), and overlaps neither otherwise.
+ *
+ * dp_op_layernorm_fwd: sum = residual + dropout(x), y = (sum - mean) rstd gamma + beta, with mean and rstd = 1 / sqrt(variance + eps) of the
+ * row (biased variance), formed in fp32 from the sum before it is rounded to its type.  x, y, gamma, beta in the storage dtype; residual and sum in
+ * the storage dtype or, with sum_f32, in fp32 (the residual stream of a stage); mean, rstd fp32 [rows].  residual, gamma with beta, sum, mean and rstd may
+ * be NULL; without residual and dropout x is the sum, which the backward then takes in its place.  sum may be residual itself, y may be x.
+ *
+ * dp_op_layernorm_bwd: with g = dy gamma and xh = (sum - mean) rstd, each row
+ *   dsum = rstd (g - average(g) - xh average(g xh)) + dsum_in,    dx = dropout of dsum (formed from dsum before it is rounded),
+ *   dgamma = sum over the rows of dy xh,    dbeta = of dy    (fp32 [d]; overwritten, or added to with accumulate).
+ * dsum is the gradient of sum and of residual, dsum_in (NULL: none) what reaches sum on other ways; both in the type of sum; dx (NULL: not wanted) is the
+ * gradient of x, in the storage dtype.  dsum, dgamma and dbeta may be NULL, but not dsum and dx both.  dsum may be dsum_in itself, dx may be dy.
+ * workspace: dp_op_layernorm_bwd_workspace_bytes(rows, d) bytes, 256-byte aligned; not needed without dgamma and dbeta.  Calls that may overlap need
+ * workspaces of their own.  Sums are in a fixed order: equal calls give equal bits.
+ * Rows of at most 8192 columns, any width and stride, less than 2^31 / 1024 rows of more than 4096 columns (narrower ones more); zero rows are a valid call (of no effect but that the backward clears dgamma and dbeta, if it does not accumulate).  Pointers 16-byte aligned. */
+int dp_op_dropout(int dtype, int rows, int cols, const void* x, int ldx, const void* residual, int ldr, float p, const uint64_t* rng, uint32_t site,
+                  uint32_t first_row, void* y, int ldy, void* hip_stream);
+int dp_op_layernorm_fwd(int dtype, int sum_f32, int rows, int d, float eps, const void* x, int ldx, const void* residual, int ldr, float p,
+                        const uint64_t* rng, uint32_t site, uint32_t first_row, const void* gamma, const void* beta, void* sum, int lds, void* y,
+                        int ldy, float* mean, float* rstd, void* hip_stream);
+size_t dp_op_layernorm_bwd_workspace_bytes(int rows, int d);
+int dp_op_layernorm_bwd(int dtype, int sum_f32, int rows, int d, const void* dy, int lddy, const void* sum, int lds, const float* mean,
+                        const float* rstd, const void* gamma, const void* dsum_in, int ldi, float p, const uint64_t* rng, uint32_t site,
+                        uint32_t first_row, void* dsum, int ldds, void* dx, int lddx, float* dgamma, float* dbeta, int accumulate, void* workspace,
+                        size_t workspace_bytes, void* hip_stream);
+
 /* Measurement aid: per-launch kernel timing.  Between dp_ktime_begin and dp_ktime_end every
  * kernel class the library launches is bracketed by hipEvents on the caller's stream; each
  * record carries the kernel kind, the algorithmic FLOPs and bytes of that launch (the

@@ -14,6 +14,7 @@ Further modules, each with its own header and pins:
   bubbles.py        1F1B bubbles and their filling (Sec. 5, Algorithms 1-2)
   search.py         the walk over (S, M, D) (Sec. 3, steps 2-5)
   image_encoder.py  3x3 convolution, GroupNorm, residual and attention blocks of the frozen image encoder
+  training_ops.py   dropout from a counter-based generator, LayerNorm behind it, attention with a relative position bias (extensions)
   fp8.py            OCP E4M3 quantisation and the FP8 projection product (an extension beyond the paper)
 
 Only tests, the smoke check and the bench's cpu_baseline leg may import this

@@ -111,7 +111,8 @@ EXPORTS = ["dp_stage_create", "dp_stage_destroy", "dp_stage_set_overlap", "dp_st
            "dp_encoder_profile", "dp_image_encoder_create", "dp_image_encoder_destroy", "dp_image_encoder_param_count",
            "dp_image_encoder_param_shape", "dp_image_encoder_layer_shape", "dp_image_encoder_workspace_bytes", "image_encoder_fwd_partial",
            "dp_image_encoder_profile", "dp_ktime_begin", "dp_ktime_end", "dp_ktime_event_overhead_ms", "dp_last_error", "dp_op_gemm", "dp_op_gemm_fp8", "dp_op_quantize_fp8", "dp_op_gemm_static", "dp_op_gemm_workspace_bytes",
-           "dp_op_attention_fwd", "dp_op_attention_bwd", "dp_partition_solve", "dp_partition_solve_bidirectional", "dp_bubbles_1f1b", "dp_bubbles_fill", "dp_schedule_search"]
+           "dp_op_attention_fwd", "dp_op_attention_bwd", "dp_op_dropout", "dp_op_layernorm_fwd", "dp_op_layernorm_bwd",
+           "dp_op_layernorm_bwd_workspace_bytes", "dp_partition_solve", "dp_partition_solve_bidirectional", "dp_bubbles_1f1b", "dp_bubbles_fill", "dp_schedule_search"]
 
 
 def library_path() -> str:
@@ -164,6 +165,11 @@ def load_library():
     lib.dp_op_gemm_static.argtypes = [i, vp, i, i, vp, i, i, i, i, i, vp, vp, i, i, i, i, vp]
     lib.dp_op_attention_fwd.argtypes = [i, i, i, i, i, i, i, f, vp, i, vp, i, vp, i, vp, i, vp, vp]
     lib.dp_op_attention_bwd.argtypes = [i, i, i, i, i, i, f, vp, i, vp, i, vp, i, vp, i, vp, vp, i, vp, vp, i, vp, i, vp, i, vp]
+    u32 = C.c_uint32
+    lib.dp_op_dropout.argtypes = [i, i, i, vp, i, vp, i, f, vp, u32, u32, vp, i, vp]
+    lib.dp_op_layernorm_fwd.argtypes = [i, i, i, i, f, vp, i, vp, i, f, vp, u32, u32, vp, vp, vp, i, vp, i, vp, vp, vp]
+    lib.dp_op_layernorm_bwd_workspace_bytes.argtypes = [i, i]; lib.dp_op_layernorm_bwd_workspace_bytes.restype = sz
+    lib.dp_op_layernorm_bwd.argtypes = [i, i, i, i, vp, i, vp, i, vp, vp, vp, vp, i, f, vp, u32, u32, vp, i, vp, i, vp, vp, i, vp, sz, vp]
     lib.dp_partition_solve.argtypes = [C.POINTER(LayerCost), i, C.POINTER(PartitionOpts), C.POINTER(PartitionPlan)]
     dptr = C.POINTER(C.c_double)
     lib.dp_bubbles_1f1b.argtypes = [i, dptr, dptr, C.POINTER(i), i, dptr, dptr, dptr, C.c_double, C.POINTER(Bubble), i, C.POINTER(i), dptr]
@@ -506,3 +512,26 @@ def op_attention_bwd(dtype, B, H, Nq, Nk, d_head, scale, q, ldq, k, ldk, v, ldv,
     _check(load_library().dp_op_attention_bwd(dtype, B, H, Nq, Nk, d_head, scale, _ptr(q), ldq, _ptr(k), ldk, _ptr(v), ldv,
                                               _ptr(o), ldo, _ptr(lse), _ptr(d_o), lddo, _ptr(delta), _ptr(dq), lddq,
                                               _ptr(dk), lddk, _ptr(dv), lddv, _stream(stream)))
+
+
+def op_dropout(dtype, rows, cols, x, ldx, residual, ldr, p, rng, site, first_row, y, ldy, stream=None):
+    """rng: two 64-bit integers on the device, {seed, step}."""
+    _check(load_library().dp_op_dropout(dtype, rows, cols, _ptr(x), ldx, _ptr(residual), ldr, p, _ptr(rng), site, first_row, _ptr(y), ldy,
+                                        _stream(stream)))
+
+
+def op_layernorm_fwd(dtype, sum_f32, rows, d, eps, x, ldx, residual, ldr, p, rng, site, first_row, gamma, beta, sum_, lds, y, ldy, mean, rstd,
+                     stream=None):
+    _check(load_library().dp_op_layernorm_fwd(dtype, int(sum_f32), rows, d, eps, _ptr(x), ldx, _ptr(residual), ldr, p, _ptr(rng), site, first_row,
+                                              _ptr(gamma), _ptr(beta), _ptr(sum_), lds, _ptr(y), ldy, _ptr(mean), _ptr(rstd), _stream(stream)))
+
+
+def op_layernorm_bwd_workspace_bytes(rows, d):
+    return load_library().dp_op_layernorm_bwd_workspace_bytes(rows, d)
+
+
+def op_layernorm_bwd(dtype, sum_f32, rows, d, dy, lddy, sum_, lds, mean, rstd, gamma, dsum_in, ldi, p, rng, site, first_row, dsum, ldds, dx, lddx,
+                     dgamma, dbeta, accumulate, workspace, stream=None):
+    _check(load_library().dp_op_layernorm_bwd(dtype, int(sum_f32), rows, d, _ptr(dy), lddy, _ptr(sum_), lds, _ptr(mean), _ptr(rstd), _ptr(gamma),
+                                              _ptr(dsum_in), ldi, p, _ptr(rng), site, first_row, _ptr(dsum), ldds, _ptr(dx), lddx, _ptr(dgamma),
+                                              _ptr(dbeta), int(accumulate), _ptr(workspace), _nbytes(workspace), _stream(stream)))

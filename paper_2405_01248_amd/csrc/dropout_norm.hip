@@ -1,0 +1,489 @@
+// Dropout (mask formed from the position, dp_dropout.h), and LayerNorm with the dropout and the residual sum in front of it, forward and
+// backward, as operators of their own: rows of any width and stride.  Bound by memory: every operand is read once and every result written once, in
+// accesses of eight columns a lane (16 bytes in bf16, 32 in fp32), which need no alignment beyond the element's; only the last group of a row whose
+// width is not a multiple of eight goes element by element.  Sums and statistics are fp32, in a fixed order.
+#include "dp_device.h"
+#include "dp_dropout.h"
+#include "dp_errors.h"
+#include "dp_host.h"
+#include "dp_kernels.h"
+#include "dp_ktime.h"
+
+#include <math.h>
+#include <type_traits>
+
+namespace dp {
+
+// Eight columns, as they lie in memory: the vector type is aligned like its element (wide global accesses do not ask for more).
+template <typename T> struct Row8;
+template <> struct Row8<bf16> { typedef bf16x8 value; typedef bf16x8 packed __attribute__((aligned(2))); };
+template <> struct Row8<float> { typedef __attribute__((ext_vector_type(8))) float value; typedef value packed __attribute__((aligned(4))); };
+
+template <typename T> __device__ __forceinline__ typename Row8<T>::value row8_load(const T* p, int n) {      // n: columns there are, the others are zero
+  if (n >= 8) return *reinterpret_cast<const typename Row8<T>::packed*>(p);
+  typename Row8<T>::value v;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = j < n ? p[j] : (T)0.f;
+  return v;
+}
+template <typename T> __device__ __forceinline__ void row8_store(T* p, int n, const float (&x)[8]) {
+  typename Row8<T>::value v;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = from_f<T>(x[j]);
+  if (n >= 8) {
+    *reinterpret_cast<typename Row8<T>::packed*>(p) = v;
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    if (j < n) p[j] = v[j];
+}
+template <typename T> __device__ __forceinline__ void row8_widen(const typename Row8<T>::value& v, float (&x)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) x[j] = to_f<T>(v[j]);
+}
+
+// ------------------------------------------------------------------ dropout
+struct DropoutK {
+  int rows, cols, groups;      // groups of eight columns in a row
+  const void* x; int ldx;
+  const void* residual; int ldr;
+  void* y; int ldy;
+  DropK drop;
+};
+
+// A thread takes U groups, 256 apart, of the workgroup's 256 U consecutive ones (rows one after the other), all requested before the first mask.
+template <typename T, int U>
+__global__ void __launch_bounds__(256) dropout_kernel(const DropoutK a) {
+  const uint64_t first = (uint64_t)blockIdx.x * (256 * U);
+  const uint32_t row_first = (uint32_t)(first / (uint32_t)a.groups), rest = (uint32_t)(first % (uint32_t)a.groups);
+  const DropKey key = drop_key(a.drop);
+  uint32_t row[U], group[U];
+  typename Row8<T>::value xv[U], rv[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const uint32_t at = rest + 256 * u + threadIdx.x, over = at / (uint32_t)a.groups;
+    row[u] = row_first + over;
+    group[u] = at - over * (uint32_t)a.groups;
+    if (row[u] >= (uint32_t)a.rows) continue;
+    const int n = a.cols - 8 * (int)group[u];
+    xv[u] = row8_load((const T*)a.x + (size_t)row[u] * a.ldx + 8 * (size_t)group[u], n);
+    if (a.residual) rv[u] = row8_load((const T*)a.residual + (size_t)row[u] * a.ldr + 8 * (size_t)group[u], n);
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (row[u] >= (uint32_t)a.rows) continue;
+    float v[8], r[8];
+    row8_widen<T>(xv[u], v);
+    drop8(a.drop, key, group[u], row[u], v);
+    if (a.residual) {
+      row8_widen<T>(rv[u], r);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] += r[j];
+    }
+    row8_store((T*)a.y + (size_t)row[u] * a.ldy + 8 * (size_t)group[u], a.cols - 8 * (int)group[u], v);
+  }
+}
+
+// ------------------------------------------------------------------ rows of a LayerNorm
+// L lanes share a row: 16, 32 or 64 of a wave, or a workgroup of 256, 512 or 1024; lane l has columns 8 (c L + l) .. + 7 for c = 0 .. NC - 1.
+constexpr int NORM_MAX_D = 8192;
+template <int L> constexpr int norm_threads = L < 256 ? 256 : L;
+template <int L> __device__ __forceinline__ float norm_row_sum(float v, float* red) {      // red: a float per wave, for a row that several waves share
+  if constexpr (L >= 64) v = reduce_halves(v, AddOp());
+  if constexpr (L >= 32) v = reduce_row_pairs(v, AddOp());
+  v = reduce_row(v, AddOp());
+  if constexpr (L > 64) {
+    if (threadIdx.x % 64 == 0) red[threadIdx.x / 64] = v;
+    __syncthreads();
+    v = red[0];
+#pragma unroll
+    for (int w = 1; w < L / 64; ++w) v += red[w];
+  }
+  return v;
+}
+
+struct NormK {
+  int rows, d;
+  float eps;
+  const void* x; int ldx;
+  const void* residual; int ldr;
+  const void* gamma; const void* beta;
+  void* sum; int lds;
+  void* y; int ldy;
+  float* mean; float* rstd;
+  DropK drop;
+};
+
+// y = LayerNorm(residual + dropout(x)).  The statistics are those of the fp32 sum: what is stored of it may have been rounded to 16 bits.
+template <typename T, typename S, int L, int NC>
+__global__ void __launch_bounds__(norm_threads<L>) norm_fwd_kernel(const NormK a) {
+  __shared__ float red[2][L > 64 ? L / 64 : 1];
+  const int l = threadIdx.x % L, wanted = blockIdx.x * (norm_threads<L> / L) + threadIdx.x / L, row = min(wanted, a.rows - 1);
+  const bool live = wanted < a.rows;
+  const T* x = (const T*)a.x + (size_t)row * a.ldx;
+  const S* res = (const S*)a.residual + (size_t)row * a.ldr;
+  auto left = [&](int c) { return a.d - 8 * (c * L + l); };      // columns from this group on
+  typename Row8<T>::value xv[NC], ga[NC], be[NC];
+  typename Row8<S>::value rv[NC];
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+    if (left(c) > 0) {
+      xv[c] = row8_load(x + 8 * (c * L + l), left(c));
+      if (a.residual) rv[c] = row8_load(res + 8 * (c * L + l), left(c));
+    }
+#pragma unroll
+  for (int c = 0; c < NC; ++c)      // (behind the row, not behind the two reductions: few rows wait for each round trip)
+    if (left(c) > 0 && a.gamma) {
+      ga[c] = row8_load((const T*)a.gamma + 8 * (c * L + l), left(c));
+      be[c] = row8_load((const T*)a.beta + 8 * (c * L + l), left(c));
+    }
+  const DropKey key = drop_key(a.drop);
+  float v[NC][8], s = 0.f;
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    if (left(c) <= 0) continue;
+    row8_widen<T>(xv[c], v[c]);
+    drop8(a.drop, key, c * L + l, row, v[c]);
+    if (a.residual) {
+      float r[8];
+      row8_widen<S>(rv[c], r);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[c][j] += r[j];
+    }
+    if (a.sum && live) row8_store((S*)a.sum + (size_t)row * a.lds + 8 * (c * L + l), left(c), v[c]);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s += v[c][j];
+  }
+  const float mu = norm_row_sum<L>(s, red[0]) / a.d;
+  float q = 0.f;
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < left(c)) {
+        v[c][j] -= mu;
+        q = fmaf(v[c][j], v[c][j], q);
+      }
+  const float rs = rsqrtf(norm_row_sum<L>(q, red[1]) / a.d + a.eps);
+  if (!live) return;
+  if (l == 0) {
+    if (a.mean) a.mean[row] = mu;
+    if (a.rstd) a.rstd[row] = rs;
+  }
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    if (left(c) <= 0) continue;
+    float g[8], b[8];
+    if (a.gamma) {
+      row8_widen<T>(ga[c], g);
+      row8_widen<T>(be[c], b);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[c][j] = a.gamma ? fmaf(v[c][j] * rs, g[j], b[j]) : v[c][j] * rs;
+    row8_store((T*)a.y + (size_t)row * a.ldy + 8 * (c * L + l), left(c), v[c]);
+  }
+}
+
+// ------------------------------------------------------------------ backward
+struct NormBwdK {
+  int rows, d;
+  const void* dy; int lddy;
+  const void* sum; int lds;
+  const float* mean; const float* rstd;
+  const void* gamma;
+  const void* dsum_in; int ldi;
+  void* dsum; int ldds;
+  void* dx; int lddx;
+  float* partial;      // [workgroup][2][d], or NULL
+  DropK drop;
+};
+
+// With g = dy gamma and xh = (sum - mean) rstd: dsum = rstd (g - mean(g) - xh mean(g xh)) + dsum_in, dx = dropout of dsum, and the columns' sums of
+// dy xh and dy.  A group of L lanes walks every G-th row, the next one's operands requested before the present one is used; a lane adds its columns of
+// dy xh and dy in registers, and the groups' sums meet in LDS at the end.
+template <typename T, typename S, int L, int NC>
+__global__ void __launch_bounds__(norm_threads<L>) norm_bwd_kernel(const NormBwdK a) {
+  constexpr int NT = norm_threads<L>, PER = NT / L;      // rows at a time
+  __shared__ float red[2][2][L > 64 ? L / 64 : 1];
+  __shared__ __attribute__((aligned(16))) float meet[PER > 1 ? NT * 8 : 8];
+  const int l = threadIdx.x % L, sub = threadIdx.x / L, step = gridDim.x * PER;
+  auto left = [&](int c) { return a.d - 8 * (c * L + l); };
+  const DropKey key = drop_key(a.drop);
+  float ga[NC][8], dg[NC][8], db[NC][8];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) { ga[c][j] = 1.f; dg[c][j] = 0.f; db[c][j] = 0.f; }
+    if (left(c) > 0 && a.gamma) row8_widen<T>(row8_load((const T*)a.gamma + 8 * (c * L + l), left(c)), ga[c]);
+  }
+  typename Row8<T>::value yv[NC];
+  typename Row8<S>::value sv[NC], iv[NC];
+  float mu, rs;
+  auto fetch = [&](int row) {
+    mu = a.mean[row];
+    rs = a.rstd[row];
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+      if (left(c) > 0) {
+        const int col = 8 * (c * L + l);
+        yv[c] = row8_load((const T*)a.dy + (size_t)row * a.lddy + col, left(c));
+        sv[c] = row8_load((const S*)a.sum + (size_t)row * a.lds + col, left(c));
+        if (a.dsum_in) iv[c] = row8_load((const S*)a.dsum_in + (size_t)row * a.ldi + col, left(c));
+      }
+  };
+  // every wave makes as many turns as its workgroup's first row group: the row sums of a workgroup per row meet at barriers
+  int row = blockIdx.x * PER + sub;
+  fetch(min(row, a.rows - 1));
+  int turn = 0;
+  for (int base = blockIdx.x * PER; base < a.rows; base += step, row += step, turn ^= 1) {
+    const bool live = row < a.rows;
+    float g[NC][8], xh[NC][8], in[NC][8], s0 = 0.f, s1 = 0.f;
+    const float r = rs;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      if (left(c) <= 0) continue;
+      float sm[8];
+      row8_widen<T>(yv[c], g[c]);
+      row8_widen<S>(sv[c], sm);
+      if (a.dsum_in) row8_widen<S>(iv[c], in[c]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const bool on = live && j < left(c);
+        xh[c][j] = on ? (sm[j] - mu) * rs : 0.f;
+        if (!live) g[c][j] = 0.f;
+        dg[c][j] = fmaf(g[c][j], xh[c][j], dg[c][j]);
+        db[c][j] += g[c][j];
+        g[c][j] *= ga[c][j];
+        s0 += g[c][j];
+        s1 = fmaf(g[c][j], xh[c][j], s1);
+      }
+    }
+    if (base + step < a.rows) fetch(min(row + step, a.rows - 1));
+    const float m0 = norm_row_sum<L>(s0, red[turn][0]) / a.d, m1 = norm_row_sum<L>(s1, red[turn][1]) / a.d;
+    if (!live) continue;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      if (left(c) <= 0) continue;
+      const int col = 8 * (c * L + l);
+      float o[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        o[j] = r * (g[c][j] - m0 - xh[c][j] * m1);
+        if (a.dsum_in) o[j] += in[c][j];
+      }
+      if (a.dsum) row8_store((S*)a.dsum + (size_t)row * a.ldds + col, left(c), o);
+      if (a.dx) {
+        drop8(a.drop, key, c * L + l, row, o);
+        row8_store((T*)a.dx + (size_t)row * a.lddx + col, left(c), o);
+      }
+    }
+  }
+  if (!a.partial) return;
+  float* out = a.partial + (size_t)blockIdx.x * 2 * a.d;
+#pragma unroll
+  for (int which = 0; which < 2; ++which)
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      float (&v)[8] = which ? db[c] : dg[c];
+      if constexpr (PER > 1) {      // lane l of the first group adds the groups' in their order
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < 8; j += 4) *reinterpret_cast<f32x4*>(&meet[threadIdx.x * 8 + j]) = f32x4{v[j], v[j + 1], v[j + 2], v[j + 3]};
+        __syncthreads();
+        if (sub == 0)
+          for (int w = 1; w < PER; ++w)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += meet[(w * L + l) * 8 + j];
+      }
+      if (sub == 0 && left(c) > 0) row8_store(out + (size_t)which * a.d + 8 * (c * L + l), left(c), v);
+    }
+}
+
+// Columns' sums of the workgroups' parts [parts][n]: 8 columns of 32 shares of the parts a workgroup, the shares added in their order.
+__global__ void __launch_bounds__(256) norm_bwd_reduce_kernel(const float* __restrict__ partial, int parts, int d, float* __restrict__ dgamma,
+                                                              float* __restrict__ dbeta, int accumulate) {
+  __shared__ float meet[32][8];
+  const int col = blockIdx.x * 8 + threadIdx.x % 8, share = threadIdx.x / 8, n = 2 * d;
+  float s = 0.f;
+  if (col < n) {
+#pragma unroll 8
+    for (int p = share; p < parts; p += 32) s += partial[(size_t)p * n + col];
+  }
+  meet[share][threadIdx.x % 8] = s;
+  __syncthreads();
+  if (threadIdx.x >= 8 || col >= n) return;
+  for (int w = 1; w < 32; ++w) s += meet[w][threadIdx.x];
+  float* out = col < d ? dgamma : dbeta;
+  const int at = col < d ? col : col - d;
+  if (!out) return;
+  out[at] = accumulate ? out[at] + s : s;
+}
+
+// ------------------------------------------------------------------ host side
+static int make_drop(float p, const uint64_t* rng, uint32_t site, uint32_t first_row, const char* who, DropK& k) {
+  if (!(p >= 0.f) || !(p <= 1.f)) return set_errorf(DP_EINVAL, "%s: the probability must lie in [0, 1]", who);
+  k = DropK{rng, (uint32_t)lrintf(p * 65536.f), site, first_row, 0.f};
+  if (k.threshold < 65536) k.up = 65536.f / (float)(65536 - k.threshold);
+  if (k.threshold == 0) return DP_OK;
+  if (!rng) return set_errorf(DP_EINVAL, "%s: dropout needs the generator's state", who);
+  if ((uintptr_t)rng % 8) return set_errorf(DP_EALIGN, "%s: the generator's state must be 8-byte aligned", who);
+  return DP_OK;
+}
+static int check_rows(const void* p, int ld, int cols, const char* who, const char* what) {
+  if (!p) return set_errorf(DP_EINVAL, "%s: %s is NULL", who, what);
+  if ((uintptr_t)p % 16) return set_errorf(DP_EALIGN, "%s: %s is not 16-byte aligned", who, what);
+  if (ld < cols) return set_errorf(DP_EINVAL, "%s: the row stride of %s is less than a row", who, what);
+  return DP_OK;
+}
+static int check_vec(const void* p, const char* who, const char* what) {
+  if ((uintptr_t)p % 16) return set_errorf(DP_EALIGN, "%s: %s is not 16-byte aligned", who, what);
+  return DP_OK;
+}
+static int launched(const char* who) {
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? DP_OK : set_errorf(DP_EHIP, "%s: launch failed (%s)", who, hipGetErrorString(e));
+}
+
+template <typename T> static int dropout_t(const DropoutK& k, hipStream_t s) {
+  const uint64_t groups = (uint64_t)k.rows * k.groups;
+  // two groups a thread where there are waves enough for the CUs anyway
+  if (groups >= 256ull * 2 * 1024) hipLaunchKernelGGL((dropout_kernel<T, 2>), dim3((unsigned)((groups + 511) / 512)), dim3(256), 0, s, k);
+  else hipLaunchKernelGGL((dropout_kernel<T, 1>), dim3((unsigned)((groups + 255) / 256)), dim3(256), 0, s, k);
+  return launched("dp_op_dropout");
+}
+
+// f(lanes, chunks) by the width of a row
+template <class F> static void norm_dispatch(int d, F f) {
+  using std::integral_constant;
+  auto with = [&](auto l, auto nc) { f(l, nc); };
+  if (d <= 128) with(integral_constant<int, 16>(), integral_constant<int, 1>());
+  else if (d <= 256) with(integral_constant<int, 16>(), integral_constant<int, 2>());
+  else if (d <= 512) with(integral_constant<int, 32>(), integral_constant<int, 2>());
+  else if (d <= 1024) with(integral_constant<int, 64>(), integral_constant<int, 2>());
+  else if (d <= 2048) with(integral_constant<int, 256>(), integral_constant<int, 1>());
+  else if (d <= 4096) with(integral_constant<int, 512>(), integral_constant<int, 1>());
+  else with(integral_constant<int, 1024>(), integral_constant<int, 1>());
+}
+static int norm_rows_per_workgroup(int d) {
+  int per = 1;
+  norm_dispatch(d, [&](auto l, auto) { per = norm_threads<l> / l; });
+  return per;
+}
+static bool norm_too_many(int rows, int d) {      // a launch has less than 2^32 threads
+  long lanes = 1;
+  norm_dispatch(d, [&](auto l, auto) { lanes = l; });
+  return rows * lanes >= (1l << 31);
+}
+// Workgroups of the backward, hence parts to be added afterwards.
+static int norm_bwd_workgroups(int rows, int d) {
+  const int per = norm_rows_per_workgroup(d);
+  return std::min((rows + per - 1) / per, d <= 2048 ? 1024 : 512);
+}
+template <typename T, typename S> static int norm_fwd_t(const NormK& k, hipStream_t s) {
+  norm_dispatch(k.d, [&](auto l, auto nc) {
+    constexpr int PER = norm_threads<l> / l;
+    hipLaunchKernelGGL((norm_fwd_kernel<T, S, l, nc>), dim3((k.rows + PER - 1) / PER), dim3(norm_threads<l>), 0, s, k);
+  });
+  return launched("dp_op_layernorm_fwd");
+}
+template <typename T, typename S> static int norm_bwd_t(const NormBwdK& k, int workgroups, hipStream_t s) {
+  norm_dispatch(k.d, [&](auto l, auto nc) { hipLaunchKernelGGL((norm_bwd_kernel<T, S, l, nc>), dim3(workgroups), dim3(norm_threads<l>), 0, s, k); });
+  return launched("dp_op_layernorm_bwd");
+}
+
+}  // namespace dp
+
+using namespace dp;
+
+extern "C" {
+
+int dp_op_dropout(int dtype, int rows, int cols, const void* x, int ldx, const void* residual, int ldr, float p, const uint64_t* rng, uint32_t site,
+                  uint32_t first_row, void* y, int ldy, void* hip_stream) {
+  const char* who = "dp_op_dropout";
+  if (dtype != DP_F32 && dtype != DP_BF16) return set_error(DP_EINVAL, "unknown dtype");
+  if (rows < 0 || cols <= 0) return set_errorf(DP_EINVAL, "%s: bad size", who);
+  DropoutK k{rows, cols, cols / 8 + (cols % 8 != 0), x, ldx, residual, ldr, y, ldy, {}};
+  DP_TRY(make_drop(p, rng, site, first_row, who, k.drop));
+  if (rows == 0) return DP_OK;
+  DP_TRY(check_rows(x, ldx, cols, who, "x"));
+  DP_TRY(check_rows(y, ldy, cols, who, "y"));
+  if (residual) DP_TRY(check_rows(residual, ldr, cols, who, "residual"));
+  if ((uint64_t)rows * k.groups >= (1ull << 31)) return set_errorf(DP_EUNSUPPORTED, "%s: 2^34 elements and more", who);      // (a launch has less than 2^32 threads)
+  const int es = dtype == DP_BF16 ? 2 : 4;
+  KScope ks(KK_OTHER, 0.0, (double)rows * cols * es * (residual ? 3 : 2), (hipStream_t)hip_stream, rows, cols);
+  return dtype == DP_BF16 ? dropout_t<bf16>(k, (hipStream_t)hip_stream) : dropout_t<float>(k, (hipStream_t)hip_stream);
+}
+
+int dp_op_layernorm_fwd(int dtype, int sum_f32, int rows, int d, float eps, const void* x, int ldx, const void* residual, int ldr, float p,
+                        const uint64_t* rng, uint32_t site, uint32_t first_row, const void* gamma, const void* beta, void* sum, int lds, void* y, int ldy,
+                        float* mean, float* rstd, void* hip_stream) {
+  const char* who = "dp_op_layernorm_fwd";
+  if (dtype != DP_F32 && dtype != DP_BF16) return set_error(DP_EINVAL, "unknown dtype");
+  if (rows < 0 || d <= 0) return set_errorf(DP_EINVAL, "%s: bad size", who);
+  if (d > NORM_MAX_D) return set_errorf(DP_EUNSUPPORTED, "%s: rows of at most %d columns", who, NORM_MAX_D);
+  if (norm_too_many(rows, d)) return set_errorf(DP_EUNSUPPORTED, "%s: too many rows", who);
+  if (!(eps > 0.f) || !(eps < INFINITY)) return set_errorf(DP_EINVAL, "%s: eps must be positive and finite", who);
+  if ((gamma == nullptr) != (beta == nullptr)) return set_errorf(DP_EINVAL, "%s: gamma and beta come together", who);
+  NormK k{rows, d, eps, x, ldx, residual, ldr, gamma, beta, sum, lds, y, ldy, mean, rstd, {}};
+  DP_TRY(make_drop(p, rng, site, first_row, who, k.drop));
+  if (rows == 0) return DP_OK;
+  DP_TRY(check_rows(x, ldx, d, who, "x"));
+  DP_TRY(check_rows(y, ldy, d, who, "y"));
+  if (residual) DP_TRY(check_rows(residual, ldr, d, who, "residual"));
+  if (sum) DP_TRY(check_rows(sum, lds, d, who, "sum"));
+  DP_TRY(check_vec(gamma, who, "gamma")); DP_TRY(check_vec(beta, who, "beta")); DP_TRY(check_vec(mean, who, "mean")); DP_TRY(check_vec(rstd, who, "rstd"));
+  hipStream_t s = (hipStream_t)hip_stream;
+  const int es = dtype == DP_BF16 ? 2 : 4, ss = dtype == DP_F32 || sum_f32 ? 4 : 2;
+  KScope ks(KK_LN_FWD, 0.0, (double)rows * d * (2 * es + (residual ? ss : 0) + (sum ? ss : 0)) + 8.0 * rows, s, rows, d);
+  if (dtype == DP_F32) return norm_fwd_t<float, float>(k, s);
+  return sum_f32 ? norm_fwd_t<bf16, float>(k, s) : norm_fwd_t<bf16, bf16>(k, s);
+}
+
+size_t dp_op_layernorm_bwd_workspace_bytes(int rows, int d) {
+  if (rows <= 0 || d <= 0 || d > NORM_MAX_D) return 0;
+  return align_up((size_t)norm_bwd_workgroups(rows, d) * 2 * d * sizeof(float), 256);
+}
+
+int dp_op_layernorm_bwd(int dtype, int sum_f32, int rows, int d, const void* dy, int lddy, const void* sum, int lds, const float* mean,
+                        const float* rstd, const void* gamma, const void* dsum_in, int ldi, float p, const uint64_t* rng, uint32_t site,
+                        uint32_t first_row, void* dsum, int ldds, void* dx, int lddx, float* dgamma, float* dbeta, int accumulate, void* workspace,
+                        size_t workspace_bytes, void* hip_stream) {
+  const char* who = "dp_op_layernorm_bwd";
+  if (dtype != DP_F32 && dtype != DP_BF16) return set_error(DP_EINVAL, "unknown dtype");
+  if (rows < 0 || d <= 0) return set_errorf(DP_EINVAL, "%s: bad size", who);
+  if (d > NORM_MAX_D) return set_errorf(DP_EUNSUPPORTED, "%s: rows of at most %d columns", who, NORM_MAX_D);
+  if (norm_too_many(rows, d)) return set_errorf(DP_EUNSUPPORTED, "%s: too many rows", who);
+  NormBwdK k{rows, d, dy, lddy, sum, lds, mean, rstd, gamma, dsum_in, ldi, dsum, ldds, dx, lddx, nullptr, {}};
+  DP_TRY(make_drop(p, rng, site, first_row, who, k.drop));
+  if (rows > 0) {
+    DP_TRY(check_rows(dy, lddy, d, who, "dy"));
+    DP_TRY(check_rows(sum, lds, d, who, "sum"));
+    DP_TRY(check_ptr(mean, "mean")); DP_TRY(check_ptr(rstd, "rstd"));
+    if (dsum_in) DP_TRY(check_rows(dsum_in, ldi, d, who, "dsum_in"));
+    if (dsum) DP_TRY(check_rows(dsum, ldds, d, who, "dsum"));
+    if (dx) DP_TRY(check_rows(dx, lddx, d, who, "dx"));
+    if (!dsum && !dx) return set_errorf(DP_EINVAL, "%s: neither dsum nor dx is wanted", who);
+  }
+  DP_TRY(check_vec(gamma, who, "gamma")); DP_TRY(check_vec(dgamma, who, "dgamma")); DP_TRY(check_vec(dbeta, who, "dbeta"));
+  hipStream_t s = (hipStream_t)hip_stream;
+  const int workgroups = rows > 0 ? norm_bwd_workgroups(rows, d) : 0, es = dtype == DP_BF16 ? 2 : 4, ss = dtype == DP_F32 || sum_f32 ? 4 : 2;
+  if (rows > 0 && (dgamma || dbeta)) {
+    const size_t need = dp_op_layernorm_bwd_workspace_bytes(rows, d);
+    DP_TRY(check_ptr(workspace, "workspace", 256));
+    if (workspace_bytes < need) return set_errorf(DP_EWORKSPACE, "%s: workspace too small (%zu bytes, needs %zu)", who, workspace_bytes, need);
+    k.partial = (float*)workspace;
+  }
+  if (rows > 0) {
+    KScope ks(KK_LN_BWD, 0.0, (double)rows * d * (es + ss + (dsum_in ? ss : 0) + (dsum ? ss : 0) + (dx ? es : 0)) + 8.0 * rows, s, rows, d);
+    if (dtype == DP_F32) DP_TRY((norm_bwd_t<float, float>(k, workgroups, s)));
+    else if (sum_f32) DP_TRY((norm_bwd_t<bf16, float>(k, workgroups, s)));
+    else DP_TRY((norm_bwd_t<bf16, bf16>(k, workgroups, s)));
+  }
+  if (!dgamma && !dbeta) return DP_OK;
+  KScope ks(KK_REDUCE, 0.0, (double)workgroups * 2 * d * 4, s, workgroups, d);
+  hipLaunchKernelGGL(norm_bwd_reduce_kernel, dim3((2 * d + 7) / 8), dim3(256), 0, s, k.partial, workgroups, d, dgamma, dbeta, accumulate != 0);
+  return launched(who);
+}
+
+}  // extern "C"

@@ -1,0 +1,264 @@
+"""Dropout and the LayerNorm operators against their definition in 64 bits: widths where the kernels change their shape, ragged rows and
+strides, infinities and NaN in dropped places, slices of a batch, captured graphs whose step moves on.
+
+Bounds are elementwise.  h(T) is half a step of the output's type, u = 2^-24.  Dropout: the factor, the product and the sum are each rounded once, 3 u of the terms
+behind h(T) of the result.  LayerNorm: a lane adds at most 16 terms and 10 partial sums are joined behind it, so a row's sum is off by at most 26 u of the sum of
+magnitudes; the mean, the centred values, their squares, the root and the two products add a few u: 64 u of the magnitudes of the terms bounds
+all of it.  Gradients of the gains are sums over rows: a lane adds rows / (rows at a time) of them, then at most 4 + 32 + 32 partial sums: (rows + 80) u.
+"""
+import numpy as np
+import pytest
+
+from oracle import training_ops as T
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+SEED, STEP, SITE = 0x0123456789ABCDEF, 41, 7
+
+
+def _half(t):
+    import torch
+    return torch.finfo(t).eps / 2
+
+
+def _types(dtype):
+    import torch
+    from paper_2405_01248_amd import binding as B
+    return (B.DP_F32, torch.float32) if dtype == "f32" else (B.DP_BF16, torch.bfloat16)
+
+
+def _rng(seed=SEED, step=STEP):
+    import torch
+    return torch.tensor([seed, step], dtype=torch.int64, device="cuda")
+
+
+def _rows(g, rows, cols, ld, t, mean=0.0, std=1.0):
+    """[rows, cols] on the device with row stride ld (NaN between the rows), and its values in 64 bits."""
+    import torch
+    x = torch.full((rows, ld), float("nan"), dtype=t, device="cuda")
+    x[:, :cols] = torch.from_numpy(g.normal(mean, std, size=(rows, cols))).to(t).cuda()
+    return x, x[:, :cols].double().cpu().numpy()
+
+
+def _out(rows, cols, ld, t):
+    import torch
+    return torch.full((rows, ld), 7.0, dtype=t, device="cuda")
+
+
+def _get(x, cols):
+    assert (x[:, cols:].float() == 7.0).all()      # what lies between the rows is left as it was
+    return x[:, :cols].double().cpu().numpy()
+
+
+def _close(got, want, bound):
+    err = np.abs(got - want)
+    assert np.isfinite(got).all()
+    assert (err <= bound).all(), (float((err / np.maximum(bound, 1e-300)).max()), np.unravel_index((err - bound).argmax(), err.shape))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols,pad,p,residual", [
+    (1, 1, 0, 0.5, False), (3, 7, 2, 0.1, True), (5, 8, 0, 0.25, True), (129, 1000, 0, 0.1, False), (33, 1001, 3, 0.9, True),
+    (600, 4096, 8, 0.1, True), (2, 70001, 0, 0.3, True), (77, 64, 0, 0.0, True), (7, 40, 0, 1.0, True), (40000, 9, 0, 0.1, False)])
+def test_dropout(dtype, rows, cols, pad, p, residual):
+    import torch
+    from paper_2405_01248_amd import binding as B
+    dt, t = _types(dtype)
+    g = np.random.default_rng(rows * 7919 + cols)
+    x, xv = _rows(g, rows, cols, cols + pad, t)
+    r, rv = _rows(g, rows, cols, cols + 2 * pad, t)
+    y = _out(rows, cols, cols + pad, t)
+    B.op_dropout(dt, rows, cols, x, cols + pad, r if residual else None, cols + 2 * pad, p, _rng() if p else None, SITE, 5, y, cols + pad)
+    torch.cuda.synchronize()
+    keep = T.keep_mask(rows, cols, p, SEED, STEP, SITE, 5)
+    dropped = T.dropout(xv, keep, p)
+    want = dropped + (rv if residual else 0.0)
+    got = _get(y, cols)
+    _close(got, want, _half(t) * np.abs(want) + 3.01 * U * (np.abs(dropped) + np.abs(rv if residual else 0.0)))
+    assert (got[~keep] == (rv if residual else np.zeros_like(rv))[~keep]).all()
+
+
+def test_dropped_elements_contribute_zero_whatever_they_hold():
+    import torch
+    from paper_2405_01248_amd import binding as B
+    keep = T.keep_mask(64, 100, 0.5, SEED, STEP, SITE)
+    x = torch.ones((64, 100), device="cuda")
+    x[torch.from_numpy(~keep).cuda()] = torch.tensor([float("nan"), float("inf"), -float("inf")], device="cuda").repeat(64 * 100)[:int((~keep).sum())]
+    y = torch.empty_like(x)
+    B.op_dropout(B.DP_F32, 64, 100, x, 100, None, 0, 0.5, _rng(), SITE, 0, y, 100)
+    assert torch.equal(y.cpu(), torch.from_numpy(2.0 * keep).float())
+    B.op_dropout(B.DP_F32, 64, 100, x, 100, x, 100, 0.5, _rng(), SITE, 0, x, 100)      # in place, onto itself
+    assert (x[torch.from_numpy(keep).cuda()] == 3.0).all()
+
+
+def test_slices_and_the_backward_draw_the_same_mask():
+    import torch
+    from paper_2405_01248_amd import binding as B
+    x = torch.randn((96, 200), device="cuda")
+    whole, parts, dx = torch.empty_like(x), torch.empty_like(x), torch.empty_like(x)
+    first = 0xFFFFFFD0      # row numbers that wrap
+    B.op_dropout(B.DP_F32, 96, 200, x, 200, None, 0, 0.3, _rng(), SITE, first, whole, 200)
+    for a, b in ((0, 1), (1, 50), (50, 96)):
+        B.op_dropout(B.DP_F32, b - a, 200, x[a:b], 200, None, 0, 0.3, _rng(), SITE, (first + a) & 0xFFFFFFFF, parts[a:b], 200)
+    B.op_dropout(B.DP_F32, 96, 200, torch.ones_like(x), 200, None, 0, 0.3, _rng(), SITE, first, dx, 200)
+    assert torch.equal(whole, parts)
+    keep = T.keep_mask(96, 200, 0.3, SEED, STEP, SITE, first)
+    assert torch.equal((dx != 0).cpu(), torch.from_numpy(keep)) and torch.equal(whole != 0, dx != 0)
+
+
+SHAPES = [  # rows, d, padding of the rows
+    (5, 1, 0), (40, 8, 0), (37, 120, 8), (3, 129, 1), (65, 250, 0), (64, 256, 0), (9, 511, 5), (130, 640, 0), (1, 768, 0), (924, 768, 0), (31, 1001, 0),
+    (17, 1032, 8), (6, 2047, 0), (5, 4099, 0), (3, 8192, 0), (2, 8185, 3), (2500, 72, 0)]
+
+
+@pytest.mark.parametrize("dtype,sum_f32", [("f32", False), ("bf16", False), ("bf16", True)])
+@pytest.mark.parametrize("rows,d,pad", SHAPES)
+@pytest.mark.parametrize("p,residual,affine", [(0.1, True, True), (0.0, False, True), (0.5, True, False)])
+def test_layernorm(dtype, sum_f32, rows, d, pad, p, residual, affine):
+    import torch
+    from paper_2405_01248_amd import binding as B
+    dt, t = _types(dtype)
+    st = torch.float32 if sum_f32 else t
+    ld, eps = d + pad, 1e-5
+    g = np.random.default_rng(rows * 8191 + d)
+    x, xv = _rows(g, rows, d, ld, t)
+    r, rv = _rows(g, rows, d, ld, st, 0.5, 2.0)
+    gamma, gv = (w[0] for w in _rows(g, 1, d, d, t, 1.0, 0.3))
+    beta, bv = (w[0] for w in _rows(g, 1, d, d, t, 0.0, 0.3))
+    if not affine:
+        gamma = beta = None
+        gv, bv = np.ones(d), np.zeros(d)
+    y, sm = _out(rows, d, ld, t), _out(rows, d, ld, st)
+    mean, rstd = (torch.empty(rows, device="cuda") for _ in range(2))
+    rng = _rng() if p else None
+    B.op_layernorm_fwd(dt, sum_f32, rows, d, eps, x, ld, r if residual else None, ld, p, rng, SITE, 3, gamma, beta, sm, ld, y, ld, mean, rstd)
+    torch.cuda.synchronize()
+    keep = T.keep_mask(rows, d, p, SEED, STEP, SITE, 3)
+    drop = T.dropout(xv, keep, p)
+    s = drop + (rv if residual else 0.0)
+    want, wm, wr = T.layernorm_fwd(s, gv, bv, eps)
+    mag = np.abs(drop) + (np.abs(rv) if residual else 0.0)
+    _close(_get(sm, d), s, _half(st) * np.abs(s) + 3.01 * U * mag)
+    gm, gr = mean.double().cpu().numpy(), rstd.double().cpu().numpy()
+    scale = mag.mean(1)
+    _close(gm, wm, 64 * U * scale)
+    _close(gr, wr, 64 * U * wr * (1 + scale * wr))
+    spread = (mag + scale[:, None]) * wr[:, None]
+    ybound = 64 * U * (spread * (1 + scale * wr)[:, None] * np.abs(gv) + np.abs(bv))
+    _close(_get(y, d), want, _half(t) * (np.abs(want) + ybound) + ybound)
+
+    # backward, from the sum as it was stored
+    dy, dyv = _rows(g, rows, d, ld, t)
+    di, div = _rows(g, rows, d, ld, st)
+    ds, dx = _out(rows, d, ld, st), _out(rows, d, ld, t)
+    dg, db = (torch.full((d,), 2.0, device="cuda") for _ in range(2))
+    ws = torch.empty(B.op_layernorm_bwd_workspace_bytes(rows, d), dtype=torch.uint8, device="cuda")
+    bwd = lambda dsum, dxo, dgo, dbo, acc: B.op_layernorm_bwd(  # noqa: E731
+        dt, sum_f32, rows, d, dy, ld, sm, ld, mean, rstd, gamma, di if residual else None, ld, p, rng, SITE, 3, dsum, ld, dxo, ld, dgo, dbo, acc, ws)
+    bwd(ds, dx, dg, db, False)
+    torch.cuda.synchronize()
+    sv = _get(sm, d)
+    wds, wdg, wdb = T.layernorm_bwd(dyv, sv, gm, gr, gv)
+    if residual:
+        wds = wds + div
+    xh = np.abs((sv - gm[:, None]) * gr[:, None]) + (np.abs(sv) + np.abs(gm)[:, None]) * gr[:, None]
+    gy = np.abs(dyv * gv)
+    bound = 64 * U * (gr[:, None] * (gy + gy.mean(1, keepdims=True) + xh * (gy * xh).mean(1, keepdims=True)) + (np.abs(div) if residual else 0.0))
+    _close(_get(ds, d), wds, _half(st) * (np.abs(wds) + bound) + bound)
+    t_ = T.dropout_threshold(p)
+    up = 65536.0 / (65536 - t_)
+    wdx = T.dropout(wds, keep, p)
+    _close(_get(dx, d), wdx, (_half(t) + 2 * U) * (np.abs(wdx) + up * bound) + up * bound * keep)
+    n = (rows + 80) * U
+    _close(dg.double().cpu().numpy(), wdg, n * (np.abs(dyv) * xh).sum(0))
+    _close(db.double().cpu().numpy(), wdb, n * np.abs(dyv).sum(0))
+    # the same bits again, into other combinations of outputs; gains added up
+    dg2, ds2, dx2 = dg.clone(), _out(rows, d, ld, st), _out(rows, d, ld, t)
+    bwd(ds2, None, dg2, None, True)
+    assert torch.equal(ds2, ds) and torch.equal(dg2, dg + dg)
+    bwd(None, dx2, None, None, False)
+    assert torch.equal(dx2, dx)
+
+
+def test_layernorm_of_a_large_offset_and_a_constant_row():
+    # rows far from zero: the centred values are formed before they are squared; a constant row has variance zero
+    import torch
+    from paper_2405_01248_amd import binding as B
+    x = torch.randn((4, 640), device="cuda") + 1000.0
+    x[1] = 5.0
+    y, mean, rstd = torch.empty_like(x), torch.empty(4, device="cuda"), torch.empty(4, device="cuda")
+    B.op_layernorm_fwd(B.DP_F32, False, 4, 640, 1e-5, x, 640, None, 0, 0.0, None, 0, 0, None, None, None, 0, y, 640, mean, rstd)
+    want, _, wr = T.layernorm_fwd(x.double().cpu().numpy(), None, None, 1e-5)
+    mag = np.abs(x.double().cpu().numpy()) * wr[:, None]
+    mag[1] = 5.0 * wr[1]
+    _close(y.double().cpu().numpy(), want, 64 * U * (mag + np.abs(want)))
+
+
+def test_layernorm_in_place_and_empty():
+    import torch
+    from paper_2405_01248_amd import binding as B
+    x = torch.randn((50, 320), device="cuda").bfloat16()
+    r = torch.randn((50, 320), device="cuda")
+    gamma, beta = torch.ones(320, device="cuda").bfloat16(), torch.zeros(320, device="cuda").bfloat16()
+    y, sm, mean, rstd = torch.empty_like(x), torch.empty_like(r), torch.empty(50, device="cuda"), torch.empty(50, device="cuda")
+    fwd = lambda xx, rr, ss, yy, rows=50: B.op_layernorm_fwd(B.DP_BF16, True, rows, 320, 1e-5, xx, 320, rr, 320, 0.2, _rng(), 1, 0, gamma, beta, ss, 320, yy, 320, mean, rstd)  # noqa: E731
+    fwd(x, r, sm, y)
+    x2, r2 = x.clone(), r.clone()
+    fwd(x2, r2, r2, x2)
+    assert torch.equal(x2, y) and torch.equal(r2, sm)
+    ws = torch.empty(B.op_layernorm_bwd_workspace_bytes(50, 320), dtype=torch.uint8, device="cuda")
+    dy, di = torch.randn_like(x), torch.randn_like(r)
+    ds, dx, dg, db = torch.empty_like(r), torch.empty_like(x), torch.empty(320, device="cuda"), torch.empty(320, device="cuda")
+    bwd = lambda dyy, dii, dss, dxx, rows=50: B.op_layernorm_bwd(B.DP_BF16, True, rows, 320, dyy, 320, sm, 320, mean, rstd, gamma, dii, 320, 0.2, _rng(), 1, 0, dss, 320, dxx, 320, dg, db, False, ws)  # noqa: E731
+    bwd(dy, di, ds, dx)
+    dy2, di2 = dy.clone(), di.clone()
+    bwd(dy2, di2, di2, dy2)
+    assert torch.equal(dy2, dx) and torch.equal(di2, ds)
+    before = y.clone()
+    fwd(x, r, sm, y, 0)
+    assert torch.equal(y, before)
+    bwd(dy, di, ds, dx, 0)
+    assert (dg == 0).all() and (db == 0).all()
+
+
+def test_captured_steps_draw_new_masks_and_agree_with_eager_calls():
+    import torch
+    from paper_2405_01248_amd import binding as B
+    rows, d = 300, 640
+    x, r = torch.randn((rows, d), device="cuda").bfloat16(), torch.randn((rows, d), device="cuda")
+    gamma, beta = torch.randn(d, device="cuda").bfloat16(), torch.randn(d, device="cuda").bfloat16()
+    rng = _rng()
+
+    def buffers():
+        e = lambda t, *s: torch.empty(s, dtype=t, device="cuda")  # noqa: E731
+        return {"sum": e(torch.float32, rows, d), "y": e(torch.bfloat16, rows, d), "mean": e(torch.float32, rows), "rstd": e(torch.float32, rows),
+                "ds": e(torch.float32, rows, d), "dx": e(torch.bfloat16, rows, d), "dg": e(torch.float32, d), "db": e(torch.float32, d), "z": e(torch.bfloat16, rows, d),
+                "ws": e(torch.uint8, B.op_layernorm_bwd_workspace_bytes(rows, d))}
+
+    def step(b):
+        B.op_layernorm_fwd(B.DP_BF16, True, rows, d, 1e-5, x, d, r, d, 0.1, rng, 1, 0, gamma, beta, b["sum"], d, b["y"], d, b["mean"], b["rstd"])
+        B.op_dropout(B.DP_BF16, rows, d, b["y"], d, x, d, 0.1, rng, 2, 0, b["z"], d)
+        B.op_layernorm_bwd(B.DP_BF16, True, rows, d, b["z"], d, b["sum"], d, b["mean"], b["rstd"], gamma, None, 0, 0.1, rng, 1, 0, b["ds"], d, b["dx"], d,
+                           b["dg"], b["db"], False, b["ws"])
+
+    cap, eager = buffers(), buffers()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(cap)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(cap)
+    last = None
+    for s in (41, 42, 43, 42):
+        rng[1] = s
+        graph.replay()
+        step(eager)
+        torch.cuda.synchronize()
+        for n in cap:
+            if n != "ws":
+                assert torch.equal(cap[n], eager[n]), n
+        assert last is None or not torch.equal(last, cap["dx"])
+        last = cap["dx"].clone()

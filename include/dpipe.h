@@ -462,6 +462,39 @@ int dp_op_attention_bwd(int dtype, int B, int H, int Nq, int Nk, int d_head, flo
                         int ldk, const void* v, int ldv, const void* o, int ldo, const float* lse, const void* d_o, int lddo,
                         float* delta, void* dq, int lddq, void* dk, int lddk, void* dv, int lddv, void* hip_stream);
 
+/* Attention with a learned relative position bias: per (batch, head)
+ *   S = Q K^T * scale + table[bucket(key position - query position), head],   O = softmax(S) V,   lse = log of the softmax's sums.
+ * Key j has position j, query i position query0 + i (a decoder's new tokens: the number of tokens before them).  Buckets as text encoders with
+ * a bucketed bias define them: with half = n / 2 of the n buckets of one direction, distances 0 .. half - 1 have one each, and bucket half + k
+ * begins at the least distance d for which d >= half (max_distance / half)^(k / (n - half)), compared exactly; the last has no end.  bidirectional:
+ * each direction has half of n_buckets, keys behind the query the second half; else all are for keys up to the query, and keys behind it
+ * share bucket 0.  dp_relative_bucket (host) returns the bucket of distance = key position - query position, or an error code.
+ *   table    [device] [n_buckets, H] in the storage dtype; n_buckets 2 .. 512 (even, at least 4, if bidirectional), max_distance above half, at most 1024.
+ *            An entry may be -infinity: its pairs are masked.
+ *   key_len  [device] int32 [B] or NULL: sample b has keys 0 .. key_len[b] - 1 (taken as at least 0 and at most Nk).  Keys and values behind are not
+ *            read; the backward writes zeros for their gradients.
+ *   causal   query i sees keys j <= query0 + i only
+ * A query that sees no key has the output zero and lse = -infinity, and contributes nothing to the gradients.  Layout of q, k, v, o, lse as in
+ * dp_op_attention_fwd; lse may be NULL in the forward.  The backward takes o and lse of the forward and writes dq, dk, dv and, unless NULL, the
+ * table's gradient dtable, fp32 [n_buckets, H], overwritten or added to with accumulate.  Sums are in a fixed order: equal calls give equal bits.
+ * d_head at most 96; d_head and row strides multiples of 8 (bf16) or 4 (fp32); scale within [1e-6, 1e6]; each operand's rows of one sample
+ * below 2 GiB; pointers 16-byte aligned (key_len 4).  Outputs may not overlap inputs.
+ * workspace: dp_op_attention_relbias_workspace_bytes bytes, 256-byte aligned, needed by the backward; the forward uses it where it splits the keys of few
+ * queries, and runs without it (NULL) unsplit.  Calls that may overlap need workspaces of their own. */
+typedef struct {
+  const void* table;
+  int n_buckets, max_distance, bidirectional, query0;
+} dp_relbias;
+int dp_relative_bucket(int n_buckets, int max_distance, int bidirectional, int distance);
+size_t dp_op_attention_relbias_workspace_bytes(int B, int H, int Nq, int Nk, int d_head, int n_buckets, int backward);
+int dp_op_attention_relbias_fwd(int dtype, int B, int H, int Nq, int Nk, int d_head, int causal, float scale, const void* q, int ldq, const void* k,
+                                int ldk, const void* v, int ldv, const dp_relbias* bias, const int32_t* key_len, void* o, int ldo, float* lse,
+                                void* workspace, size_t workspace_bytes, void* hip_stream);
+int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_head, int causal, float scale, const void* q, int ldq, const void* k,
+                                int ldk, const void* v, int ldv, const dp_relbias* bias, const int32_t* key_len, const void* o, int ldo,
+                                const float* lse, const void* d_o, int lddo, void* dq, int lddq, void* dk, int lddk, void* dv, int lddv, float* dtable,
+                                int accumulate, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Dropout, and LayerNorm behind a dropout and a residual sum, for training: the end of a transformer sub-layer.
  *
  * No mask is stored.  Whether an element is kept follows from its position alone: the Philox4x32-10 generator, called with the counter

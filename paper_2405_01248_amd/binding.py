@@ -51,6 +51,15 @@ class LayerCost(C.Structure):
         return {n: getattr(self, n) for n, _ in self._fields_}
 
 
+class RelBias(C.Structure):
+    """dp_relbias: the bias table (a device tensor, kept alive here) and how positions map to its rows."""
+    _fields_ = [("table", C.c_void_p)] + [(n, C.c_int) for n in ("n_buckets", "max_distance", "bidirectional", "query0")]
+
+    def __init__(self, table, n_buckets, max_distance, bidirectional, query0=0):
+        super().__init__(_ptr(table), n_buckets, max_distance, int(bidirectional), query0)
+        self.tensor = table
+
+
 DP_MAX_STAGES = 64
 
 
@@ -111,7 +120,8 @@ EXPORTS = ["dp_stage_create", "dp_stage_destroy", "dp_stage_set_overlap", "dp_st
            "dp_encoder_profile", "dp_image_encoder_create", "dp_image_encoder_destroy", "dp_image_encoder_param_count",
            "dp_image_encoder_param_shape", "dp_image_encoder_layer_shape", "dp_image_encoder_workspace_bytes", "image_encoder_fwd_partial",
            "dp_image_encoder_profile", "dp_ktime_begin", "dp_ktime_end", "dp_ktime_event_overhead_ms", "dp_last_error", "dp_op_gemm", "dp_op_gemm_fp8", "dp_op_quantize_fp8", "dp_op_gemm_static", "dp_op_gemm_workspace_bytes",
-           "dp_op_attention_fwd", "dp_op_attention_bwd", "dp_op_dropout", "dp_op_layernorm_fwd", "dp_op_layernorm_bwd",
+           "dp_op_attention_fwd", "dp_op_attention_bwd", "dp_relative_bucket", "dp_op_attention_relbias_workspace_bytes", "dp_op_attention_relbias_fwd", "dp_op_attention_relbias_bwd",
+           "dp_op_dropout", "dp_op_layernorm_fwd", "dp_op_layernorm_bwd",
            "dp_op_layernorm_bwd_workspace_bytes", "dp_partition_solve", "dp_partition_solve_bidirectional", "dp_bubbles_1f1b", "dp_bubbles_fill", "dp_schedule_search"]
 
 
@@ -165,6 +175,11 @@ def load_library():
     lib.dp_op_gemm_static.argtypes = [i, vp, i, i, vp, i, i, i, i, i, vp, vp, i, i, i, i, vp]
     lib.dp_op_attention_fwd.argtypes = [i, i, i, i, i, i, i, f, vp, i, vp, i, vp, i, vp, i, vp, vp]
     lib.dp_op_attention_bwd.argtypes = [i, i, i, i, i, i, f, vp, i, vp, i, vp, i, vp, i, vp, vp, i, vp, vp, i, vp, i, vp, i, vp]
+    rel = C.POINTER(RelBias)
+    lib.dp_relative_bucket.argtypes = [i, i, i, i]
+    lib.dp_op_attention_relbias_workspace_bytes.argtypes = [i] * 7; lib.dp_op_attention_relbias_workspace_bytes.restype = sz
+    lib.dp_op_attention_relbias_fwd.argtypes = [i] * 7 + [f, vp, i, vp, i, vp, i, rel, vp, vp, i, vp, vp, sz, vp]
+    lib.dp_op_attention_relbias_bwd.argtypes = [i] * 7 + [f, vp, i, vp, i, vp, i, rel, vp, vp, i, vp, vp, i, vp, i, vp, i, vp, i, vp, i, vp, sz, vp]
     u32 = C.c_uint32
     lib.dp_op_dropout.argtypes = [i, i, i, vp, i, vp, i, f, vp, u32, u32, vp, i, vp]
     lib.dp_op_layernorm_fwd.argtypes = [i, i, i, i, f, vp, i, vp, i, f, vp, u32, u32, vp, vp, vp, i, vp, i, vp, vp, vp]
@@ -535,3 +550,28 @@ def op_layernorm_bwd(dtype, sum_f32, rows, d, dy, lddy, sum_, lds, mean, rstd, g
     _check(load_library().dp_op_layernorm_bwd(dtype, int(sum_f32), rows, d, _ptr(dy), lddy, _ptr(sum_), lds, _ptr(mean), _ptr(rstd), _ptr(gamma),
                                               _ptr(dsum_in), ldi, p, _ptr(rng), site, first_row, _ptr(dsum), ldds, _ptr(dx), lddx, _ptr(dgamma),
                                               _ptr(dbeta), int(accumulate), _ptr(workspace), _nbytes(workspace), _stream(stream)))
+
+
+def relative_bucket(n_buckets, max_distance, bidirectional, distance):
+    rc = load_library().dp_relative_bucket(n_buckets, max_distance, int(bidirectional), distance)
+    if rc < 0:
+        _check(rc)
+    return rc
+
+
+def op_attention_relbias_workspace_bytes(B, H, Nq, Nk, d_head, n_buckets, backward):
+    return load_library().dp_op_attention_relbias_workspace_bytes(B, H, Nq, Nk, d_head, n_buckets, int(backward))
+
+
+def op_attention_relbias_fwd(dtype, B, H, Nq, Nk, d_head, causal, scale, q, ldq, k, ldk, v, ldv, bias, key_len, o, ldo, lse, workspace, stream=None):
+    _check(load_library().dp_op_attention_relbias_fwd(dtype, B, H, Nq, Nk, d_head, int(causal), scale, _ptr(q), ldq, _ptr(k), ldk, _ptr(v), ldv,
+                                                      C.byref(bias), _ptr(key_len), _ptr(o), ldo, _ptr(lse), _ptr(workspace), _nbytes(workspace),
+                                                      _stream(stream)))
+
+
+def op_attention_relbias_bwd(dtype, B, H, Nq, Nk, d_head, causal, scale, q, ldq, k, ldk, v, ldv, bias, key_len, o, ldo, lse, d_o, lddo, dq, lddq, dk,
+                             lddk, dv, lddv, dtable, accumulate, workspace, stream=None):
+    _check(load_library().dp_op_attention_relbias_bwd(dtype, B, H, Nq, Nk, d_head, int(causal), scale, _ptr(q), ldq, _ptr(k), ldk, _ptr(v), ldv,
+                                                      C.byref(bias), _ptr(key_len), _ptr(o), ldo, _ptr(lse), _ptr(d_o), lddo, _ptr(dq), lddq,
+                                                      _ptr(dk), lddk, _ptr(dv), lddv, _ptr(dtable), int(accumulate), _ptr(workspace),
+                                                      _nbytes(workspace), _stream(stream)))

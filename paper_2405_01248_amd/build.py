@@ -8,7 +8,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdpipe.so")
-SOURCES = ["gemm.hip", "gemm_dw.hip", "gemm_few_rows.hip", "gemm_f32.hip", "attention.hip", "elementwise.hip", "dropout_norm.hip", "stage.hip", "ktime.hip", "partition.hip", "bubbles.hip", "noalloc.hip", "conv.hip", "image_encoder.hip", "search.hip", "errors.hip"]
+SOURCES = ["gemm.hip", "gemm_dw.hip", "gemm_few_rows.hip", "gemm_f32.hip", "attention.hip", "attention_relbias.hip", "elementwise.hip", "dropout_norm.hip", "stage.hip", "ktime.hip", "partition.hip", "bubbles.hip", "noalloc.hip", "conv.hip", "image_encoder.hip", "search.hip", "errors.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 

@@ -1,0 +1,996 @@
+// Attention with a learned relative position bias, forward and backward: S = scale Q K^T + table[bucket(key - query), head] under key lengths and an
+// optional causal mask, O = softmax(S) V, and the gradients of Q, K, V and of the table.
+//
+// bf16: the tiles, operand layouts and splits of the kernels without a bias (dp_attention_tile.h): a wave owns 32 queries (forward, dQ) or 32 keys
+// (dK / dV), scores come out of the matrix instruction with one query (key) a lane, and the other side streams through LDS in tiles of 64.
+// The bias costs these loops no vector instruction.  What the accumulators of the scores are cleared with otherwise is the bias over the scale:
+//   - bias over distance lies in LDS (fp32) from the last distance at which the bucket still changes to the other one, and 96 distances
+//     of the end buckets beyond either, as far as a tile that touches the middle reaches;
+//   - four neighbouring accumulator registers are four neighbouring distances, so they are one 16-byte read; as its address is a multiple of four
+//     distances only for one lane in four, the table lies there four times, each copy one distance further on;
+//   - a tile of 64 keys and 32 queries outside of the middle lies in one bucket: its accumulators begin with a constant.
+// The table's gradient, the sum of dS over the pairs of a bucket: in the middle a wave adds dS to sums over distances in LDS, an atomic addition per register
+// whose address is constant but for the lane; no two lanes of one instruction and no two waves share an address, so the order of
+// additions is the program's and the result the same bits every time.  Beyond the middle each lane adds to one sum per side.  The sums over distances become
+// sums over buckets at the end of the workgroup, and a second kernel adds those of all samples and query tiles in their order.
+#include "dp_attention_tile.h"
+#include "dp_device.h"
+#include "dp_errors.h"
+#include "dp_host.h"
+#include "dp_kernels.h"
+#include "dp_ktime.h"
+
+#include <math.h>
+#include <algorithm>
+#include <atomic>
+#include <type_traits>
+#include <vector>
+
+namespace dp {
+
+constexpr int REL_MAX_BUCKETS = 512, REL_MAX_DISTANCE = 1024, REL_MARGIN = 96;
+
+struct RelBucketsK {
+  int n_buckets, per_side, half;      // buckets in all, of one direction, of one distance each
+  int bidirectional;
+  int lo, hi;                         // the bucket of every distance <= lo is lo's, of every one >= hi is hi's
+};
+// Least distance of bucket half + k.  A kernel argument of its own, which each workgroup copies to LDS: indexed by lane inside the other arguments, it would
+// send all of them through scratch memory.
+struct RelStarts { uint16_t of[REL_MAX_BUCKETS / 2]; };
+
+struct RelAttnK {
+  int B, H, Nq, Nk, dh, causal, query0;
+  float scale, scale_log2, inv_scale;
+  const void* q; int ldq;
+  const void* k; int ldk;
+  const void* v; int ldv;
+  const void* table;
+  const int* key_len;
+  void* o; int ldo;
+  float* lse;
+  const void* dout; int lddo;
+  float* delta;
+  void* dq; int lddq;
+  void* dk; int lddk;
+  void* dv; int lddv;
+  float* dtable_partial;      // [head][sample and query tile][bucket]
+  int even;
+  RelBucketsK bk;
+};
+
+__device__ __forceinline__ void rel_copy_starts(const RelBucketsK& r, const RelStarts& st, uint16_t* start, int threads) {
+  for (int k = threadIdx.x; k < r.per_side - r.half; k += threads) start[k] = st.of[k];
+  __syncthreads();
+}
+__device__ __forceinline__ int rel_bucket(const RelBucketsK& r, const uint16_t* start, int dist) {
+  const int n = r.bidirectional ? abs(dist) : max(-dist, 0), side = r.bidirectional && dist > 0 ? r.per_side : 0;
+  if (n < r.half) return side + n;
+  int k = 0, end = r.per_side - r.half;      // the last k whose start is not above n
+  while (end - k > 1) {
+    const int mid = (k + end) / 2;
+    if (start[mid] <= n) k = mid;
+    else end = mid;
+  }
+  return side + r.half + k;
+}
+__host__ __device__ __forceinline__ int rel_entries(const RelBucketsK& r) { return r.hi - r.lo + 1 + 2 * REL_MARGIN; }
+// floats from one copy to the next: neighbouring lanes read neighbouring copies, 16 banks apart
+__host__ __device__ __forceinline__ int rel_copy_stride(const RelBucketsK& r) { return (rel_entries(r) + 63) / 64 * 64 + 16; }
+__host__ __device__ __forceinline__ int rel_table_bytes(const RelBucketsK& r) { return 4 * rel_copy_stride(r) * (int)sizeof(float); }
+__device__ __forceinline__ int rel_keys(const RelAttnK& p, int b) { return p.key_len ? max(0, min(p.key_len[b], p.Nk)) : p.Nk; }
+
+// Bias over scale of head h by distance, copy c beginning with entry c.  Entry e is distance lo - margin + e, or, REVERSED, hi + margin - e.
+template <typename T, bool REVERSED>
+__device__ __forceinline__ void rel_fill(const RelAttnK& p, const uint16_t* start, int h, float* tab, int threads) {
+  const int n = rel_entries(p.bk), stride = rel_copy_stride(p.bk);
+  for (int e = threadIdx.x; e < n; e += threads) {
+    const int dist = REVERSED ? p.bk.hi + REL_MARGIN - e : p.bk.lo - REL_MARGIN + e;
+    const float v = to_f<T>(((const T*)p.table)[(size_t)rel_bucket(p.bk, start, dist) * p.H + h]) * p.inv_scale;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      if (e >= c) tab[c * stride + e - c] = v;
+  }
+}
+// Where a lane finds entry `entry` and the three behind it; 4 k floats further on it is the same for entry + 4 k.  (Not a place in the table by
+// itself: only a tile that touches the middle reaches one.)
+__device__ __forceinline__ int rel_lane(const RelAttnK& p, int entry) {
+  const int c = entry & 3;
+  return c * rel_copy_stride(p.bk) + (entry - c);
+}
+
+// byte extent of n rows, which may be none
+__device__ __forceinline__ uint32_t rel_slice_bytes(int n, int ld, int dh) { return (uint32_t)__builtin_amdgcn_readfirstlane(n > 0 ? (int)attn_slice_bytes(n, ld, dh) : 0); }
+
+// ------------------------------------------------------------------ forward (bf16)
+// 128 queries a workgroup, keys in tiles of 64, two LDS stages; online softmax with a reference point that moves when the sum outgrows it (see
+// attn_fwd_bf16_kernel).  A query that sees no key keeps the reference -inf and the sum 0: zeros, and lse = -inf.
+template <int DHP, int KC, int MINW>
+__global__ void __launch_bounds__(256, MINW) rel_fwd_bf16_kernel(const RelAttnK p, const RelStarts st) {
+  __shared__ uint16_t start[REL_MAX_BUCKETS / 2];
+  constexpr int DT = DHP / 32, BQ = 128, TILE = 64 * DHP;
+  __shared__ __attribute__((aligned(1024))) bf16 Ks[2][TILE];
+  __shared__ __attribute__((aligned(1024))) bf16 Vs[2][TILE];
+  extern __shared__ __attribute__((aligned(16))) float rel_lds[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, l32 = lane & 31;
+  const int bk_lo = p.bk.lo, bk_hi = p.bk.hi;
+  int qtile, bh;
+  attn_block_map(blockIdx.x, (p.Nq + BQ - 1) / BQ, p.B * p.H, qtile, bh);
+  const int b = bh / p.H, h = bh % p.H;
+  const int q0 = qtile * BQ + wave * 32, qi = q0 + l32, pos0 = p.query0 + q0, pos = pos0 + l32;
+  const int keys = __builtin_amdgcn_readfirstlane(rel_keys(p, b));
+  const int lim = p.causal ? min(keys, pos + 1) : keys;                                   // keys that this lane's query sees
+  const int lim_all = p.causal ? min(keys, pos0 + 1) : keys;                              // ... that all queries of the wave see
+  const int lim_any = p.causal ? min(keys, p.query0 + min(p.Nq, qtile * BQ + BQ)) : keys;  // ... that some query of the workgroup sees
+  const int nkt = __builtin_amdgcn_readfirstlane(lim_any > 0 ? (lim_any + 63) / 64 : 0);
+  const bf16* qb = (const bf16*)p.q + (size_t)b * p.Nq * p.ldq + h * p.dh;
+  const u32x4 kr = make_raw_rsrc((const bf16*)p.k + (size_t)b * p.Nk * p.ldk + h * p.dh, rel_slice_bytes(keys, p.ldk, p.dh));
+  const u32x4 vr = make_raw_rsrc((const bf16*)p.v + (size_t)b * p.Nk * p.ldv + h * p.dh, rel_slice_bytes(keys, p.ldv, p.dh));
+
+  AttnFragOff<DHP, KC> fo;
+  fo.init(lane);
+  AttnTileCopy<DHP> ck, cv;
+  ck.init(wave, lane, p.ldk, p.dh);
+  cv.init(wave, lane, p.ldv, p.dh);
+  if (nkt > 0) {
+    ck.issue(kr, 0, p.ldk, Ks[0], wave);
+    cv.issue(vr, 0, p.ldv, Vs[0], wave);
+  }
+  rel_copy_starts(p.bk, st, start, 256);
+  rel_fill<bf16, false>(p, start, h, rel_lds, 256);
+  const int tab = rel_lane(p, 4 * g - pos - (bk_lo - REL_MARGIN));
+  bf16x8 qf[KC];
+#pragma unroll
+  for (int c = 0; c < KC; ++c) qf[c] = ld8(qb + (size_t)qi * p.ldq + 16 * c + 8 * g, qi < p.Nq && 16 * c + 8 * g < p.dh);
+  f32x16 oacc[DT];
+  float m = -INFINITY, lsum = 0.f;
+#pragma unroll
+  for (int i = 0; i < DT; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) oacc[i][r] = 0.f;
+  wait_vmcnt<0>();
+  __syncthreads();
+  const float far_lo = rel_lds[0], far_hi = rel_lds[rel_entries(p.bk) - 1];
+
+  for (int kt = 0; kt < nkt; ++kt) {
+    const int buf = kt & 1;
+    take_turns(p.even, kt);
+    if (kt + 1 < nkt) {      // every wave left stage buf ^ 1 at the barrier that ended the previous iteration
+      ck.issue(kr, (kt + 1) * 64, p.ldk, Ks[buf ^ 1], wave);
+      cv.issue(vr, (kt + 1) * 64, p.ldv, Vs[buf ^ 1], wave);
+    }
+    f32x16 s[2];
+    auto scores = [&]() __attribute__((always_inline)) {      // S^T = K Q^T + bias, over the scale
+      if (kt * 64 + 63 - pos0 > bk_lo && kt * 64 - pos0 - 31 < bk_hi) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int r4 = 0; r4 < 4; ++r4) {
+            const f32x4 v = *reinterpret_cast<const f32x4*>(rel_lds + (tab + kt * 64) + 32 * t + 8 * r4);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) s[t][4 * r4 + u] = v[u];
+          }
+      } else {
+        const float below = far_lo, above = far_hi, far = kt * 64 - pos0 - 31 < bk_hi ? below : above;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[t][r] = far;
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int c = 0; c < KC; ++c) s[t] = mfma32(fo.row_frag(Ks[buf], t, c), qf[c], s[t]);
+      if (kt * 64 + 64 > lim_all) {      // (one wave-uniform branch around a block of selects)
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[t][r] = kt * 64 + 32 * t + acc_row(r, g) < lim ? s[t][r] : -INFINITY;
+      }
+    };
+    float rs;
+    auto probabilities = [&]() __attribute__((always_inline)) {
+      const float mref = m == -INFINITY ? 0.f : m;
+      rs = 0.f;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float e = __builtin_amdgcn_exp2f(fmaf(s[t][r], p.scale_log2, -mref));
+          s[t][r] = e;
+          rs += e;
+        }
+    };
+    auto move_reference = [&]() __attribute__((always_inline)) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[t][r]);
+      mx = fmaxf(m, fmaf(reduce_halves(mx, MaxOp()), p.scale_log2, 8.0f));
+      if (kt > 0) {
+        const float alpha = __builtin_amdgcn_exp2f(m - (mx == -INFINITY ? 0.f : mx));
+        lsum *= alpha;
+#pragma unroll
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) oacc[i][r] *= alpha;
+      }
+      m = mx;
+    };
+    scores();
+    if (kt == 0) move_reference();
+    probabilities();
+    if (__any(!(rs <= 256.f) || m == -INFINITY)) {
+      if (kt > 0) {
+        scores();
+        move_reference();
+        probabilities();
+      }
+    }
+    lsum += rs;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)      // O^T += V^T P^T
+#pragma unroll
+      for (int cc = 0; cc < 2; ++cc) {
+        const bf16x8 pf = pack8(s[t], 8 * cc);
+#pragma unroll
+        for (int i = 0; i < DT; ++i) oacc[i] = mfma32(fo.tr_frag(Vs[buf], 32 * t + 16 * cc, i), pf, oacc[i]);
+      }
+    wait_vmcnt<0>();
+    __syncthreads();
+  }
+
+  lsum = reduce_halves(lsum, AddOp());      // (each lane summed its own keys)
+  if (qi >= p.Nq) return;
+  const float inv = lsum > 0.f ? 1.0f / lsum : (lsum == 0.f ? 0.f : lsum);      // (NaN stays)
+  bf16* ob = (bf16*)p.o + ((size_t)b * p.Nq + qi) * p.ldo + h * p.dh;
+#pragma unroll
+  for (int i = 0; i < DT; ++i)
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4) {
+      const int col = 32 * i + 8 * r4 + 4 * g;
+      if (col < p.dh) {
+        bf16x4 o;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) o[u] = (bf16)(oacc[i][4 * r4 + u] * inv);
+        *reinterpret_cast<bf16x4*>(ob + col) = o;
+      }
+    }
+  if (p.lse && g == 0) p.lse[((size_t)b * p.H + h) * p.Nq + qi] = lsum == 0.f ? -INFINITY : fmaf(m, LN2, logf(lsum));
+}
+
+// ------------------------------------------------------------------ dQ and the table's gradient (bf16)
+// Sums of dS over distances: [wave][half of the wave][entry].
+__host__ __device__ __forceinline__ int rel_sum_stride(const RelBucketsK& r) { return (rel_entries(r) + 63) / 64 * 64 + 32; }
+__host__ __device__ __forceinline__ int rel_sums_bytes(const RelBucketsK& r) { return 8 * rel_sum_stride(r) * (int)sizeof(float); }
+
+__device__ __forceinline__ void lds_add(float* p, float v) { __builtin_amdgcn_ds_faddf((DP_LDS float*)p, v, __ATOMIC_RELAXED, 2, false); }
+
+template <int DHP, int KC>
+__global__ void __launch_bounds__(256, DHP == 64 ? 3 : 2) rel_bwd_dq_bf16_kernel(const RelAttnK p, const RelStarts st) {
+  __shared__ uint16_t start[REL_MAX_BUCKETS / 2];
+  constexpr int DT = DHP / 32, TILE = 64 * DHP;
+  __shared__ __attribute__((aligned(1024))) bf16 Ks[2][TILE];
+  __shared__ __attribute__((aligned(1024))) bf16 Vs[2][TILE];
+  __shared__ float far_sums[2][4];
+  extern __shared__ __attribute__((aligned(16))) float rel_lds[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, l32 = lane & 31;
+  const int qtiles = (p.Nq + 127) / 128, entries = rel_entries(p.bk);
+  int qtile, bh;
+  attn_block_map(blockIdx.x, qtiles, p.B * p.H, qtile, bh);
+  const int b = bh / p.H, h = bh % p.H;
+  const int q0 = qtile * 128 + wave * 32, qi = q0 + l32, pos0 = p.query0 + q0, pos = pos0 + l32;
+  const bool qok = qi < p.Nq;
+  const int keys = __builtin_amdgcn_readfirstlane(rel_keys(p, b));
+  const int lim = p.causal ? min(keys, pos + 1) : keys, lim_all = p.causal ? min(keys, pos0 + 1) : keys;
+  const int lim_any = p.causal ? min(keys, p.query0 + min(p.Nq, qtile * 128 + 128)) : keys;
+  const int nkt = __builtin_amdgcn_readfirstlane(lim_any > 0 ? (lim_any + 63) / 64 : 0);
+  const u32x4 kr = make_raw_rsrc((const bf16*)p.k + (size_t)b * p.Nk * p.ldk + h * p.dh, rel_slice_bytes(keys, p.ldk, p.dh));
+  const u32x4 vr = make_raw_rsrc((const bf16*)p.v + (size_t)b * p.Nk * p.ldv + h * p.dh, rel_slice_bytes(keys, p.ldv, p.dh));
+  const bf16* qrow = (const bf16*)p.q + ((size_t)b * p.Nq + qi) * p.ldq + h * p.dh;
+  const bf16* dorow = (const bf16*)p.dout + ((size_t)b * p.Nq + qi) * p.lddo + h * p.dh;
+
+  AttnFragOff<DHP, KC> fo;
+  fo.init(lane);
+  AttnTileCopy<DHP> ck, cv;
+  ck.init(wave, lane, p.ldk, p.dh);
+  cv.init(wave, lane, p.ldv, p.dh);
+  if (nkt > 0) {
+    ck.issue(kr, 0, p.ldk, Ks[0], wave);
+    cv.issue(vr, 0, p.ldv, Vs[0], wave);
+  }
+  rel_copy_starts(p.bk, st, start, 256);
+  rel_fill<bf16, false>(p, start, h, rel_lds, 256);
+  float* sums = rel_lds + 4 * rel_copy_stride(p.bk);
+  const int sum_stride = rel_sum_stride(p.bk);
+  for (int e = tid; e < 8 * sum_stride; e += 256) sums[e] = 0.f;
+  const int entry = 4 * g - pos - (p.bk.lo - REL_MARGIN);
+  const int tab = rel_lane(p, entry);
+  const int mine = (2 * wave + g) * sum_stride + entry;
+  float far_sum_lo = 0.f, far_sum_hi = 0.f;
+
+  bf16x8 qf[KC], dof[KC];
+#pragma unroll
+  for (int c = 0; c < KC; ++c) {
+    const bool ok = qok && 16 * c + 8 * g < p.dh;
+    qf[c] = ld8(qrow + 16 * c + 8 * g, ok);
+    dof[c] = ld8(dorow + 16 * c + 8 * g, ok);
+  }
+  const size_t sidx = ((size_t)b * p.H + h) * p.Nq + qi;
+  float lse2 = INFINITY;      // of no query, and of one that sees no key: its probabilities are zero
+  if (qok) {
+    const float l = p.lse[sidx];
+    if (l != -INFINITY) lse2 = l * LOG2E;
+  }
+  float dlt = 0.f;      // delta = rowsum(dO * O), see attn_bwd_dq_bf16_kernel
+  {
+    const bf16* orow = (const bf16*)p.o + ((size_t)b * p.Nq + qi) * p.ldo + h * p.dh;
+#pragma unroll
+    for (int c = 0; c < KC; ++c) {
+      const bf16x8 of = ld8(orow + 16 * c + 8 * g, qok && 16 * c + 8 * g < p.dh);
+#pragma unroll
+      for (int u = 0; u < 8; ++u) dlt = fmaf((float)of[u], (float)dof[c][u], dlt);
+    }
+    dlt = reduce_halves(dlt, AddOp());
+    if (qok && g == 0) p.delta[sidx] = dlt;
+  }
+  f32x16 acc[DT];
+#pragma unroll
+  for (int i = 0; i < DT; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[i][r] = 0.f;
+  wait_vmcnt<0>();
+  __syncthreads();
+  const float far_lo = rel_lds[0], far_hi = rel_lds[entries - 1];
+
+  auto tile = [&](int kt, auto bc) {
+    take_turns(p.even, kt);
+    constexpr int buf = bc();
+    if (kt + 1 < nkt) {
+      ck.issue(kr, (kt + 1) * 64, p.ldk, Ks[buf ^ 1], wave);
+      cv.issue(vr, (kt + 1) * 64, p.ldv, Vs[buf ^ 1], wave);
+    }
+    const bool below = kt * 64 + 63 - pos0 <= p.bk.lo, above = kt * 64 - pos0 - 31 >= p.bk.hi;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      f32x16 s, dp;
+      if (below || above) {
+        const float far = below ? far_lo : far_hi;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = far;
+      } else {
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4) {
+          const f32x4 v = *reinterpret_cast<const f32x4*>(rel_lds + (tab + kt * 64) + 32 * t + 8 * r4);
+#pragma unroll
+          for (int u = 0; u < 4; ++u) s[4 * r4 + u] = v[u];
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) dp[r] = -dlt;      // dP - delta: the products accumulate onto -delta
+#pragma unroll
+      for (int c = 0; c < KC; ++c) {
+        s = mfma32(fo.row_frag(Ks[buf], t, c), qf[c], s);
+        dp = mfma32(fo.row_frag(Vs[buf], t, c), dof[c], dp);
+      }
+      if (kt * 64 + 64 > lim_all) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = kt * 64 + 32 * t + acc_row(r, g) < lim ? s[r] : -INFINITY;
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], p.scale_log2, -lse2)) * dp[r];
+      if (below || above) {
+        float sum = 0.f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sum += s[r];
+        if (below) far_sum_lo += sum;
+        else far_sum_hi += sum;
+      } else {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) lds_add(sums + (mine + kt * 64) + 32 * t + acc_row(r, 0), s[r]);
+      }
+#pragma unroll
+      for (int cc = 0; cc < 2; ++cc) {
+        const bf16x8 dsf = pack8(s, 8 * cc);
+#pragma unroll
+        for (int i = 0; i < DT; ++i) acc[i] = mfma32(fo.tr_frag(Ks[buf], 32 * t + 16 * cc, i), dsf, acc[i]);
+      }
+    }
+    wait_vmcnt<0>();
+    __syncthreads();
+  };
+  two_stages(0, nkt, tile);
+  if (qok) {
+    bf16* ob = (bf16*)p.dq + ((size_t)b * p.Nq + qi) * p.lddq + h * p.dh;
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        const int col = 32 * i + 8 * r4 + 4 * g;
+        if (col < p.dh) {
+          bf16x4 o;
+#pragma unroll
+          for (int u = 0; u < 4; ++u) o[u] = (bf16)(acc[i][4 * r4 + u] * p.scale);
+          *reinterpret_cast<bf16x4*>(ob + col) = o;
+        }
+      }
+  }
+  if (!p.dtable_partial) return;
+  // the eight sums of a distance, then the distances of a bucket: eight lanes each
+  far_sum_lo = wave_sum(far_sum_lo);
+  far_sum_hi = wave_sum(far_sum_hi);
+  if (lane == 0) { far_sums[0][wave] = far_sum_lo; far_sums[1][wave] = far_sum_hi; }
+  __syncthreads();
+  for (int e = tid; e < entries; e += 256) {
+    float v = sums[e];
+#pragma unroll
+    for (int w = 1; w < 8; ++w) v += sums[w * sum_stride + e];
+    sums[e] = v;
+  }
+  __syncthreads();
+  float* out = p.dtable_partial + ((size_t)h * p.B * qtiles + (size_t)b * qtiles + qtile) * p.bk.n_buckets;
+  const int first = p.bk.lo - REL_MARGIN, last = p.bk.hi + REL_MARGIN;
+  for (int bucket = tid / 8; bucket < (p.bk.n_buckets + 31) / 32 * 32; bucket += 32) {
+    const bool on = bucket < p.bk.n_buckets;
+    const int side = on && p.bk.bidirectional && bucket >= p.bk.per_side, k = on ? bucket - side * p.bk.per_side : 0;
+    auto first_of = [&](int i) { return i < p.bk.half ? i : (i < p.bk.per_side ? (int)start[i - p.bk.half] : 1 << 28); };
+    const int n0 = first_of(k), n1 = first_of(k + 1) - 1;      // distances n0 .. n1 of this direction
+    int d0, d1;
+    if (side) d0 = max(n0, 1), d1 = min(n1, last);
+    else d0 = max(-n1, first), d1 = -n0;
+    if (!p.bk.bidirectional && k == 0) d1 = last;        // keys behind the query
+    float v = 0.f;
+    if (on)
+      for (int d = d0 + tid % 8; d <= d1; d += 8) v += sums[d - first];
+    v += lane_dpp<0xB1>(v);       // lanes i ^ 1, i ^ 2, i ^ 7 (by then equal within four): the eight of a bucket
+    v += lane_dpp<0x4E>(v);
+    v += lane_dpp<0x141>(v);      // row_half_mirror
+    if (on && tid % 8 == 0) {
+      const int lo_bucket = p.bk.per_side - 1, hi_bucket = p.bk.bidirectional ? 2 * p.bk.per_side - 1 : 0;
+      if (bucket == lo_bucket) v += (far_sums[0][0] + far_sums[0][1]) + (far_sums[0][2] + far_sums[0][3]);
+      if (bucket == hi_bucket) v += (far_sums[1][0] + far_sums[1][1]) + (far_sums[1][2] + far_sums[1][3]);
+      out[bucket] = v;
+    }
+  }
+}
+
+// dtable[bucket][head] = sum over the parts, in their order: 32 buckets of a head a workgroup, eight shares of the parts.
+__global__ void __launch_bounds__(256) rel_dtable_kernel(const float* __restrict__ partial, int parts, int n_buckets, int H, float* __restrict__ dtable, int accumulate) {
+  __shared__ float meet[8][32];
+  const int h = blockIdx.x, lane = threadIdx.x % 32, share = threadIdx.x / 32, bucket = blockIdx.y * 32 + lane;
+  float s = 0.f;
+  if (bucket < n_buckets) {
+#pragma unroll 8
+    for (int i = share; i < parts; i += 8) s += partial[((size_t)h * parts + i) * n_buckets + bucket];
+  }
+  meet[share][lane] = s;
+  __syncthreads();
+  if (share || bucket >= n_buckets) return;
+#pragma unroll
+  for (int w = 1; w < 8; ++w) s += meet[w][lane];
+  float* out = dtable + (size_t)bucket * H + h;
+  *out = accumulate ? *out + s : s;
+}
+
+// ------------------------------------------------------------------ dK, dV (bf16)
+// Each wave owns 32 keys and walks the queries in tiles of 64, from the first that sees one of the workgroup's keys (see attn_bwd_dkv_bf16_kernel).
+template <int DHP, int KC, int MINW>
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(MINW, MINW))) rel_bwd_dkv_bf16_kernel(const RelAttnK p, const RelStarts st) {
+  __shared__ uint16_t start[REL_MAX_BUCKETS / 2];
+  constexpr int DT = DHP / 32, TILE = 64 * DHP;
+  __shared__ __attribute__((aligned(1024))) bf16 Qs[2][TILE];
+  __shared__ __attribute__((aligned(1024))) bf16 Ds[2][TILE];
+  __shared__ __attribute__((aligned(16))) float lse_s[2][64];
+  __shared__ __attribute__((aligned(16))) float dlt_s[2][64];
+  extern __shared__ __attribute__((aligned(16))) float rel_lds[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, l32 = lane & 31;
+  int ktile, bh;
+  attn_block_map(blockIdx.x, (p.Nk + 127) / 128, p.B * p.H, ktile, bh);
+  const int b = bh / p.H, h = bh % p.H;
+  const int k0 = ktile * 128 + wave * 32, ki = k0 + l32;
+  const int keys = __builtin_amdgcn_readfirstlane(rel_keys(p, b));
+  const bool kok = ki < keys;
+  const u32x4 qr = make_raw_rsrc((const bf16*)p.q + (size_t)b * p.Nq * p.ldq + h * p.dh, attn_slice_bytes(p.Nq, p.ldq, p.dh));
+  const u32x4 dr = make_raw_rsrc((const bf16*)p.dout + (size_t)b * p.Nq * p.lddo + h * p.dh, attn_slice_bytes(p.Nq, p.lddo, p.dh));
+  const bf16* krow = (const bf16*)p.k + ((size_t)b * p.Nk + ki) * p.ldk + h * p.dh;
+  const bf16* vrow = (const bf16*)p.v + ((size_t)b * p.Nk + ki) * p.ldv + h * p.dh;
+  const float* lse_b = p.lse + ((size_t)b * p.H + h) * p.Nq;
+  const float* dlt_b = p.delta + ((size_t)b * p.H + h) * p.Nq;
+
+  const int nqt = __builtin_amdgcn_readfirstlane(ktile * 128 < keys ? (p.Nq + 63) / 64 : 0);      // (no query sees keys past the sample's length)
+  const int qt0 = p.causal ? max(0, ktile * 128 - p.query0) / 64 : 0;
+  AttnFragOff<DHP, KC> fo;
+  fo.init(lane);
+  AttnTileCopy<DHP> cq, cd;
+  cq.init(wave, lane, p.ldq, p.dh);
+  cd.init(wave, lane, p.lddo, p.dh);
+  if (qt0 < nqt) {
+    cq.issue(qr, qt0 * 64, p.ldq, Qs[0], wave);
+    cd.issue(dr, qt0 * 64, p.lddo, Ds[0], wave);
+  }
+  float stat = 0.f;      // of a query tile: wave 0 lse, wave 1 delta; as loaded until the end of the tile before
+  const float* stat_b = wave == 0 ? lse_b : dlt_b;
+  auto load_stats = [&](int qt) {
+    if (wave < 2) stat = stat_b[min((uint32_t)(qt * 64 + lane), (uint32_t)p.Nq - 1u)];
+  };
+  auto store_stats = [&](int qt, int buf) {
+    const bool ok = qt * 64 + lane < p.Nq;
+    if (wave == 0) lse_s[buf][lane] = ok && stat != -INFINITY ? stat * LOG2E : INFINITY;      // (a query that sees no key has no probabilities)
+    if (wave == 1) dlt_s[buf][lane] = ok ? -stat : 0.f;
+  };
+  load_stats(qt0);
+  rel_copy_starts(p.bk, st, start, 256);
+  rel_fill<bf16, true>(p, start, h, rel_lds, 256);
+  const int tab = rel_lane(p, 4 * g + p.query0 - ki + p.bk.hi + REL_MARGIN);
+
+  bf16x8 kf[KC], vf[KC];
+#pragma unroll
+  for (int c = 0; c < KC; ++c) {
+    const bool ok = kok && 16 * c + 8 * g < p.dh;
+    kf[c] = ld8(krow + 16 * c + 8 * g, ok);
+    vf[c] = ld8(vrow + 16 * c + 8 * g, ok);
+  }
+  f32x16 dkacc[DT], dvacc[DT];
+#pragma unroll
+  for (int i = 0; i < DT; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) { dkacc[i][r] = 0.f; dvacc[i][r] = 0.f; }
+  store_stats(qt0, 0);
+  wait_vmcnt<0>();
+  __syncthreads();
+  const float far_hi = rel_lds[0], far_lo = rel_lds[rel_entries(p.bk) - 1];
+
+  auto tile = [&](int qt, auto bc) {
+    take_turns(p.even, qt);
+    constexpr int buf = bc();
+    const bool more = qt + 1 < nqt;
+    if (more) {
+      cq.issue(qr, (qt + 1) * 64, p.ldq, Qs[buf ^ 1], wave);
+      cd.issue(dr, (qt + 1) * 64, p.lddo, Ds[buf ^ 1], wave);
+      load_stats(qt + 1);
+    }
+    const int pos = p.query0 + qt * 64;      // of the tile's first query; distances k0 - pos - 63 .. k0 + 31 - pos
+    const bool below = k0 + 31 - pos <= p.bk.lo, above = k0 - pos - 63 >= p.bk.hi;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      if (MINW > 2) __builtin_amdgcn_sched_barrier(0);
+      f32x16 s, dp;
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        const f32x4 d4 = *reinterpret_cast<const f32x4*>(&dlt_s[buf][32 * t + 8 * r4 + 4 * g]);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) dp[4 * r4 + u] = d4[u];
+      }
+      if (below || above) {
+        const float far = below ? far_lo : far_hi;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = far;
+      } else {
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4) {
+          const f32x4 v = *reinterpret_cast<const f32x4*>(rel_lds + (tab + qt * 64) + 32 * t + 8 * r4);
+#pragma unroll
+          for (int u = 0; u < 4; ++u) s[4 * r4 + u] = v[u];
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < KC; ++c) {
+        s = mfma32(fo.row_frag(Qs[buf], t, c), kf[c], s);
+        dp = mfma32(fo.row_frag(Ds[buf], t, c), vf[c], dp);
+      }
+      if (p.causal && k0 + 31 > pos) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = ki <= pos + 32 * t + acc_row(r, g) ? s[r] : -INFINITY;
+      }
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        const f32x4 l4 = *reinterpret_cast<const f32x4*>(&lse_s[buf][32 * t + 8 * r4 + 4 * g]);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int r = 4 * r4 + u;
+          // a lane whose key is past the sample's length computes garbage that stays in its own accumulator columns, which are not stored
+          s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], p.scale_log2, -l4[u]));
+          dp[r] *= s[r];
+        }
+      }
+#pragma unroll
+      for (int cc = 0; cc < 2; ++cc) {
+        const bf16x8 pf = pack8(s, 8 * cc);
+        const bf16x8 dsf = pack8(dp, 8 * cc);
+#pragma unroll
+        for (int i = 0; i < DT; ++i) {
+          dvacc[i] = mfma32(fo.tr_frag(Ds[buf], 32 * t + 16 * cc, i), pf, dvacc[i]);
+          dkacc[i] = mfma32(fo.tr_frag(Qs[buf], 32 * t + 16 * cc, i), dsf, dkacc[i]);
+        }
+      }
+    }
+    if (MINW > 2) __builtin_amdgcn_sched_barrier(0);
+    if (more) store_stats(qt + 1, buf ^ 1);
+    wait_vmcnt<0>();
+    __syncthreads();
+  };
+  two_stages(qt0, nqt, tile);
+  if (ki >= p.Nk) return;
+  bf16* dkb = (bf16*)p.dk + ((size_t)b * p.Nk + ki) * p.lddk + h * p.dh;
+  bf16* dvb = (bf16*)p.dv + ((size_t)b * p.Nk + ki) * p.lddv + h * p.dh;
+#pragma unroll
+  for (int i = 0; i < DT; ++i)
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4) {
+      const int col = 32 * i + 8 * r4 + 4 * g;
+      if (col < p.dh) {
+        bf16x4 ok_, ov;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          ok_[u] = (bf16)(kok ? dkacc[i][4 * r4 + u] * p.scale : 0.f);
+          ov[u] = (bf16)(kok ? dvacc[i][4 * r4 + u] : 0.f);
+        }
+        *reinterpret_cast<bf16x4*>(dkb + col) = ok_;
+        *reinterpret_cast<bf16x4*>(dvb + col) = ov;
+      }
+    }
+}
+
+// ------------------------------------------------------------------ fp32: a wave a row
+constexpr int REL_F32_MAX_D = 96;
+__device__ __forceinline__ float rel_bias_f32(const RelAttnK& p, const uint16_t* start, int h, int dist) {
+  return ((const float*)p.table)[(size_t)rel_bucket(p.bk, start, max(p.bk.lo, min(p.bk.hi, dist))) * p.H + h];
+}
+
+__global__ void __launch_bounds__(64) rel_fwd_f32_kernel(const RelAttnK p, const RelStarts st) {
+  __shared__ uint16_t start[REL_MAX_BUCKETS / 2];
+  extern __shared__ float sc[];        // [Nk]
+  __shared__ float qs[REL_F32_MAX_D];
+  const int lane = threadIdx.x, i = blockIdx.x % p.Nq, bh = blockIdx.x / p.Nq, b = bh / p.H, h = bh % p.H, pos = p.query0 + i;
+  const int keys = rel_keys(p, b), lim = p.causal ? min(keys, pos + 1) : keys;
+  const float* q = (const float*)p.q + ((size_t)b * p.Nq + i) * p.ldq + h * p.dh;
+  const float* kb = (const float*)p.k + (size_t)b * p.Nk * p.ldk + h * p.dh;
+  const float* vb = (const float*)p.v + (size_t)b * p.Nk * p.ldv + h * p.dh;
+  rel_copy_starts(p.bk, st, start, 64);
+  for (int t = lane; t < p.dh; t += 64) qs[t] = q[t];
+  __syncthreads();
+  float mx = -INFINITY;
+  for (int j = lane; j < lim; j += 64) {
+    float s = 0.f;
+#pragma unroll 16
+    for (int t = 0; t < p.dh; ++t) s = fmaf(qs[t], kb[(size_t)j * p.ldk + t], s);
+    s = fmaf(s, p.scale, rel_bias_f32(p, start, h, j - pos));
+    sc[j] = s;
+    mx = fmaxf(mx, s);
+  }
+  mx = wave_max(mx);
+  const float ref = mx == -INFINITY ? 0.f : mx;
+  float sum = 0.f;
+  for (int j = lane; j < lim; j += 64) {
+    const float e = expf(sc[j] - ref);
+    sc[j] = e;
+    sum += e;
+  }
+  sum = wave_sum(sum);
+  __syncthreads();
+  float* o = (float*)p.o + ((size_t)b * p.Nq + i) * p.ldo + h * p.dh;
+  for (int t = lane; t < p.dh; t += 64) {
+    float a = 0.f;
+#pragma unroll 16
+    for (int j = 0; j < lim; ++j) a = fmaf(sc[j], vb[(size_t)j * p.ldv + t], a);
+    o[t] = sum == 0.f ? 0.f : a / sum;
+  }
+  if (p.lse && lane == 0) p.lse[((size_t)b * p.H + h) * p.Nq + i] = sum == 0.f ? -INFINITY : mx + logf(sum);
+}
+
+__global__ void __launch_bounds__(64) rel_bwd_dq_f32_kernel(const RelAttnK p, const RelStarts st) {
+  __shared__ uint16_t start[REL_MAX_BUCKETS / 2];
+  extern __shared__ float sc[];        // [Nk]
+  __shared__ float qs[REL_F32_MAX_D], dos[REL_F32_MAX_D];
+  const int lane = threadIdx.x, i = blockIdx.x % p.Nq, bh = blockIdx.x / p.Nq, b = bh / p.H, h = bh % p.H, pos = p.query0 + i;
+  const int keys = rel_keys(p, b), lim = max(0, p.causal ? min(keys, pos + 1) : keys);
+  const float* q = (const float*)p.q + ((size_t)b * p.Nq + i) * p.ldq + h * p.dh;
+  const float* dor = (const float*)p.dout + ((size_t)b * p.Nq + i) * p.lddo + h * p.dh;
+  const float* orow = (const float*)p.o + ((size_t)b * p.Nq + i) * p.ldo + h * p.dh;
+  const float* kb = (const float*)p.k + (size_t)b * p.Nk * p.ldk + h * p.dh;
+  const float* vb = (const float*)p.v + (size_t)b * p.Nk * p.ldv + h * p.dh;
+  const size_t sidx = ((size_t)b * p.H + h) * p.Nq + i;
+  const float l = p.lse[sidx], lse = l == -INFINITY ? INFINITY : l;
+  float dlt = 0.f;
+  rel_copy_starts(p.bk, st, start, 64);
+  for (int t = lane; t < p.dh; t += 64) { qs[t] = q[t]; dos[t] = dor[t]; dlt = fmaf(dor[t], orow[t], dlt); }
+  dlt = wave_sum(dlt);
+  if (lane == 0) p.delta[sidx] = dlt;
+  __syncthreads();
+  for (int j = lane; j < lim; j += 64) {
+    float s = 0.f, dp = 0.f;
+#pragma unroll 16
+    for (int t = 0; t < p.dh; ++t) {
+      s = fmaf(qs[t], kb[(size_t)j * p.ldk + t], s);
+      dp = fmaf(dos[t], vb[(size_t)j * p.ldv + t], dp);
+    }
+    sc[j] = expf(fmaf(s, p.scale, rel_bias_f32(p, start, h, j - pos)) - lse) * (dp - dlt);
+  }
+  __syncthreads();
+  float* dq = (float*)p.dq + ((size_t)b * p.Nq + i) * p.lddq + h * p.dh;
+  for (int t = lane; t < p.dh; t += 64) {
+    float a = 0.f;
+#pragma unroll 16
+    for (int j = 0; j < lim; ++j) a = fmaf(sc[j], kb[(size_t)j * p.ldk + t], a);
+    dq[t] = a * p.scale;
+  }
+  if (!p.dtable_partial) return;
+  float* out = p.dtable_partial + (((size_t)h * p.B + b) * p.Nq + i) * p.bk.n_buckets;
+  for (int bucket = lane; bucket < p.bk.n_buckets; bucket += 64) {      // a lane adds its bucket's keys
+    const int side = p.bk.bidirectional && bucket >= p.bk.per_side, k = bucket - side * p.bk.per_side;
+    auto first_of = [&](int n) { return n < p.bk.half ? n : (n < p.bk.per_side ? (int)start[n - p.bk.half] : 1 << 30); };
+    const int n0 = first_of(k), n1 = first_of(k + 1) - 1;
+    int j0 = side ? pos + max(n0, 1) : pos - n1, j1 = min(lim - 1, side ? pos + n1 : pos - n0);
+    if (!p.bk.bidirectional && k == 0) j1 = lim - 1;
+    float v = 0.f;
+    for (int j = max(0, j0); j <= j1; ++j) v += sc[j];
+    out[bucket] = v;
+  }
+}
+
+__global__ void __launch_bounds__(64) rel_bwd_dkv_f32_kernel(const RelAttnK p, const RelStarts st) {
+  __shared__ uint16_t start[REL_MAX_BUCKETS / 2];
+  extern __shared__ float sc[];        // [2][Nq]: P and dS
+  __shared__ float ks[REL_F32_MAX_D], vs[REL_F32_MAX_D];
+  const int lane = threadIdx.x, j = blockIdx.x % p.Nk, bh = blockIdx.x / p.Nk, b = bh / p.H, h = bh % p.H;
+  float* dk = (float*)p.dk + ((size_t)b * p.Nk + j) * p.lddk + h * p.dh;
+  float* dv = (float*)p.dv + ((size_t)b * p.Nk + j) * p.lddv + h * p.dh;
+  if (j >= rel_keys(p, b)) {
+    for (int t = lane; t < p.dh; t += 64) { dk[t] = 0.f; dv[t] = 0.f; }
+    return;
+  }
+  const float* kr = (const float*)p.k + ((size_t)b * p.Nk + j) * p.ldk + h * p.dh;
+  const float* vr = (const float*)p.v + ((size_t)b * p.Nk + j) * p.ldv + h * p.dh;
+  const float* qb = (const float*)p.q + (size_t)b * p.Nq * p.ldq + h * p.dh;
+  const float* dob = (const float*)p.dout + (size_t)b * p.Nq * p.lddo + h * p.dh;
+  const float* lse_b = p.lse + ((size_t)b * p.H + h) * p.Nq;
+  const float* dlt_b = p.delta + ((size_t)b * p.H + h) * p.Nq;
+  rel_copy_starts(p.bk, st, start, 64);
+  for (int t = lane; t < p.dh; t += 64) { ks[t] = kr[t]; vs[t] = vr[t]; }
+  __syncthreads();
+  const int i0 = p.causal ? max(0, j - p.query0) : 0;
+  float* pp = sc; float* dsp = sc + p.Nq;
+  for (int i = i0 + lane; i < p.Nq; i += 64) {
+    float s = 0.f, dp = 0.f;
+    for (int t = 0; t < p.dh; ++t) {
+      s = fmaf(qb[(size_t)i * p.ldq + t], ks[t], s);
+      dp = fmaf(dob[(size_t)i * p.lddo + t], vs[t], dp);
+    }
+    const float l = lse_b[i];
+    const float pr = expf(fmaf(s, p.scale, rel_bias_f32(p, start, h, j - p.query0 - i)) - (l == -INFINITY ? INFINITY : l));
+    pp[i] = pr;
+    dsp[i] = pr * (dp - dlt_b[i]);
+  }
+  __syncthreads();
+  for (int t = lane; t < p.dh; t += 64) {
+    float a = 0.f, c = 0.f;
+    for (int i = i0; i < p.Nq; ++i) {
+      a = fmaf(dsp[i], qb[(size_t)i * p.ldq + t], a);
+      c = fmaf(pp[i], dob[(size_t)i * p.lddo + t], c);
+    }
+    dk[t] = a * p.scale;
+    dv[t] = c;
+  }
+}
+
+// ------------------------------------------------------------------ host side
+// base^e * other^f as words of 32 bits, least first
+static std::vector<uint32_t> rel_power(uint32_t base, int e, uint32_t other, int f) {
+  std::vector<uint32_t> w{1};
+  for (int i = 0; i < e + f; ++i) {
+    uint64_t carry = 0;
+    for (uint32_t& x : w) {
+      carry += (uint64_t)x * (i < e ? base : other);
+      x = (uint32_t)carry;
+      carry >>= 32;
+    }
+    if (carry) w.push_back((uint32_t)carry);
+  }
+  return w;
+}
+static bool rel_less(const std::vector<uint32_t>& a, const std::vector<uint32_t>& b) {
+  if (a.size() != b.size()) return a.size() < b.size();
+  return std::lexicographical_compare(a.rbegin(), a.rend(), b.rbegin(), b.rend());
+}
+
+// Bucket half + k begins with the least whole n for which n >= half (far / half)^(k / rest).  Where that border is a whole number or next to one, as it is for
+// the usual powers of two, n^rest half^k and far^k half^rest are compared as whole numbers.
+static int rel_buckets(const char* who, int n_buckets, int max_distance, int bidirectional, RelBucketsK& r, RelStarts& st) {
+  if (n_buckets < 2 || max_distance < 1) return set_errorf(DP_EINVAL, "%s: bad number of buckets or distance", who);
+  if (n_buckets > REL_MAX_BUCKETS || max_distance > REL_MAX_DISTANCE)
+    return set_errorf(DP_EUNSUPPORTED, "%s: at most %d buckets and a distance of %d", who, REL_MAX_BUCKETS, REL_MAX_DISTANCE);
+  if (bidirectional && n_buckets % 2) return set_errorf(DP_EINVAL, "%s: buckets of two directions must be even in number", who);
+  r.n_buckets = n_buckets;
+  r.bidirectional = bidirectional != 0;
+  r.per_side = bidirectional ? n_buckets / 2 : n_buckets;
+  r.half = r.per_side / 2;
+  if (r.per_side < 2) return set_errorf(DP_EINVAL, "%s: a direction needs two buckets", who);
+  if (max_distance <= r.half) return set_errorf(DP_EINVAL, "%s: the largest distance must exceed %d, the buckets of one distance each", who, r.half);
+  const int rest = r.per_side - r.half;
+  st.of[0] = (uint16_t)r.half;
+  for (int k = 1; k < rest; ++k) {
+    const double border = r.half * pow((double)max_distance / r.half, (double)k / rest), near = nearbyint(border);
+    int n = (int)ceil(border);
+    if (fabs(border - near) < 1e-6) {
+      n = (int)near;
+      if (rel_less(rel_power((uint32_t)n, rest, (uint32_t)r.half, k), rel_power((uint32_t)max_distance, k, (uint32_t)r.half, rest))) ++n;
+    }
+    st.of[k] = (uint16_t)n;
+  }
+  r.lo = -(int)st.of[rest - 1];
+  r.hi = bidirectional ? st.of[rest - 1] : 0;
+  return DP_OK;
+}
+
+static size_t rel_align(size_t n) { return align_up(n, 256); }
+struct RelWorkspace { size_t delta, partial, bytes; };
+// dQ workgroups (bf16) or rows (fp32) of a head, each with its sums over buckets
+static size_t rel_parts(int B, int Nq, bool f32) { return (size_t)B * (f32 ? Nq : (Nq + 127) / 128); }
+static RelWorkspace rel_workspace(int B, int H, int Nq, int n_buckets) {
+  RelWorkspace w;
+  w.delta = 0;
+  w.partial = rel_align((size_t)B * H * Nq * sizeof(float));
+  w.bytes = w.partial + rel_align((size_t)H * rel_parts(B, Nq, true) * n_buckets * sizeof(float));
+  return w;
+}
+
+// Dynamic LDS beyond 64 KB in all has to be asked for, once per kernel and device; asking again does no harm.
+template <class K> static int rel_allow_lds(K kern, int dhp, int bytes) {
+  if (512 * dhp + 1088 + bytes <= 64 * 1024) return DP_OK;      // (two stages of two tiles, and a few rows of statistics)
+  if (hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return set_error(DP_EHIP, "hipFuncSetAttribute(attention) failed");
+  return DP_OK;
+}
+template <class F> static int rel_dispatch(int d_head, F f) {
+  using std::integral_constant;
+  if (d_head <= 48) return f(integral_constant<int, 64>(), integral_constant<int, 3>());
+  if (d_head <= 64) return f(integral_constant<int, 64>(), integral_constant<int, 4>());
+  if (d_head <= 80) return f(integral_constant<int, 96>(), integral_constant<int, 5>());
+  return f(integral_constant<int, 96>(), integral_constant<int, 6>());
+}
+static int rel_takes_turns(long blocks, int per_cu) { return blocks > 256 && blocks <= 256L * per_cu; }
+static int rel_launched() {
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? DP_OK : set_errorf(DP_EHIP, "attention with a relative position bias: launch failed (%s)", hipGetErrorString(e));
+}
+
+static int check_rel(const char* who, int dtype, const RelAttnK& k, const dp_relbias* bias, bool bwd) {
+  if (dtype != DP_F32 && dtype != DP_BF16) return set_error(DP_EINVAL, "unknown dtype");
+  if (k.B <= 0 || k.H <= 0 || k.Nq <= 0 || k.Nk <= 0 || k.dh <= 0) return set_errorf(DP_EINVAL, "%s: non-positive size", who);
+  if (!(k.scale > 0.f) || !(k.scale < INFINITY)) return set_errorf(DP_EINVAL, "%s: the scale must be positive and finite", who);
+  if (k.scale < 1e-6f || k.scale > 1e6f) return set_errorf(DP_EUNSUPPORTED, "%s: a scale between 1e-6 and 1e6", who);      // (the bias is held over the scale)
+  if ((size_t)k.B * k.H > 65535) return set_errorf(DP_EUNSUPPORTED, "%s: batch * heads exceeds 65535", who);
+  const int grid = dtype == DP_BF16 ? 8 : 4, es = dtype == DP_BF16 ? 2 : 4;
+  if (k.dh % grid || k.dh > 96) return set_errorf(DP_EUNSUPPORTED, "%s: d_head must be a multiple of %d, at most 96", who, grid);
+  if (k.query0 > (1 << 29) || k.query0 < -(1 << 29) || k.Nq > (1 << 29) || k.Nk > (1 << 29)) return set_errorf(DP_EUNSUPPORTED, "%s: positions beyond 2^29", who);
+  const size_t tiles = (size_t)(std::max(k.Nq, k.Nk) + 127) / 128 * k.B * k.H;
+  if (tiles >= (1u << 24)) return set_errorf(DP_EUNSUPPORTED, "%s: too many tiles for one launch", who);      // (2^32 threads)
+  const int span = k.H * k.dh;
+  struct Op { const void* p; int ld, n; const char* name; };
+  const Op ops[] = {{k.q, k.ldq, k.Nq, "q"}, {k.k, k.ldk, k.Nk, "k"}, {k.v, k.ldv, k.Nk, "v"}, {k.o, k.ldo, k.Nq, "o"},
+                    {k.dout, k.lddo, k.Nq, "d_o"}, {k.dq, k.lddq, k.Nq, "dq"}, {k.dk, k.lddk, k.Nk, "dk"}, {k.dv, k.lddv, k.Nk, "dv"}};
+  for (int i = 0; i < (bwd ? 8 : 4); ++i) {
+    DP_TRY(check_ptr(ops[i].p, ops[i].name));
+    if (ops[i].ld < span) return set_errorf(DP_EINVAL, "%s: the row stride of %s is less than heads * d_head", who, ops[i].name);
+    if (ops[i].ld % grid) return set_errorf(DP_EUNSUPPORTED, "%s: the row stride of %s must be a multiple of %d", who, ops[i].name, grid);
+    // one (sample, head) is addressed with 32-bit byte offsets, of which bit 31 means "no data"
+    if ((size_t)ops[i].n * ops[i].ld * es >= (1ull << 31)) return set_errorf(DP_EUNSUPPORTED, "%s: the rows of one sample of %s must span less than 2 GiB", who, ops[i].name);
+  }
+  if (!bias) return set_errorf(DP_EINVAL, "%s: bias is NULL", who);
+  DP_TRY(check_ptr(bias->table, "the bias table"));
+  if (k.key_len && (uintptr_t)k.key_len % 4) return set_errorf(DP_EALIGN, "%s: key_len must be 4-byte aligned", who);
+  if (bwd && !k.lse) return set_errorf(DP_EINVAL, "%s: lse is NULL", who);
+  if (k.lse && (uintptr_t)k.lse % 16) return set_errorf(DP_EALIGN, "%s: lse is not 16-byte aligned", who);
+  if (dtype == DP_F32) {
+    if ((size_t)k.B * k.H * std::max(k.Nq, k.Nk) >= (1u << 26)) return set_errorf(DP_EUNSUPPORTED, "%s: too many rows for one launch", who);
+    if ((size_t)k.Nk * 4 > 60000 || (bwd && (size_t)k.Nq * 8 > 60000)) return set_errorf(DP_EUNSUPPORTED, "%s: sequence too long for fp32", who);
+  }
+  return DP_OK;
+}
+
+}  // namespace dp
+
+using namespace dp;
+
+extern "C" {
+
+int dp_relative_bucket(int n_buckets, int max_distance, int bidirectional, int distance) {
+  RelBucketsK r;
+  RelStarts st;
+  DP_TRY(rel_buckets("dp_relative_bucket", n_buckets, max_distance, bidirectional, r, st));
+  const int n = bidirectional ? (distance < 0 ? -(int64_t)distance > INT32_MAX ? INT32_MAX : -distance : distance) : (distance < 0 ? (distance == INT32_MIN ? INT32_MAX : -distance) : 0);
+  const int side = bidirectional && distance > 0 ? r.per_side : 0;
+  if (n < r.half) return side + n;
+  const int k = (int)(std::upper_bound(st.of, st.of + (r.per_side - r.half), n) - st.of) - 1;
+  return side + r.half + k;
+}
+
+size_t dp_op_attention_relbias_workspace_bytes(int B, int H, int Nq, int Nk, int d_head, int n_buckets, int backward) {
+  if (B <= 0 || H <= 0 || Nq <= 0 || Nk <= 0 || d_head <= 0 || n_buckets <= 0) return 0;
+  return backward ? rel_workspace(B, H, Nq, n_buckets).bytes : 0;
+}
+
+int dp_op_attention_relbias_fwd(int dtype, int B, int H, int Nq, int Nk, int d_head, int causal, float scale, const void* q, int ldq, const void* k,
+                                int ldk, const void* v, int ldv, const dp_relbias* bias, const int32_t* key_len, void* o, int ldo, float* lse,
+                                void* workspace, size_t workspace_bytes, void* hip_stream) {
+  const char* who = "dp_op_attention_relbias_fwd";
+  RelAttnK a{};
+  RelStarts st;
+  a.B = B; a.H = H; a.Nq = Nq; a.Nk = Nk; a.dh = d_head; a.causal = causal != 0; a.query0 = bias ? bias->query0 : 0;
+  a.scale = scale; a.scale_log2 = scale * LOG2E; a.inv_scale = 1.0f / scale;
+  a.q = q; a.ldq = ldq; a.k = k; a.ldk = ldk; a.v = v; a.ldv = ldv; a.table = bias ? bias->table : nullptr; a.key_len = key_len; a.o = o; a.ldo = ldo; a.lse = lse;
+  DP_TRY(check_rel(who, dtype, a, bias, false));
+  DP_TRY(rel_buckets(who, bias->n_buckets, bias->max_distance, bias->bidirectional, a.bk, st));
+  hipStream_t s = (hipStream_t)hip_stream;
+  KScope ks(dtype == DP_BF16 ? KK_ATTN_FWD : KK_ATTN_F32, 4.0 * B * H * (double)Nq * Nk * d_head, (dtype == DP_BF16 ? 2.0 : 4.0) * B * H * d_head * (2.0 * Nq + 2.0 * Nk), s, Nq, Nk, d_head);
+  if (dtype == DP_F32) {
+    hipLaunchKernelGGL(rel_fwd_f32_kernel, dim3((unsigned)(B * H) * Nq), dim3(64), (size_t)Nk * sizeof(float), s, a, st);
+    return rel_launched();
+  }
+  const long blocks = (long)((Nq + 127) / 128) * B * H;
+  const int lds = rel_table_bytes(a.bk);
+  a.even = rel_takes_turns(blocks, d_head <= 64 ? 4 : 3);
+  return rel_dispatch(d_head, [&](auto dhp, auto kc) {
+    constexpr int W = dhp == 64 ? 4 : 3;
+    DP_TRY(rel_allow_lds(rel_fwd_bf16_kernel<dhp, kc, W>, dhp, lds));
+    hipLaunchKernelGGL((rel_fwd_bf16_kernel<dhp, kc, W>), dim3((unsigned)blocks), dim3(256), lds, s, a, st);
+    return rel_launched();
+  });
+}
+
+int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_head, int causal, float scale, const void* q, int ldq, const void* k,
+                                int ldk, const void* v, int ldv, const dp_relbias* bias, const int32_t* key_len, const void* o, int ldo,
+                                const float* lse, const void* d_o, int lddo, void* dq, int lddq, void* dk, int lddk, void* dv, int lddv, float* dtable,
+                                int accumulate, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  const char* who = "dp_op_attention_relbias_bwd";
+  RelAttnK a{};
+  RelStarts st;
+  a.B = B; a.H = H; a.Nq = Nq; a.Nk = Nk; a.dh = d_head; a.causal = causal != 0; a.query0 = bias ? bias->query0 : 0;
+  a.scale = scale; a.scale_log2 = scale * LOG2E; a.inv_scale = 1.0f / scale;
+  a.q = q; a.ldq = ldq; a.k = k; a.ldk = ldk; a.v = v; a.ldv = ldv; a.table = bias ? bias->table : nullptr; a.key_len = key_len;
+  a.o = const_cast<void*>(o); a.ldo = ldo; a.lse = const_cast<float*>(lse); a.dout = d_o; a.lddo = lddo;
+  a.dq = dq; a.lddq = lddq; a.dk = dk; a.lddk = lddk; a.dv = dv; a.lddv = lddv;
+  DP_TRY(check_rel(who, dtype, a, bias, true));
+  DP_TRY(rel_buckets(who, bias->n_buckets, bias->max_distance, bias->bidirectional, a.bk, st));
+  if (dtable && (uintptr_t)dtable % 16) return set_errorf(DP_EALIGN, "%s: dtable is not 16-byte aligned", who);
+  const RelWorkspace w = rel_workspace(B, H, Nq, bias->n_buckets);
+  DP_TRY(check_ptr(workspace, "workspace", 256));
+  if (workspace_bytes < w.bytes) return set_errorf(DP_EWORKSPACE, "%s: workspace too small (%zu bytes, needs %zu)", who, workspace_bytes, w.bytes);
+  a.delta = (float*)((char*)workspace + w.delta);
+  a.dtable_partial = dtable ? (float*)((char*)workspace + w.partial) : nullptr;
+  hipStream_t s = (hipStream_t)hip_stream;
+  const int parts = (int)rel_parts(B, Nq, dtype == DP_F32);
+  const double fl = 4.0 * B * H * (double)Nq * Nk * d_head, by = (dtype == DP_BF16 ? 2.0 : 4.0) * B * H * d_head * (3.0 * Nq + 2.0 * Nk);
+  if (dtype == DP_F32) {
+    KScope ks(KK_ATTN_F32, 2 * fl, 2 * by, s, Nq, Nk, d_head);
+    hipLaunchKernelGGL(rel_bwd_dq_f32_kernel, dim3((unsigned)(B * H) * Nq), dim3(64), (size_t)Nk * sizeof(float), s, a, st);
+    DP_TRY(rel_launched());
+    hipLaunchKernelGGL(rel_bwd_dkv_f32_kernel, dim3((unsigned)(B * H) * Nk), dim3(64), (size_t)2 * Nq * sizeof(float), s, a, st);
+    DP_TRY(rel_launched());
+  } else {
+    const long qblocks = (long)((Nq + 127) / 128) * B * H, kblocks = (long)((Nk + 127) / 128) * B * H;
+    const int table = rel_table_bytes(a.bk), both = table + rel_sums_bytes(a.bk);
+    {
+      KScope ks(KK_ATTN_BWD_DQ, fl, by, s, Nq, Nk, d_head);
+      a.even = rel_takes_turns(qblocks, d_head <= 64 ? 3 : 2);
+      DP_TRY(rel_dispatch(d_head, [&](auto dhp, auto kc) {
+        DP_TRY(rel_allow_lds(rel_bwd_dq_bf16_kernel<dhp, kc>, dhp, both));
+        hipLaunchKernelGGL((rel_bwd_dq_bf16_kernel<dhp, kc>), dim3((unsigned)qblocks), dim3(256), both, s, a, st);
+        return rel_launched();
+      }));
+    }
+    KScope ks(KK_ATTN_BWD_DKV, fl, by, s, Nq, Nk, d_head);
+    a.even = rel_takes_turns(kblocks, 2);
+    DP_TRY(rel_dispatch(d_head, [&](auto dhp, auto kc) {
+      DP_TRY(rel_allow_lds(rel_bwd_dkv_bf16_kernel<dhp, kc, 2>, dhp, table));
+      hipLaunchKernelGGL((rel_bwd_dkv_bf16_kernel<dhp, kc, 2>), dim3((unsigned)kblocks), dim3(256), table, s, a, st);
+      return rel_launched();
+    }));
+  }
+  if (!dtable) return DP_OK;
+  KScope ks(KK_REDUCE, 0.0, (double)H * parts * bias->n_buckets * 4, s, parts, H, bias->n_buckets);
+  hipLaunchKernelGGL(rel_dtable_kernel, dim3((unsigned)H, (unsigned)(bias->n_buckets + 31) / 32), dim3(256), 0, s, a.dtable_partial, parts, bias->n_buckets, H, dtable, accumulate != 0);
+  return rel_launched();
+}
+
+}  // extern "C"

@@ -1,0 +1,203 @@
+"""Attention with a relative position bias against its definition in 64 bits: lengths from one key up, ragged tiles, key lengths down to none, causal
+masks that leave queries without a key, bias tables of few and of many buckets, entries of -infinity, NaN behind a sample's keys.
+
+Bounds are elementwise.  U = 2^-24; h = 2^-8 where probabilities, dS and outputs are rounded to bf16, U where they stay fp32.
+  logits      d_head products and the bias are added in fp32, scaled, and taken relative to a reference or to lse: off by at most
+              e = (d_head + 32) U (scale |q| |k| + |bias| + |lse| + 1), which is the relative error of exp (the hardware's own 2 U are in the 32)
+  o           sum over keys of P (h + 2 e + 2 average(e) + n U) |v|, and its own rounding
+  lse         2 average(e) + (n + 64) U
+  dS          P ((d_head + 8) U (|dO| |V| + |dO| |O|)) + 2 e |dS|
+  dq, dk, dv  sums of (h |dS| or h P, the above, and n U for the additions), and their own rounding
+  dtable      the sum of the errors of dS, and (2 (nq + nk) + 200) U of its magnitudes: at most nq + nk additions into one place, then the joining.
+"""
+import numpy as np
+import pytest
+
+from oracle import training_ops as T
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+
+
+def _make(dtype, B, H, nq, nk, d, seed, n_buckets, lens, gain=1.0, pad=0):
+    """Device tensors (rows H * d + pad apart, NaN between them and behind the keys of a sample) and 64-bit values [B, H, n, d]."""
+    import torch
+    t = torch.float32 if dtype == "f32" else torch.bfloat16
+    g = np.random.default_rng(seed)
+    dev, val = {}, {}
+    for name, n, std in (("q", nq, gain), ("k", nk, 1.0), ("v", nk, 1.0), ("do", nq, 1.0)):
+        x = torch.full((B, n, H * d + pad), float("nan"), dtype=t, device="cuda")
+        x[:, :, :H * d] = torch.from_numpy(g.normal(0, std, size=(B, n, H * d))).to(t).cuda()
+        w = x[:, :, :H * d].double().cpu().numpy().reshape(B, n, H, d).transpose(0, 2, 1, 3).copy()
+        if name in "kv" and lens is not None:
+            for b, m in enumerate(lens):
+                x[b, max(m, 0):] = float("nan")
+                w[b, :, max(m, 0):] = 0.0
+        dev[name], val[name] = x, w
+    table = torch.from_numpy(g.normal(0, 1.5, size=(n_buckets, H))).to(t).cuda()
+    return t, dev, val, table, table.double().cpu().numpy()
+
+
+def _close(got, want, bound, what):
+    err = np.abs(got - want)
+    assert np.isfinite(got).all(), what
+    assert (err <= bound).all(), (what, float((err / np.maximum(bound, 1e-300)).max()), np.unravel_index((err - bound).argmax(), err.shape))
+
+
+def _check(dtype, B, H, nq, nk, d, causal, bidirectional, n_buckets, distance, query0, lens, gain=1.0, pad=0, forbid=(), workspace=True, seed=0):
+    import torch
+    from paper_2405_01248_amd import binding as K
+    t, dev, val, table, tv = _make(dtype, B, H, nq, nk, d, seed + nq * 31 + nk, n_buckets, lens, gain, pad)
+    for bk in forbid:
+        table[bk] = -float("inf")
+        tv[bk] = -np.inf
+    dt, ld, scale = (K.DP_F32 if dtype == "f32" else K.DP_BF16), H * d + pad, 1.0 / np.sqrt(d)
+    scale = float(np.float32(scale))
+    key_len = torch.tensor(lens, dtype=torch.int32, device="cuda") if lens is not None else None
+    bias = K.RelBias(table, n_buckets, distance, bidirectional, query0)
+    out = lambda n: torch.full((B, n, ld), 7.0, dtype=t, device="cuda")  # noqa: E731
+    o, dq, dk, dv = out(nq), out(nq), out(nk), out(nk)
+    lse = torch.full((B, H, nq), 7.0, device="cuda")
+    dtable = torch.full((n_buckets, H), 2.0, device="cuda")
+
+    def ws(backward):
+        n = K.op_attention_relbias_workspace_bytes(B, H, nq, nk, d, n_buckets, backward)
+        return torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda") if n else None
+
+    def get(x):
+        assert (x[:, :, H * d:].float() == 7.0).all()      # what lies between the rows is left as it was
+        return x[:, :, :H * d].double().cpu().numpy().reshape(B, -1, H, d).transpose(0, 2, 1, 3)
+
+    def fwd(oo, ll):
+        K.op_attention_relbias_fwd(dt, B, H, nq, nk, d, causal, scale, dev["q"], ld, dev["k"], ld, dev["v"], ld, bias, key_len, oo, ld, ll, ws(False) if workspace else None)
+
+    fwd(o, lse)
+    torch.cuda.synchronize()
+    bk = T.buckets(nq, nk, query0, n_buckets, distance, bidirectional)
+    lens0 = None if lens is None else [min(max(m, 0), nk) for m in lens]
+    args = (val["q"], val["k"], val["v"])
+    wo, wlse = T.attention_relbias_fwd(*args, scale, tv, bk, causal, query0, lens0)
+    n, h = nq + nk, (U if dtype == "f32" else 2.0 ** -8)
+    with np.errstate(invalid="ignore"):
+        s = T._logits(val["q"], val["k"], scale, tv, bk, causal, query0, lens0)
+        P = np.exp(s - np.where(np.isneginf(wlse), 0.0, wlse)[..., None])
+    mag = np.where(np.isneginf(s), 0.0, scale * (np.abs(val["q"]) @ np.abs(val["k"]).swapaxes(-1, -2)) + np.abs(np.where(np.isinf(tv), 0.0, tv)[bk]).transpose(2, 0, 1)[None])
+    e = (d + 32) * U * (mag + np.where(np.isneginf(wlse), 0.0, np.abs(wlse))[..., None] + 1)
+    avg = (P * e).sum(-1)
+    _close(get(o), wo, h * np.abs(wo) + (P * (h + 2 * e + 2 * avg[..., None] + n * U)) @ np.abs(val["v"]) * (1 + h), "o")
+    glse = lse.double().cpu().numpy()
+    empty = np.isneginf(wlse)
+    assert (np.isneginf(glse) == empty).all() and (get(o)[empty] == 0).all()
+    _close(np.where(empty, 0, glse), np.where(empty, 0, wlse), 2 * avg + (n + 64) * U * (1 + np.where(empty, 0, np.abs(wlse))), "lse")
+    o2 = out(nq)
+    fwd(o2, None)
+    assert torch.equal(o2, o)
+
+    # backward, from o and lse as they were stored
+    def bwd(q_, k_, v_, tab, accumulate):
+        K.op_attention_relbias_bwd(dt, B, H, nq, nk, d, causal, scale, dev["q"], ld, dev["k"], ld, dev["v"], ld, bias, key_len, o, ld, lse, dev["do"], ld,
+                                   q_, ld, k_, ld, v_, ld, tab, accumulate, ws(True))
+
+    bwd(dq, dk, dv, dtable, False)
+    torch.cuda.synchronize()
+    ov, do = get(o), val["do"]
+    wdq, wdk, wdv, wdt = T.attention_relbias_bwd(*args, ov, glse, do, scale, tv, bk, causal, query0, lens0)
+    with np.errstate(invalid="ignore"):
+        P = np.exp(s - np.where(empty, 0.0, glse)[..., None])
+    dS = np.abs(P * (do @ val["v"].swapaxes(-1, -2) - (do * ov).sum(-1, keepdims=True)))
+    E = P * ((d + 8) * U * (np.abs(do) @ np.abs(val["v"]).swapaxes(-1, -2) + (np.abs(do) * np.abs(ov)).sum(-1, keepdims=True))) + 2 * e * dS
+    side = scale * ((h + n * U) * dS + (1 + h) * E)
+    fin = (1 + h) if dtype == "bf16" else 1.0
+    _close(get(dq), wdq, h * np.abs(wdq) + side @ np.abs(val["k"]) * fin, "dq")
+    _close(get(dk), wdk, h * np.abs(wdk) + side.swapaxes(-1, -2) @ np.abs(val["q"]) * fin, "dk")
+    _close(get(dv), wdv, h * np.abs(wdv) + (P * (h + 2 * e + n * U)).swapaxes(-1, -2) @ np.abs(do) * fin, "dv")
+    per = (E + (2 * n + 200) * U * dS).sum(0)
+    bound = np.stack([np.bincount(bk.ravel(), per[i].ravel(), n_buckets) for i in range(H)], 1)
+    _close(dtable.double().cpu().numpy(), wdt, bound + U * np.abs(wdt), "dtable")
+    if lens is not None:
+        for b, m in enumerate(lens0):
+            assert (get(dk)[b, :, m:] == 0).all() and (get(dv)[b, :, m:] == 0).all()
+    # the same bits again, without the table and with its gradient added up
+    q2, k2, v2, t2 = out(nq), out(nk), out(nk), dtable.clone()
+    bwd(q2, k2, v2, t2, True)
+    assert torch.equal(q2, dq) and torch.equal(k2, dk) and torch.equal(v2, dv) and torch.equal(t2, dtable + dtable)
+    bwd(out(nq), out(nk), out(nk), None, False)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,H,nq,nk,d,causal,bidirectional,n_buckets,distance,query0,lens", [
+    (1, 1, 1, 1, 8, False, True, 4, 2, 0, None),
+    (2, 3, 77, 77, 64, False, True, 32, 128, 0, [77, 13]),
+    (2, 2, 130, 257, 40, False, True, 16, 64, 127, [257, 0]),        # a sample without keys
+    (1, 2, 513, 513, 72, True, False, 32, 128, 0, None),
+    (1, 1, 200, 64, 96, True, True, 4, 7, -70, None),                # 70 queries before the first key
+    (3, 2, 1, 1000, 64, True, False, 32, 128, 999, [1000, 1, 517]),  # one new token each
+    (2, 1, 5, 4097, 88, False, False, 32, 100, 4000, [4097, 2049]),
+    (1, 2, 300, 300, 48, False, True, 320, 800, 0, None),            # more distances than a tile has
+    (1, 1, 1100, 1100, 64, False, True, 64, 1024, 0, None),
+    (1, 3, 700, 200, 80, True, False, 2, 2, 0, None),                # two buckets
+    (2, 2, 63, 65, 24, True, False, 512, 1024, 5, [64, 66]),         # a length beyond the keys
+    (1, 1, 128, 128, 64, True, True, 32, 128, 1000000, [100]),       # far behind all keys
+    (1, 1, 640, 640, 64, False, True, 32, 128, -300, [-5]),          # a negative length: no keys
+    (5, 7, 33, 31, 16, False, True, 8, 20, 0, [31, 30, 29, 1, 0]),
+    (16, 20, 129, 130, 64, False, True, 32, 128, 0, None),
+])
+def test_against_the_definition(dtype, B, H, nq, nk, d, causal, bidirectional, n_buckets, distance, query0, lens):
+    _check(dtype, B, H, nq, nk, d, causal, bidirectional, n_buckets, distance, query0, lens)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_strides_large_logits_and_forbidden_buckets(dtype):
+    _check(dtype, 2, 3, 150, 190, 40, False, True, 32, 128, 20, [190, 77], pad=24)
+    _check(dtype, 1, 2, 260, 260, 64, True, False, 32, 128, 0, None, gain=12.0)
+    _check(dtype, 1, 2, 400, 400, 64, False, True, 32, 128, 0, None, gain=12.0)
+    _check(dtype, 1, 2, 260, 300, 64, False, True, 32, 128, 0, None, forbid=(0, 3, 15, 31))      # -infinity: near, middle and both ends
+    _check(dtype, 1, 2, 70, 70, 64, True, False, 8, 16, 0, [70], forbid=range(8))               # nothing is visible at all
+
+
+@pytest.mark.parametrize("nq,nk", [(1, 3001), (32, 2500), (33, 700)])
+def test_few_queries_without_a_workspace(nq, nk):
+    _check("bf16", 2, 2, nq, nk, 64, True, False, 32, 128, nk - nq, [nk, nk // 3], workspace=False)
+
+
+def test_captured_passes_and_another_stream():
+    import torch
+    from paper_2405_01248_amd import binding as K
+    B, H, n, d, nb = 3, 4, 200, 64, 32
+    qkv = torch.randn((B, n, 3 * H * d), device="cuda").bfloat16()
+    q, k, v = (qkv[:, :, i * H * d:] for i in range(3))
+    do, table = torch.randn((B, n, H * d), device="cuda").bfloat16(), torch.randn((nb, H), device="cuda").bfloat16()
+    key_len = torch.tensor([200, 64, 0], dtype=torch.int32, device="cuda")
+
+    def buffers():
+        return {"o": torch.empty_like(do), "lse": torch.empty((B, H, n), device="cuda"), "dqkv": torch.empty_like(qkv), "dt": torch.empty((nb, H), device="cuda"),
+                "ws": torch.empty(K.op_attention_relbias_workspace_bytes(B, H, n, n, d, nb, True), dtype=torch.uint8, device="cuda")}
+
+    def step(b):
+        bias, ld, hd = K.RelBias(table, nb, 128, True, 0), 3 * H * d, H * d
+        K.op_attention_relbias_fwd(K.DP_BF16, B, H, n, n, d, False, 0.125, q, ld, k, ld, v, ld, bias, key_len, b["o"], hd, b["lse"], None)
+        g = [b["dqkv"][:, :, i * hd:] for i in range(3)]
+        K.op_attention_relbias_bwd(K.DP_BF16, B, H, n, n, d, False, 0.125, q, ld, k, ld, v, ld, bias, key_len, b["o"], hd, b["lse"], do, hd, g[0], ld, g[1], ld,
+                                   g[2], ld, b["dt"], False, b["ws"])
+
+    cap, eager, other = buffers(), buffers(), buffers()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(cap)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(cap)
+    for i in range(3):
+        qkv.normal_()
+        key_len[1] = 64 + 50 * i
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):      # beside the others, with a workspace of its own
+            step(other)
+        graph.replay()
+        step(eager)
+        torch.cuda.synchronize()
+        for name in ("o", "lse", "dqkv", "dt"):
+            assert torch.equal(cap[name], eager[name]) and torch.equal(other[name], eager[name]), name

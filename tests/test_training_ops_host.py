@@ -71,3 +71,70 @@ def test_layernorm_workspace_serves_fewer_rows(lib):
     for d in (1, 16, 640, 1001, 8192):
         sizes = [lib.dp_op_layernorm_bwd_workspace_bytes(n, d) for n in (1, 2, 17, 255, 1000, 4097, 100000)]
         assert all(a <= b for a, b in zip(sizes, sizes[1:]))
+
+
+def test_attention_refusals(lib):
+    from paper_2405_01248_amd import binding as K
+
+    def need(backward=1, B=2, H=2, nq=64, nk=64, d=64, nb=32):
+        return lib.dp_op_attention_relbias_workspace_bytes(B, H, nq, nk, d, nb, backward)
+
+    def args(a, bwd):
+        bias = K.RelBias(a.pop("table", P), a.pop("nb", 32), a.pop("far", 128), a.pop("both", 1), a.pop("q0", 0))
+        bias = None if a.pop("no_bias", False) else C.byref(bias)
+        ld = a.pop("ld", 128)
+        g = lambda n, default=P: _vp(a.pop(n, default))  # noqa: E731
+        l = lambda n: a.pop("ld" + n, ld)  # noqa: E741, E731
+        head = [a.pop("dtype", 1), a.pop("B", 2), a.pop("H", 2), a.pop("nq", 64), a.pop("nk", 64), a.pop("d", 64), 0, C.c_float(a.pop("scale", 0.125)),
+                g("q"), l("q"), g("k"), l("k"), g("v"), l("v"), bias, g("lens", 0)]
+        if bwd:
+            out = head + [g("o"), l("o"), g("lse"), g("do"), l("do"), g("dq"), l("dq"), g("dk"), l("dk"), g("dv"), l("dv"), g("dt"), 0, g("ws"), a.pop("wsb", need()), None]
+        else:
+            out = head + [g("o"), l("o"), g("lse"), g("ws", 0), a.pop("wsb", 0), None]
+        assert not a, a
+        return out
+
+    fwd = lambda **a: lib.dp_op_attention_relbias_fwd(*args(a, False))  # noqa: E731
+    bwd = lambda **a: lib.dp_op_attention_relbias_bwd(*args(a, True))  # noqa: E731
+    for call in (fwd, bwd):
+        for n in ("B", "H", "nq", "nk", "d"):
+            assert call(**{n: 0}) == EINVAL and call(**{n: -1}) == EINVAL
+        assert call(dtype=2) == EINVAL and call(no_bias=True) == EINVAL and call(table=0) == EINVAL and call(table=OFF) == EALIGN
+        assert call(scale=0.0) == EINVAL and call(scale=NAN) == EINVAL and call(scale=-1.0) == EINVAL and call(scale=1e-7) == EUNSUPPORTED and call(scale=1e7) == EUNSUPPORTED
+        assert call(d=104, ld=208) == EUNSUPPORTED and call(d=60, ld=120) == EUNSUPPORTED and call(dtype=0, d=62) == EUNSUPPORTED
+        assert call(ld=132) == EUNSUPPORTED and call(ld=120) == EINVAL and call(dtype=0, ld=130) == EUNSUPPORTED
+        assert call(nb=1) == EINVAL and call(nb=33) == EINVAL and call(nb=2) == EINVAL and call(nb=514) == EUNSUPPORTED and call(far=1025) == EUNSUPPORTED
+        assert call(far=8) == EINVAL and call(far=16, both=0) == EINVAL and call(far=0) == EINVAL
+        assert call(q0=(1 << 29) + 1) == EUNSUPPORTED and call(q0=-(1 << 29) - 1) == EUNSUPPORTED
+        assert call(nk=1 << 23) == EUNSUPPORTED and b"2 GiB" in lib.dp_last_error()
+        assert call(B=256, H=256, ld=1 << 14) == EUNSUPPORTED
+        assert call(lens=P + 2) == EALIGN and call(lse=OFF) == EALIGN
+        for n in ("q", "k", "v", "o"):
+            assert call(**{n: 0}) == EINVAL and call(**{n: OFF}) == EALIGN and call(**{"ld" + n: 120}) == EINVAL
+    for n in ("do", "dq", "dk", "dv"):
+        assert bwd(**{n: 0}) == EINVAL and bwd(**{n: OFF}) == EALIGN and bwd(**{"ld" + n: 120}) == EINVAL
+    assert bwd(lse=0) == EINVAL and bwd(dt=OFF) == EALIGN and bwd(ws=0) == EINVAL and bwd(ws=P + 64) == EALIGN
+    assert bwd(wsb=need() - 1) == EWORKSPACE
+    assert need(B=0) == 0 and need(nb=0) == 0
+
+
+def test_attention_workspace_serves_smaller_batches(lib):
+    for backward in (0, 1):
+        sizes = [lib.dp_op_attention_relbias_workspace_bytes(b, 12, 300, 300, 64, 32, backward) for b in range(1, 40)]
+        assert all(a <= b for a, b in zip(sizes, sizes[1:]))
+
+
+def test_bucket_refusals(lib):
+    from paper_2405_01248_amd import binding as K
+    for bad in ((1, 128, 0), (0, 128, 0), (-4, 128, 0), (33, 128, 1), (2, 128, 1), (32, 16, 0), (32, 8, 1), (513, 1024, 0), (32, 1025, 1)):
+        assert lib.dp_relative_bucket(*bad, 5) < 0
+        with pytest.raises(K.DpipeError):
+            K.relative_bucket(*bad, 5)
+    assert lib.dp_relative_bucket(32, 128, 1, 0) == 0 and lib.dp_relative_bucket(32, 128, 1, -(2 ** 31)) == 15 and lib.dp_relative_bucket(32, 128, 0, 7) == 0
+
+
+def test_buckets_agree_with_the_definition(lib):
+    from oracle import training_ops as T
+    for n, far, both in ((32, 128, True), (32, 128, False), (16, 64, True), (64, 256, True), (32, 100, False), (320, 800, True), (512, 1024, False), (4, 2, True), (2, 1024, False), (14, 27, True)):
+        for dist in list(range(-1100, 1101)) + [-2 ** 31, 2 ** 31 - 1, -(2 ** 31) + 1]:
+            assert lib.dp_relative_bucket(n, far, int(both), dist) == T.bucket(dist, n, far, both), (n, far, both, dist)

@@ -21,6 +21,7 @@
 #include "dp_ktime.h"
 
 #include <math.h>
+#include <string.h>
 #include <algorithm>
 #include <atomic>
 #include <type_traits>
@@ -35,9 +36,9 @@ struct RelBucketsK {
   int bidirectional;
   int lo, hi;                         // the bucket of every distance <= lo is lo's, of every one >= hi is hi's
 };
-// Least distance of bucket half + k.  A kernel argument of its own, which each workgroup copies to LDS: indexed by lane inside the other arguments, it would
-// send all of them through scratch memory.
-struct RelStarts { uint16_t of[REL_MAX_BUCKETS / 2]; };
+// Least distance of bucket half + k, two to a word; past the last 0xFFFF.  A kernel argument of its own: indexed inside the other arguments, it would send
+// all of them through scratch memory.
+struct RelStarts { uint32_t of[REL_MAX_BUCKETS / 4]; };
 
 struct RelAttnK {
   int B, H, Nq, Nk, dh, causal, query0;
@@ -56,23 +57,29 @@ struct RelAttnK {
   void* dv; int lddv;
   float* dtable_partial;      // [head][sample and query tile][bucket]
   int even;
+  int shares; float* part;      // few queries: shares of the keys, and what they leave: outputs [share][row][column], references and sums [share][row][2]
   RelBucketsK bk;
 };
 
-__device__ __forceinline__ void rel_copy_starts(const RelBucketsK& r, const RelStarts& st, uint16_t* start, int threads) {
-  for (int k = threadIdx.x; k < r.per_side - r.half; k += threads) start[k] = st.of[k];
-  __syncthreads();
-}
-__device__ __forceinline__ int rel_bucket(const RelBucketsK& r, const uint16_t* start, int dist) {
+// Counts the starts that are not above the distance, sixteen (eight scalar registers) at a time: no lane waits for a memory access of its own.
+__device__ __forceinline__ int rel_bucket(const RelBucketsK& r, const RelStarts& st, int dist) {
   const int n = r.bidirectional ? abs(dist) : max(-dist, 0), side = r.bidirectional && dist > 0 ? r.per_side : 0;
-  if (n < r.half) return side + n;
-  int k = 0, end = r.per_side - r.half;      // the last k whose start is not above n
-  while (end - k > 1) {
-    const int mid = (k + end) / 2;
-    if (start[mid] <= n) k = mid;
-    else end = mid;
+  int k = r.half - 1;
+  for (int w = 0; w < (r.per_side - r.half + 1) / 2; w += 8) {
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const uint32_t two = st.of[w + u];
+      k += (int)(two & 0xFFFFu) <= n;
+      k += (int)(two >> 16) <= n;
+    }
   }
-  return side + r.half + k;
+  return side + (n < r.half ? n : k);
+}
+__device__ __forceinline__ int rel_start(const RelBucketsK& r, const RelStarts& st, int k) {      // least distance of a direction's bucket k
+  if (k < r.half) return k;
+  if (k >= r.per_side) return 1 << 28;
+  const uint32_t two = st.of[(k - r.half) / 2];
+  return (int)((k - r.half) & 1 ? two >> 16 : two & 0xFFFFu);
 }
 __host__ __device__ __forceinline__ int rel_entries(const RelBucketsK& r) { return r.hi - r.lo + 1 + 2 * REL_MARGIN; }
 __host__ __device__ __forceinline__ int rel_table_floats(const RelBucketsK& r) { return (rel_entries(r) + 3) / 4 * 4; }
@@ -80,11 +87,11 @@ __device__ __forceinline__ int rel_keys(const RelAttnK& p, int b) { return p.key
 
 // Bias over scale of head h by distance.  Entry e is distance lo - margin + e, or, REVERSED, hi + margin - e.
 template <typename T, bool REVERSED>
-__device__ __forceinline__ void rel_fill(const RelAttnK& p, const uint16_t* start, int h, float* tab, int threads) {
+__device__ __forceinline__ void rel_fill(const RelAttnK& p, const RelStarts& st, int h, float* tab, int threads) {
   const int n = rel_entries(p.bk);
   for (int e = threadIdx.x; e < n; e += threads) {
     const int dist = REVERSED ? p.bk.hi + REL_MARGIN - e : p.bk.lo - REL_MARGIN + e;
-    tab[e] = to_f<T>(((const T*)p.table)[(size_t)rel_bucket(p.bk, start, dist) * p.H + h]) * p.inv_scale;
+    tab[e] = to_f<T>(((const T*)p.table)[(size_t)rel_bucket(p.bk, st, dist) * p.H + h]) * p.inv_scale;
   }
 }
 // Four neighbouring entries
@@ -112,7 +119,6 @@ __device__ __forceinline__ uint32_t rel_slice_bytes(int n, int ld, int dh) { ret
 // attn_fwd_bf16_kernel).  A query that sees no key keeps the reference -inf and the sum 0: zeros, and lse = -inf.
 template <int DHP, int KC, int MINW>
 __global__ void __launch_bounds__(256, MINW) rel_fwd_bf16_kernel(const RelAttnK p, const RelStarts st) {
-  __shared__ uint16_t start[REL_MAX_BUCKETS / 2];
   constexpr int DT = DHP / 32, BQ = 128, TILE = 64 * DHP;
   __shared__ __attribute__((aligned(1024))) bf16 Ks[2][TILE];
   __shared__ __attribute__((aligned(1024))) bf16 Vs[2][TILE];
@@ -141,8 +147,7 @@ __global__ void __launch_bounds__(256, MINW) rel_fwd_bf16_kernel(const RelAttnK 
     ck.issue(kr, 0, p.ldk, Ks[0], wave);
     cv.issue(vr, 0, p.ldv, Vs[0], wave);
   }
-  rel_copy_starts(p.bk, st, start, 256);
-  rel_fill<bf16, false>(p, start, h, rel_lds, 256);
+  rel_fill<bf16, false>(p, st, h, rel_lds, 256);
   const int tab = 4 * g - pos - (bk_lo - REL_MARGIN);      // entry of this lane's first key
 
   bf16x8 qf[KC];
@@ -266,6 +271,216 @@ __global__ void __launch_bounds__(256, MINW) rel_fwd_bf16_kernel(const RelAttnK 
   if (p.lse && g == 0) p.lse[((size_t)b * p.H + h) * p.Nq + qi] = lsum == 0.f ? -INFINITY : fmaf(m, LN2, logf(lsum));
 }
 
+// Four columns of a query's output, unscaled, and (first column) the logarithm of its sum; m: reference of its exponentials (log2 domain).
+__device__ __forceinline__ void rel_store_o(const RelAttnK& p, const f32x4& o, float sum, float m, int b, int h, int row, int col) {
+  const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+  bf16x4 v;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) v[u] = (bf16)(o[u] * inv);
+  *reinterpret_cast<bf16x4*>((bf16*)p.o + ((size_t)b * p.Nq + row) * p.ldo + h * p.dh + col) = v;
+  if (p.lse && col == 0) p.lse[((size_t)b * p.H + h) * p.Nq + row] = sum == 0.f ? -INFINITY : fmaf(m, LN2, logf(sum));
+}
+
+// ------------------------------------------------------------------ forward of few queries (bf16)
+// A workgroup has 32 queries of a head and one share of its tiles of 64 keys, each wave every fourth tile of them: K straight from memory into the
+// operand's registers, V through an LDS tile of the wave's own, both requested a tile ahead; nothing waits at a barrier before the waves' sums meet at the end.
+// Bound by reading K and V, of which a wave keeps a tile each in flight.  With several shares each leaves its unscaled output, reference and sum,
+// and rel_join_kernel adds them in their order.
+template <int DHP, int KC>
+__global__ void __launch_bounds__(256, DHP == 64 ? 2 : 1) rel_fwd_few_bf16_kernel(const RelAttnK p, const RelStarts st) {
+  constexpr int DT = DHP / 32, TILE = 64 * DHP;
+  __shared__ __attribute__((aligned(1024))) bf16 Vs[4][2][TILE];
+  __shared__ float stat[4][2][32];
+  extern __shared__ __attribute__((aligned(16))) float rel_lds[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, l32 = lane & 31;
+  const int bk_lo = p.bk.lo, bk_hi = p.bk.hi, qtiles = (p.Nq + 31) / 32;
+  // the shares and query tiles of a head next to each other in turns of eight: on one XCD
+  int part, bh;
+  attn_block_map(blockIdx.x, qtiles * p.shares, p.B * p.H, part, bh);
+  const int qtile = part / p.shares, share = part % p.shares, b = bh / p.H, h = bh % p.H;
+  const int qi = qtile * 32 + l32, pos0 = p.query0 + qtile * 32, pos = pos0 + l32;
+  const int keys = __builtin_amdgcn_readfirstlane(rel_keys(p, b));
+  const int lim = p.causal ? min(keys, pos + 1) : keys, lim_all = p.causal ? min(keys, pos0 + 1) : keys;
+  const int lim_any = p.causal ? min(keys, p.query0 + min(p.Nq, qtile * 32 + 32)) : keys;
+  const int nkt = __builtin_amdgcn_readfirstlane(lim_any > 0 ? (lim_any + 63) / 64 : 0);
+  const int first = (int)((long)nkt * share / p.shares) + wave, last = (int)((long)nkt * (share + 1) / p.shares);
+  const bf16* kb = (const bf16*)p.k + (size_t)b * p.Nk * p.ldk + h * p.dh;
+  const u32x4 vr = make_raw_rsrc((const bf16*)p.v + (size_t)b * p.Nk * p.ldv + h * p.dh, rel_slice_bytes(keys, p.ldv, p.dh));
+
+  AttnFragOff<DHP, KC> fo;
+  fo.init(lane);
+  AttnTileCopy<DHP> cv[4];
+#pragma unroll
+  for (int w = 0; w < 4; ++w) cv[w].init(w, lane, p.ldv, p.dh);
+  bf16x8 kn[2][KC];
+  auto request = [&](int kt, int buf) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int c = 0; c < KC; ++c) {
+        const int key = kt * 64 + 32 * t + l32;
+        kn[t][c] = ld8(kb + (size_t)key * p.ldk + 16 * c + 8 * g, key < keys && 16 * c + 8 * g < p.dh);
+      }
+#pragma unroll
+    for (int w = 0; w < 4; ++w) cv[w].issue(vr, kt * 64, p.ldv, Vs[wave][buf], w);
+  };
+  if (first < last) request(first, 0);
+  rel_fill<bf16, false>(p, st, h, rel_lds, 256);
+  const int tab = 4 * g - pos - (bk_lo - REL_MARGIN);
+  bf16x8 qf[KC];
+  const bf16* qrow = (const bf16*)p.q + ((size_t)b * p.Nq + qi) * p.ldq + h * p.dh;
+#pragma unroll
+  for (int c = 0; c < KC; ++c) qf[c] = ld8(qrow + 16 * c + 8 * g, qi < p.Nq && 16 * c + 8 * g < p.dh);
+  f32x16 oacc[DT];
+  float m = -INFINITY, lsum = 0.f;
+#pragma unroll
+  for (int i = 0; i < DT; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) oacc[i][r] = 0.f;
+  __syncthreads();
+  const float far_lo = rel_lds[0], far_hi = rel_lds[rel_entries(p.bk) - 1];
+
+  auto tile = [&](int kt, auto bc) __attribute__((always_inline)) {
+    constexpr int buf = bc();
+    wait_vmcnt<0>();      // this wave's own tile has landed
+    asm volatile("" ::: "memory");
+    f32x16 s[2];
+    if (kt * 64 + 63 - pos0 > bk_lo && kt * 64 - pos0 - 31 < bk_hi) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4) {
+          const f32x4 v = rel_read4(rel_lds + (tab + kt * 64) + 32 * t + 8 * r4);
+#pragma unroll
+          for (int u = 0; u < 4; ++u) s[t][4 * r4 + u] = v[u];
+        }
+    } else {
+      const float below = far_lo, above = far_hi, far = kt * 64 - pos0 - 31 < bk_hi ? below : above;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[t][r] = far;
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int c = 0; c < KC; ++c) s[t] = mfma32(kn[t][c], qf[c], s[t]);
+    if (kt + 4 < last) request(kt + 4, buf ^ 1);
+    if (kt * 64 + 64 > lim_all) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[t][r] = kt * 64 + 32 * t + acc_row(r, g) < lim ? s[t][r] : -INFINITY;
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[t][r]);
+    mx = fmaxf(m, reduce_halves(mx, MaxOp()) * p.scale_log2);
+    const float ref = mx == -INFINITY ? 0.f : mx, alpha = __builtin_amdgcn_exp2f(m - ref);
+    m = mx;
+    lsum *= alpha;
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) oacc[i][r] *= alpha;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[t][r] = __builtin_amdgcn_exp2f(fmaf(s[t][r], p.scale_log2, -ref));
+        lsum += s[t][r];
+      }
+#pragma unroll
+      for (int cc = 0; cc < 2; ++cc) {
+        const bf16x8 pf = pack8(s[t], 8 * cc);
+#pragma unroll
+        for (int i = 0; i < DT; ++i) oacc[i] = mfma32(fo.tr_frag(Vs[wave][buf], 32 * t + 16 * cc, i), pf, oacc[i]);
+      }
+    }
+  };
+  for (int kt = first; kt < last; kt += 8) {
+    tile(kt, std::integral_constant<int, 0>());
+    if (kt + 4 < last) tile(kt + 4, std::integral_constant<int, 1>());
+  }
+
+  // the four waves' outputs, over their common reference, in their order: [query][column] of each in its own V tiles
+  lsum = reduce_halves(lsum, AddOp());
+  if (g == 0) { stat[wave][0][l32] = m; stat[wave][1][l32] = lsum; }
+  constexpr int OLD = DHP + 4;      // floats from query to query
+  static_assert(32 * OLD * 4 <= 2 * TILE * 2, "a wave's output lies in its V tiles");
+  float* mine = reinterpret_cast<float*>(Vs[wave][0]);
+  asm volatile("" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < DT; ++i)
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4)
+      *reinterpret_cast<f32x4*>(mine + l32 * OLD + 32 * i + 8 * r4 + 4 * g) = f32x4{oacc[i][4 * r4], oacc[i][4 * r4 + 1], oacc[i][4 * r4 + 2], oacc[i][4 * r4 + 3]};
+  __syncthreads();
+  for (int at = tid; at < 32 * (DHP / 4); at += 256) {
+    const int q = at / (DHP / 4), col = at % (DHP / 4) * 4, row = qtile * 32 + q;
+    if (row >= p.Nq || col >= p.dh) continue;
+    float top = fmaxf(fmaxf(stat[0][0][q], stat[1][0][q]), fmaxf(stat[2][0][q], stat[3][0][q])), sum = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float a = __builtin_amdgcn_exp2f(stat[w][0][q] - (top == -INFINITY ? 0.f : top));
+      sum = fmaf(a, stat[w][1][q], sum);
+      const f32x4 v = *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(Vs[w][0]) + q * OLD + col);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) o[u] = fmaf(a, v[u], o[u]);
+    }
+    const size_t srow = (size_t)bh * p.Nq + row;
+    if (p.shares > 1) {
+      const size_t rows = (size_t)p.B * p.H * p.Nq;
+      *reinterpret_cast<f32x4*>(p.part + (share * rows + srow) * p.dh + col) = o;
+      if (col == 0) *reinterpret_cast<u32x2*>(p.part + p.shares * rows * p.dh + 2 * (share * rows + srow)) = u32x2{__builtin_bit_cast(uint32_t, top), __builtin_bit_cast(uint32_t, sum)};
+    } else {
+      rel_store_o(p, o, sum, top, b, h, row, col);
+    }
+  }
+}
+
+// The shares of few queries, over their common reference, in their order; four columns a thread.
+__global__ void __launch_bounds__(256) rel_join_kernel(const RelAttnK p) {
+  const int per_row = p.dh / 4;
+  const size_t rows = (size_t)p.B * p.H * p.Nq, at = blockIdx.x * 256ul + threadIdx.x, srow = at / per_row;
+  if (srow >= rows) return;
+  const int col = (int)(at % per_row) * 4, bh = (int)(srow / p.Nq), row = (int)(srow % p.Nq);
+  const float* stat = p.part + p.shares * rows * p.dh;
+  float top = -INFINITY, sum = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int first = 0; first < p.shares; first += 8) {      // eight shares' values at once, behind what there is already
+    float m[8], l[8], most = top;
+    f32x4 v[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const size_t i = min(first + u, p.shares - 1) * rows + srow;
+      m[u] = stat[2 * i];
+      l[u] = stat[2 * i + 1];
+      v[u] = *reinterpret_cast<const f32x4*>(p.part + i * p.dh + col);
+      if (first + u >= p.shares) m[u] = -INFINITY;
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) most = fmaxf(most, m[u]);
+    const float ref = most == -INFINITY ? 0.f : most, keep = __builtin_amdgcn_exp2f(top - ref);
+    top = most;
+    sum *= keep;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) o[c] *= keep;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const float a = __builtin_amdgcn_exp2f(m[u] - ref);
+      if (first + u >= p.shares) continue;
+      sum = fmaf(a, l[u], sum);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) o[c] = fmaf(a, v[u][c], o[c]);
+    }
+  }
+  rel_store_o(p, o, sum, top, bh / p.H, bh % p.H, row, col);
+}
+
 // ------------------------------------------------------------------ dQ and the table's gradient (bf16)
 // Sums of dS over distances: [wave][entry].
 __host__ __device__ __forceinline__ int rel_sum_stride(const RelBucketsK& r) { return (rel_entries(r) + 3) / 4 * 4; }
@@ -287,7 +502,6 @@ __device__ __forceinline__ float rel_diagonals(const float* stage, int lane) {
 
 template <int DHP, int KC>
 __global__ void __launch_bounds__(256, DHP == 64 ? 3 : 2) rel_bwd_dq_bf16_kernel(const RelAttnK p, const RelStarts st) {
-  __shared__ uint16_t start[REL_MAX_BUCKETS / 2];
   constexpr int DT = DHP / 32, TILE = 64 * DHP;
   __shared__ __attribute__((aligned(1024))) bf16 Ks[2][TILE];
   __shared__ __attribute__((aligned(1024))) bf16 Vs[2][TILE];
@@ -318,8 +532,7 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 3 : 2) rel_bwd_dq_bf16_kernel
     ck.issue(kr, 0, p.ldk, Ks[0], wave);
     cv.issue(vr, 0, p.ldv, Vs[0], wave);
   }
-  rel_copy_starts(p.bk, st, start, 256);
-  rel_fill<bf16, false>(p, start, h, rel_lds, 256);
+  rel_fill<bf16, false>(p, st, h, rel_lds, 256);
   float* sums = rel_lds + rel_table_floats(p.bk);
   const int sum_stride = rel_sum_stride(p.bk);
   float* stage = sums + 4 * sum_stride + 32 + wave * REL_STAGE;      // (what is read of no query's keys lies within 32 floats before and behind)
@@ -462,8 +675,7 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 3 : 2) rel_bwd_dq_bf16_kernel
   for (int bucket = tid / 8; bucket < (p.bk.n_buckets + 31) / 32 * 32; bucket += 32) {
     const bool on = bucket < p.bk.n_buckets;
     const int side = on && p.bk.bidirectional && bucket >= p.bk.per_side, k = on ? bucket - side * p.bk.per_side : 0;
-    auto first_of = [&](int i) { return i < p.bk.half ? i : (i < p.bk.per_side ? (int)start[i - p.bk.half] : 1 << 28); };
-    const int n0 = first_of(k), n1 = first_of(k + 1) - 1;      // distances n0 .. n1 of this direction
+    const int n0 = rel_start(p.bk, st, k), n1 = rel_start(p.bk, st, k + 1) - 1;      // distances n0 .. n1 of this direction
     int d0, d1;
     if (side) d0 = max(n0, 1), d1 = min(n1, last);
     else d0 = max(-n1, first), d1 = -n0;
@@ -503,9 +715,8 @@ __global__ void __launch_bounds__(256) rel_dtable_kernel(const float* __restrict
 
 // ------------------------------------------------------------------ dK, dV (bf16)
 // Each wave owns 32 keys and walks the queries in tiles of 64, from the first that sees one of the workgroup's keys (see attn_bwd_dkv_bf16_kernel).
-template <int DHP, int KC, int MINW>
-__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(MINW, MINW))) rel_bwd_dkv_bf16_kernel(const RelAttnK p, const RelStarts st) {
-  __shared__ uint16_t start[REL_MAX_BUCKETS / 2];
+template <int DHP, int KC>
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) rel_bwd_dkv_bf16_kernel(const RelAttnK p, const RelStarts st) {
   constexpr int DT = DHP / 32, TILE = 64 * DHP;
   __shared__ __attribute__((aligned(1024))) bf16 Qs[2][TILE];
   __shared__ __attribute__((aligned(1024))) bf16 Ds[2][TILE];
@@ -548,8 +759,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(MINW, 
     if (wave == 1) dlt_s[buf][lane] = ok ? -stat : 0.f;
   };
   load_stats(qt0);
-  rel_copy_starts(p.bk, st, start, 256);
-  rel_fill<bf16, true>(p, start, h, rel_lds, 256);
+  rel_fill<bf16, true>(p, st, h, rel_lds, 256);
   const int tab = 4 * g + p.query0 - ki + p.bk.hi + REL_MARGIN;      // entry of this lane's first query
 
   bf16x8 kf[KC], vf[KC];
@@ -582,7 +792,6 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(MINW, 
     const bool below = k0 + 31 - pos <= p.bk.lo, above = k0 - pos - 63 >= p.bk.hi;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      if (MINW > 2) __builtin_amdgcn_sched_barrier(0);
       f32x16 s, dp;
 #pragma unroll
       for (int r4 = 0; r4 < 4; ++r4) {
@@ -633,7 +842,6 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(MINW, 
         }
       }
     }
-    if (MINW > 2) __builtin_amdgcn_sched_barrier(0);
     if (more) store_stats(qt + 1, buf ^ 1);
     wait_vmcnt<0>();
     __syncthreads();
@@ -662,12 +870,11 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(MINW, 
 
 // ------------------------------------------------------------------ fp32: a wave a row
 constexpr int REL_F32_MAX_D = 96;
-__device__ __forceinline__ float rel_bias_f32(const RelAttnK& p, const uint16_t* start, int h, int dist) {
-  return ((const float*)p.table)[(size_t)rel_bucket(p.bk, start, max(p.bk.lo, min(p.bk.hi, dist))) * p.H + h];
+__device__ __forceinline__ float rel_bias_f32(const RelAttnK& p, const RelStarts& st, int h, int dist) {
+  return ((const float*)p.table)[(size_t)rel_bucket(p.bk, st, max(p.bk.lo, min(p.bk.hi, dist))) * p.H + h];
 }
 
 __global__ void __launch_bounds__(64) rel_fwd_f32_kernel(const RelAttnK p, const RelStarts st) {
-  __shared__ uint16_t start[REL_MAX_BUCKETS / 2];
   extern __shared__ float sc[];        // [Nk]
   __shared__ float qs[REL_F32_MAX_D];
   const int lane = threadIdx.x, i = blockIdx.x % p.Nq, bh = blockIdx.x / p.Nq, b = bh / p.H, h = bh % p.H, pos = p.query0 + i;
@@ -675,7 +882,6 @@ __global__ void __launch_bounds__(64) rel_fwd_f32_kernel(const RelAttnK p, const
   const float* q = (const float*)p.q + ((size_t)b * p.Nq + i) * p.ldq + h * p.dh;
   const float* kb = (const float*)p.k + (size_t)b * p.Nk * p.ldk + h * p.dh;
   const float* vb = (const float*)p.v + (size_t)b * p.Nk * p.ldv + h * p.dh;
-  rel_copy_starts(p.bk, st, start, 64);
   for (int t = lane; t < p.dh; t += 64) qs[t] = q[t];
   __syncthreads();
   float mx = -INFINITY;
@@ -683,7 +889,7 @@ __global__ void __launch_bounds__(64) rel_fwd_f32_kernel(const RelAttnK p, const
     float s = 0.f;
 #pragma unroll 16
     for (int t = 0; t < p.dh; ++t) s = fmaf(qs[t], kb[(size_t)j * p.ldk + t], s);
-    s = fmaf(s, p.scale, rel_bias_f32(p, start, h, j - pos));
+    s = fmaf(s, p.scale, rel_bias_f32(p, st, h, j - pos));
     sc[j] = s;
     mx = fmaxf(mx, s);
   }
@@ -708,7 +914,6 @@ __global__ void __launch_bounds__(64) rel_fwd_f32_kernel(const RelAttnK p, const
 }
 
 __global__ void __launch_bounds__(64) rel_bwd_dq_f32_kernel(const RelAttnK p, const RelStarts st) {
-  __shared__ uint16_t start[REL_MAX_BUCKETS / 2];
   extern __shared__ float sc[];        // [Nk]
   __shared__ float qs[REL_F32_MAX_D], dos[REL_F32_MAX_D];
   const int lane = threadIdx.x, i = blockIdx.x % p.Nq, bh = blockIdx.x / p.Nq, b = bh / p.H, h = bh % p.H, pos = p.query0 + i;
@@ -721,7 +926,6 @@ __global__ void __launch_bounds__(64) rel_bwd_dq_f32_kernel(const RelAttnK p, co
   const size_t sidx = ((size_t)b * p.H + h) * p.Nq + i;
   const float l = p.lse[sidx], lse = l == -INFINITY ? INFINITY : l;
   float dlt = 0.f;
-  rel_copy_starts(p.bk, st, start, 64);
   for (int t = lane; t < p.dh; t += 64) { qs[t] = q[t]; dos[t] = dor[t]; dlt = fmaf(dor[t], orow[t], dlt); }
   dlt = wave_sum(dlt);
   if (lane == 0) p.delta[sidx] = dlt;
@@ -733,7 +937,7 @@ __global__ void __launch_bounds__(64) rel_bwd_dq_f32_kernel(const RelAttnK p, co
       s = fmaf(qs[t], kb[(size_t)j * p.ldk + t], s);
       dp = fmaf(dos[t], vb[(size_t)j * p.ldv + t], dp);
     }
-    sc[j] = expf(fmaf(s, p.scale, rel_bias_f32(p, start, h, j - pos)) - lse) * (dp - dlt);
+    sc[j] = expf(fmaf(s, p.scale, rel_bias_f32(p, st, h, j - pos)) - lse) * (dp - dlt);
   }
   __syncthreads();
   float* dq = (float*)p.dq + ((size_t)b * p.Nq + i) * p.lddq + h * p.dh;
@@ -747,8 +951,7 @@ __global__ void __launch_bounds__(64) rel_bwd_dq_f32_kernel(const RelAttnK p, co
   float* out = p.dtable_partial + (((size_t)h * p.B + b) * p.Nq + i) * p.bk.n_buckets;
   for (int bucket = lane; bucket < p.bk.n_buckets; bucket += 64) {      // a lane adds its bucket's keys
     const int side = p.bk.bidirectional && bucket >= p.bk.per_side, k = bucket - side * p.bk.per_side;
-    auto first_of = [&](int n) { return n < p.bk.half ? n : (n < p.bk.per_side ? (int)start[n - p.bk.half] : 1 << 30); };
-    const int n0 = first_of(k), n1 = first_of(k + 1) - 1;
+    const int n0 = rel_start(p.bk, st, k), n1 = rel_start(p.bk, st, k + 1) - 1;
     int j0 = side ? pos + max(n0, 1) : pos - n1, j1 = min(lim - 1, side ? pos + n1 : pos - n0);
     if (!p.bk.bidirectional && k == 0) j1 = lim - 1;
     float v = 0.f;
@@ -758,7 +961,6 @@ __global__ void __launch_bounds__(64) rel_bwd_dq_f32_kernel(const RelAttnK p, co
 }
 
 __global__ void __launch_bounds__(64) rel_bwd_dkv_f32_kernel(const RelAttnK p, const RelStarts st) {
-  __shared__ uint16_t start[REL_MAX_BUCKETS / 2];
   extern __shared__ float sc[];        // [2][Nq]: P and dS
   __shared__ float ks[REL_F32_MAX_D], vs[REL_F32_MAX_D];
   const int lane = threadIdx.x, j = blockIdx.x % p.Nk, bh = blockIdx.x / p.Nk, b = bh / p.H, h = bh % p.H;
@@ -774,7 +976,6 @@ __global__ void __launch_bounds__(64) rel_bwd_dkv_f32_kernel(const RelAttnK p, c
   const float* dob = (const float*)p.dout + (size_t)b * p.Nq * p.lddo + h * p.dh;
   const float* lse_b = p.lse + ((size_t)b * p.H + h) * p.Nq;
   const float* dlt_b = p.delta + ((size_t)b * p.H + h) * p.Nq;
-  rel_copy_starts(p.bk, st, start, 64);
   for (int t = lane; t < p.dh; t += 64) { ks[t] = kr[t]; vs[t] = vr[t]; }
   __syncthreads();
   const int i0 = p.causal ? max(0, j - p.query0) : 0;
@@ -786,7 +987,7 @@ __global__ void __launch_bounds__(64) rel_bwd_dkv_f32_kernel(const RelAttnK p, c
       dp = fmaf(dob[(size_t)i * p.lddo + t], vs[t], dp);
     }
     const float l = lse_b[i];
-    const float pr = expf(fmaf(s, p.scale, rel_bias_f32(p, start, h, j - p.query0 - i)) - (l == -INFINITY ? INFINITY : l));
+    const float pr = expf(fmaf(s, p.scale, rel_bias_f32(p, st, h, j - p.query0 - i)) - (l == -INFINITY ? INFINITY : l));
     pp[i] = pr;
     dsp[i] = pr * (dp - dlt_b[i]);
   }
@@ -836,18 +1037,20 @@ static int rel_buckets(const char* who, int n_buckets, int max_distance, int bid
   if (r.per_side < 2) return set_errorf(DP_EINVAL, "%s: a direction needs two buckets", who);
   if (max_distance <= r.half) return set_errorf(DP_EINVAL, "%s: the largest distance must exceed %d, the buckets of one distance each", who, r.half);
   const int rest = r.per_side - r.half;
-  st.of[0] = (uint16_t)r.half;
-  for (int k = 1; k < rest; ++k) {
+  memset(&st, 0xFF, sizeof(st));
+  int last = r.half;
+  for (int k = 0; k < rest; ++k) {
     const double border = r.half * pow((double)max_distance / r.half, (double)k / rest), near = nearbyint(border);
     int n = (int)ceil(border);
     if (fabs(border - near) < 1e-6) {
       n = (int)near;
       if (rel_less(rel_power((uint32_t)n, rest, (uint32_t)r.half, k), rel_power((uint32_t)max_distance, k, (uint32_t)r.half, rest))) ++n;
     }
-    st.of[k] = (uint16_t)n;
+    ((uint16_t*)st.of)[k] = (uint16_t)n;
+    last = n;
   }
-  r.lo = -(int)st.of[rest - 1];
-  r.hi = bidirectional ? st.of[rest - 1] : 0;
+  r.lo = -last;
+  r.hi = bidirectional ? last : 0;
   return DP_OK;
 }
 
@@ -865,7 +1068,7 @@ static RelWorkspace rel_workspace(int B, int H, int Nq, int n_buckets) {
 
 // Dynamic LDS beyond 64 KB in all has to be asked for, once per kernel and device; asking again does no harm.
 template <class K> static int rel_allow_lds(K kern, int dhp, int bytes) {
-  if (512 * dhp + 1088 + bytes <= 64 * 1024) return DP_OK;      // (two stages of two tiles, and a few rows of statistics)
+  if (512 * dhp + 2048 + bytes <= 64 * 1024) return DP_OK;      // (two stages of two tiles, and a few rows of statistics)
   if (hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return set_error(DP_EHIP, "hipFuncSetAttribute(attention) failed");
   return DP_OK;
 }
@@ -881,6 +1084,23 @@ static int rel_launched() {
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? DP_OK : set_errorf(DP_EHIP, "attention with a relative position bias: launch failed (%s)", hipGetErrorString(e));
 }
+
+// Shares of the keys for workgroups of 32 queries: until three workgroups a CU are there, none with less than two tiles for each of its waves.  16 x 12 heads, one
+// query, 4000 keys: 1 / 2 / 3 / 4 / 5 / 8 shares 44 / 40 / 41 / 36 / 37 / 38 us, keys of different lengths 37 / 33 / 30 / 26 / 27 / 28; 12 heads 31 / 19 / 15 / 12 / 11 / 9.
+static int rel_shares(int B, int H, int Nq, int Nk) {
+  const long blocks = (long)B * H * ((Nq + 31) / 32), tiles = (Nk + 63) / 64;
+  return (int)std::max<long>(1, std::min<long>((tiles + 7) / 8, (768 + blocks - 1) / blocks));
+}
+// Whether the forward takes 32 queries a workgroup and shares the keys out, instead of 128 queries that read each key once: where those are too few for
+// the CUs and these all run at once.  Heads, queries x keys, width, us by 32 (with what joins the shares) and by 128: 8, 64 x 4096, 64 14.8 / 65.6; 8, 256 x 4096, 64 18.9 / 66.4; 8,
+// 1024 x 1024, 64 16.4 / 20.8; 4, 2000 x 2000, 40 24 / 30.4; 32, 512 x 512, 64 12.9 / 14.2; 64, 128 x 256, 64 7.7 / 9.8; 32, 200 x 512, 72 11.8 / 14.4; but 32, 300 x 1000, 72 34.5 / 22.3;
+// 144, 77 x 77, 64 8.3 / 7.8; 768, 77 x 77, 64 29.7 / 13.1.
+static bool rel_few(int B, int H, int Nq, int Nk, int d_head) {
+  if (Nq <= 32) return true;
+  const long blocks = (long)B * H * ((Nq + 31) / 32);
+  return blocks <= (d_head <= 64 && Nk > 128 ? 512 : 256);
+}
+static size_t rel_share_bytes(int B, int H, int Nq, int d_head, int shares) { return shares > 1 ? align_up((size_t)shares * B * H * Nq * (d_head + 2) * sizeof(float), 256) : 0; }
 
 static int check_rel(const char* who, int dtype, const RelAttnK& k, const dp_relbias* bias, bool bwd) {
   if (dtype != DP_F32 && dtype != DP_BF16) return set_error(DP_EINVAL, "unknown dtype");
@@ -929,13 +1149,14 @@ int dp_relative_bucket(int n_buckets, int max_distance, int bidirectional, int d
   const int n = bidirectional ? (distance < 0 ? -(int64_t)distance > INT32_MAX ? INT32_MAX : -distance : distance) : (distance < 0 ? (distance == INT32_MIN ? INT32_MAX : -distance) : 0);
   const int side = bidirectional && distance > 0 ? r.per_side : 0;
   if (n < r.half) return side + n;
-  const int k = (int)(std::upper_bound(st.of, st.of + (r.per_side - r.half), n) - st.of) - 1;
+  const int k = (int)(std::upper_bound((const uint16_t*)st.of, (const uint16_t*)st.of + (r.per_side - r.half), n) - (const uint16_t*)st.of) - 1;
   return side + r.half + k;
 }
 
 size_t dp_op_attention_relbias_workspace_bytes(int B, int H, int Nq, int Nk, int d_head, int n_buckets, int backward) {
   if (B <= 0 || H <= 0 || Nq <= 0 || Nk <= 0 || d_head <= 0 || n_buckets <= 0) return 0;
-  return backward ? rel_workspace(B, H, Nq, n_buckets).bytes : 0;
+  if (backward) return rel_workspace(B, H, Nq, n_buckets).bytes;
+  return rel_few(B, H, Nq, Nk, d_head) ? rel_share_bytes(B, H, Nq, d_head, rel_shares(B, H, Nq, Nk)) : 0;
 }
 
 int dp_op_attention_relbias_fwd(int dtype, int B, int H, int Nq, int Nk, int d_head, int causal, float scale, const void* q, int ldq, const void* k,
@@ -945,7 +1166,7 @@ int dp_op_attention_relbias_fwd(int dtype, int B, int H, int Nq, int Nk, int d_h
   RelAttnK a{};
   RelStarts st;
   a.B = B; a.H = H; a.Nq = Nq; a.Nk = Nk; a.dh = d_head; a.causal = causal != 0; a.query0 = bias ? bias->query0 : 0;
-  a.scale = scale; a.scale_log2 = scale * LOG2E; a.inv_scale = 1.0f / scale;
+  a.scale = scale; a.scale_log2 = scale * LOG2E; a.inv_scale = 1.0f / scale; a.shares = 1;
   a.q = q; a.ldq = ldq; a.k = k; a.ldk = ldk; a.v = v; a.ldv = ldv; a.table = bias ? bias->table : nullptr; a.key_len = key_len; a.o = o; a.ldo = ldo; a.lse = lse;
   DP_TRY(check_rel(who, dtype, a, bias, false));
   DP_TRY(rel_buckets(who, bias->n_buckets, bias->max_distance, bias->bidirectional, a.bk, st));
@@ -955,8 +1176,26 @@ int dp_op_attention_relbias_fwd(int dtype, int B, int H, int Nq, int Nk, int d_h
     hipLaunchKernelGGL(rel_fwd_f32_kernel, dim3((unsigned)(B * H) * Nq), dim3(64), (size_t)Nk * sizeof(float), s, a, st);
     return rel_launched();
   }
-  const long blocks = (long)((Nq + 127) / 128) * B * H;
   const int lds = rel_table_floats(a.bk) * 4;
+  if (rel_few(B, H, Nq, Nk, d_head)) {
+    if (workspace) {
+      const int shares = rel_shares(B, H, Nq, Nk);
+      const size_t need = rel_share_bytes(B, H, Nq, d_head, shares);
+      if ((uintptr_t)workspace % 256) return set_errorf(DP_EALIGN, "%s: workspace is not 256-byte aligned", who);
+      if (workspace_bytes < need) return set_errorf(DP_EWORKSPACE, "%s: workspace too small (%zu bytes, needs %zu)", who, workspace_bytes, need);
+      a.shares = shares;
+      a.part = (float*)workspace;
+    }
+    DP_TRY(rel_dispatch(d_head, [&](auto dhp, auto kc) {
+      DP_TRY(rel_allow_lds(rel_fwd_few_bf16_kernel<dhp, kc>, 2 * dhp, lds));
+      hipLaunchKernelGGL((rel_fwd_few_bf16_kernel<dhp, kc>), dim3((unsigned)((Nq + 31) / 32 * B * H * a.shares)), dim3(256), lds, s, a, st);
+      return rel_launched();
+    }));
+    if (a.shares == 1) return DP_OK;
+    hipLaunchKernelGGL(rel_join_kernel, dim3((unsigned)(((size_t)B * H * Nq * (d_head / 4) + 255) / 256)), dim3(256), 0, s, a);
+    return rel_launched();
+  }
+  const long blocks = (long)((Nq + 127) / 128) * B * H;
   a.even = rel_takes_turns(blocks, d_head <= 64 ? 4 : 3);
   return rel_dispatch(d_head, [&](auto dhp, auto kc) {
     constexpr int W = dhp == 64 ? 4 : 3;
@@ -1010,8 +1249,8 @@ int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_h
     KScope ks(KK_ATTN_BWD_DKV, fl, by, s, Nq, Nk, d_head);
     a.even = rel_takes_turns(kblocks, 2);
     DP_TRY(rel_dispatch(d_head, [&](auto dhp, auto kc) {
-      DP_TRY(rel_allow_lds(rel_bwd_dkv_bf16_kernel<dhp, kc, 2>, dhp, table));
-      hipLaunchKernelGGL((rel_bwd_dkv_bf16_kernel<dhp, kc, 2>), dim3((unsigned)kblocks), dim3(256), table, s, a, st);
+      DP_TRY(rel_allow_lds(rel_bwd_dkv_bf16_kernel<dhp, kc>, dhp, table));
+      hipLaunchKernelGGL((rel_bwd_dkv_bf16_kernel<dhp, kc>), dim3((unsigned)kblocks), dim3(256), table, s, a, st);
       return rel_launched();
     }));
   }

@@ -85,15 +85,17 @@ __host__ __device__ __forceinline__ int rel_entries(const RelBucketsK& r) { retu
 __host__ __device__ __forceinline__ int rel_table_floats(const RelBucketsK& r) { return (rel_entries(r) + 3) / 4 * 4; }
 __device__ __forceinline__ int rel_keys(const RelAttnK& p, int b) { return p.key_len ? max(0, min(p.key_len[b], p.Nk)) : p.Nk; }
 
-// Bias over scale of head h by distance.  Entry e is distance lo - margin + e, or, REVERSED, hi + margin - e.
+// Bias of head h by distance, times a factor.  Entry e is distance lo - margin + e, or, REVERSED, hi + margin - e.
 template <typename T, bool REVERSED>
-__device__ __forceinline__ void rel_fill(const RelAttnK& p, const RelStarts& st, int h, float* tab, int threads) {
+__device__ __forceinline__ void rel_fill(const RelAttnK& p, const RelStarts& st, int h, float* tab, int threads, float factor) {
   const int n = rel_entries(p.bk);
   for (int e = threadIdx.x; e < n; e += threads) {
     const int dist = REVERSED ? p.bk.hi + REL_MARGIN - e : p.bk.lo - REL_MARGIN + e;
-    tab[e] = to_f<T>(((const T*)p.table)[(size_t)rel_bucket(p.bk, st, dist) * p.H + h]) * p.inv_scale;
+    tab[e] = to_f<T>(((const T*)p.table)[(size_t)rel_bucket(p.bk, st, dist) * p.H + h]) * factor;
   }
 }
+// The same in all lanes, hence in a scalar register
+__device__ __forceinline__ float rel_uniform(float v) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v))); }
 // Four neighbouring entries
 __device__ __forceinline__ f32x4 rel_read4(const float* t) { return f32x4{t[0], t[1], t[2], t[3]}; }
 
@@ -147,7 +149,7 @@ __global__ void __launch_bounds__(256, MINW) rel_fwd_bf16_kernel(const RelAttnK 
     ck.issue(kr, 0, p.ldk, Ks[0], wave);
     cv.issue(vr, 0, p.ldv, Vs[0], wave);
   }
-  rel_fill<bf16, false>(p, st, h, rel_lds, 256);
+  rel_fill<bf16, false>(p, st, h, rel_lds, 256, p.inv_scale);
   const int tab = 4 * g - pos - (bk_lo - REL_MARGIN);      // entry of this lane's first key
 
   bf16x8 qf[KC];
@@ -161,7 +163,7 @@ __global__ void __launch_bounds__(256, MINW) rel_fwd_bf16_kernel(const RelAttnK 
     for (int r = 0; r < 16; ++r) oacc[i][r] = 0.f;
   wait_vmcnt<0>();
   __syncthreads();
-  const float far_lo = rel_lds[0], far_hi = rel_lds[rel_entries(p.bk) - 1];
+  const float far_lo = rel_uniform(rel_lds[0]), far_hi = rel_uniform(rel_lds[rel_entries(p.bk) - 1]);
 
   for (int kt = 0; kt < nkt; ++kt) {
     const int buf = kt & 1;
@@ -325,7 +327,7 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 2 : 1) rel_fwd_few_bf16_kerne
     for (int w = 0; w < 4; ++w) cv[w].issue(vr, kt * 64, p.ldv, Vs[wave][buf], w);
   };
   if (first < last) request(first, 0);
-  rel_fill<bf16, false>(p, st, h, rel_lds, 256);
+  rel_fill<bf16, false>(p, st, h, rel_lds, 256, p.inv_scale);
   const int tab = 4 * g - pos - (bk_lo - REL_MARGIN);
   bf16x8 qf[KC];
   const bf16* qrow = (const bf16*)p.q + ((size_t)b * p.Nq + qi) * p.ldq + h * p.dh;
@@ -338,7 +340,7 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 2 : 1) rel_fwd_few_bf16_kerne
 #pragma unroll
     for (int r = 0; r < 16; ++r) oacc[i][r] = 0.f;
   __syncthreads();
-  const float far_lo = rel_lds[0], far_hi = rel_lds[rel_entries(p.bk) - 1];
+  const float far_lo = rel_uniform(rel_lds[0]), far_hi = rel_uniform(rel_lds[rel_entries(p.bk) - 1]);
 
   auto tile = [&](int kt, auto bc) __attribute__((always_inline)) {
     constexpr int buf = bc();
@@ -500,6 +502,60 @@ __device__ __forceinline__ float rel_diagonals(const float* stage, int lane) {
   return v;
 }
 
+// Adds a block of dS, 32 queries (lanes) x 32 keys, along its diagonals to the wave's sums over distances; mine: where this lane's distance of its first key lies.
+__device__ __forceinline__ void rel_add_diagonals(const f32x16& s, float* stage, float* mine, int g, int l32, int lane) {
+#pragma unroll
+  for (int part = 0; part < 32 / REL_SQ; ++part) {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (l32 / REL_SQ == part) {
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4)
+        *reinterpret_cast<f32x4*>(stage + l32 % REL_SQ * 36 + 8 * r4 + 4 * g) = f32x4{s[4 * r4], s[4 * r4 + 1], s[4 * r4 + 2], s[4 * r4 + 3]};
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    mine[-REL_SQ * part] += rel_diagonals(stage, lane);
+  }
+}
+
+// The end of a dQ workgroup: the waves' sums of a distance, then the distances of a bucket (eight lanes each), then what lay beyond the middle.
+__device__ __forceinline__ void rel_bucket_sums(const RelAttnK& p, const RelStarts& st, float* sums, int sum_stride, float (&far_sums)[2][4], float far_sum_lo,
+                                                float far_sum_hi, float* out) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, entries = rel_entries(p.bk);
+  far_sum_lo = wave_sum(far_sum_lo);
+  far_sum_hi = wave_sum(far_sum_hi);
+  if (lane == 0) { far_sums[0][wave] = far_sum_lo; far_sums[1][wave] = far_sum_hi; }
+  __syncthreads();
+  for (int e = tid; e < entries; e += 256) {
+    float v = sums[e];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) v += sums[w * sum_stride + e];
+    sums[e] = v;
+  }
+  __syncthreads();
+  const int first = p.bk.lo - REL_MARGIN, last = p.bk.hi + REL_MARGIN;
+  for (int bucket = tid / 8; bucket < (p.bk.n_buckets + 31) / 32 * 32; bucket += 32) {
+    const bool on = bucket < p.bk.n_buckets;
+    const int side = on && p.bk.bidirectional && bucket >= p.bk.per_side, k = on ? bucket - side * p.bk.per_side : 0;
+    const int n0 = rel_start(p.bk, st, k), n1 = rel_start(p.bk, st, k + 1) - 1;      // distances n0 .. n1 of this direction
+    int d0, d1;
+    if (side) d0 = max(n0, 1), d1 = min(n1, last);
+    else d0 = max(-n1, first), d1 = -n0;
+    if (!p.bk.bidirectional && k == 0) d1 = last;        // keys behind the query
+    float v = 0.f;
+    if (on)
+      for (int d = d0 + tid % 8; d <= d1; d += 8) v += sums[d - first];
+    v += lane_dpp<0xB1>(v);       // lanes i ^ 1, i ^ 2, i ^ 7 (by then equal within four): the eight of a bucket
+    v += lane_dpp<0x4E>(v);
+    v += lane_dpp<0x141>(v);      // row_half_mirror
+    if (on && tid % 8 == 0) {
+      const int lo_bucket = p.bk.per_side - 1, hi_bucket = p.bk.bidirectional ? 2 * p.bk.per_side - 1 : 0;
+      if (bucket == lo_bucket) v += (far_sums[0][0] + far_sums[0][1]) + (far_sums[0][2] + far_sums[0][3]);
+      if (bucket == hi_bucket) v += (far_sums[1][0] + far_sums[1][1]) + (far_sums[1][2] + far_sums[1][3]);
+      out[bucket] = v;
+    }
+  }
+}
+
 template <int DHP, int KC>
 __global__ void __launch_bounds__(256, DHP == 64 ? 3 : 2) rel_bwd_dq_bf16_kernel(const RelAttnK p, const RelStarts st) {
   constexpr int DT = DHP / 32, TILE = 64 * DHP;
@@ -508,14 +564,14 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 3 : 2) rel_bwd_dq_bf16_kernel
   __shared__ float far_sums[2][4];
   extern __shared__ __attribute__((aligned(16))) float rel_lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, l32 = lane & 31;
-  const int qtiles = (p.Nq + 127) / 128, entries = rel_entries(p.bk);
+  const int qtiles = (p.Nq + 127) / 128, entries = rel_entries(p.bk), bk_lo = p.bk.lo, bk_hi = p.bk.hi;
   int qtile, bh;
   rel_block_map(p, blockIdx.x, qtiles, true, qtile, bh);
   const int b = bh / p.H, h = bh % p.H;
   const int q0 = qtile * 128 + wave * 32, qi = q0 + l32, pos0 = p.query0 + q0, pos = pos0 + l32;
   const bool qok = qi < p.Nq;
   const int keys = __builtin_amdgcn_readfirstlane(rel_keys(p, b));
-  const int lim = p.causal ? min(keys, pos + 1) : keys, lim_all = p.causal ? min(keys, pos0 + 1) : keys;
+  const int lim = p.causal ? min(keys, pos + 1) : keys, lim_all = p.causal ? min(keys, pos0 + 1) : keys, lim_wave = p.causal ? min(keys, pos0 + 32) : keys;
   const int lim_any = p.causal ? min(keys, p.query0 + min(p.Nq, qtile * 128 + 128)) : keys;
   const int nkt = __builtin_amdgcn_readfirstlane(lim_any > 0 ? (lim_any + 63) / 64 : 0);
   const u32x4 kr = make_raw_rsrc((const bf16*)p.k + (size_t)b * p.Nk * p.ldk + h * p.dh, rel_slice_bytes(keys, p.ldk, p.dh));
@@ -532,7 +588,7 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 3 : 2) rel_bwd_dq_bf16_kernel
     ck.issue(kr, 0, p.ldk, Ks[0], wave);
     cv.issue(vr, 0, p.ldv, Vs[0], wave);
   }
-  rel_fill<bf16, false>(p, st, h, rel_lds, 256);
+  rel_fill<bf16, false>(p, st, h, rel_lds, 256, p.inv_scale);
   float* sums = rel_lds + rel_table_floats(p.bk);
   const int sum_stride = rel_sum_stride(p.bk);
   float* stage = sums + 4 * sum_stride + 32 + wave * REL_STAGE;      // (what is read of no query's keys lies within 32 floats before and behind)
@@ -566,6 +622,9 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 3 : 2) rel_bwd_dq_bf16_kernel
     dlt = reduce_halves(dlt, AddOp());
     if (qok && g == 0) p.delta[sidx] = dlt;
   }
+  f32x16 ndelta;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) ndelta[r] = -dlt;
   f32x16 acc[DT];
 #pragma unroll
   for (int i = 0; i < DT; ++i)
@@ -573,7 +632,7 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 3 : 2) rel_bwd_dq_bf16_kernel
     for (int r = 0; r < 16; ++r) acc[i][r] = 0.f;
   wait_vmcnt<0>();
   __syncthreads();
-  const float far_lo = rel_lds[0], far_hi = rel_lds[entries - 1];
+  const float far_lo = rel_uniform(rel_lds[0]), far_hi = rel_uniform(rel_lds[entries - 1]);
 
   auto tile = [&](int kt, auto bc) {
     take_turns(p.even, kt);
@@ -582,14 +641,15 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 3 : 2) rel_bwd_dq_bf16_kernel
       ck.issue(kr, (kt + 1) * 64, p.ldk, Ks[buf ^ 1], wave);
       cv.issue(vr, (kt + 1) * 64, p.ldv, Vs[buf ^ 1], wave);
     }
-    const bool below = kt * 64 + 63 - pos0 <= p.bk.lo, above = kt * 64 - pos0 - 31 >= p.bk.hi;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
+      if (kt * 64 + 32 * t >= lim_wave) continue;      // (masked throughout)
+      const bool below = kt * 64 + 32 * t + 31 - pos0 <= bk_lo, above = kt * 64 + 32 * t - pos0 - 31 >= bk_hi;
       f32x16 s, dp;
+      float minus = -lse2;
       if (below || above) {
-        const float far = below ? far_lo : far_hi;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = far;
+        minus += (below ? far_lo : far_hi) * p.scale_log2;
+        s = mfma32(fo.row_frag(Ks[buf], t, 0), qf[0], f32x16{});
       } else {
 #pragma unroll
         for (int r4 = 0; r4 < 4; ++r4) {
@@ -597,20 +657,20 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 3 : 2) rel_bwd_dq_bf16_kernel
 #pragma unroll
           for (int u = 0; u < 4; ++u) s[4 * r4 + u] = v[u];
         }
+        s = mfma32(fo.row_frag(Ks[buf], t, 0), qf[0], s);
       }
+      dp = mfma32(fo.row_frag(Vs[buf], t, 0), dof[0], ndelta);      // dP - delta: the products accumulate onto -delta
 #pragma unroll
-      for (int r = 0; r < 16; ++r) dp[r] = -dlt;      // dP - delta: the products accumulate onto -delta
-#pragma unroll
-      for (int c = 0; c < KC; ++c) {
+      for (int c = 1; c < KC; ++c) {
         s = mfma32(fo.row_frag(Ks[buf], t, c), qf[c], s);
         dp = mfma32(fo.row_frag(Vs[buf], t, c), dof[c], dp);
       }
-      if (kt * 64 + 64 > lim_all) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = kt * 64 + 32 * t + acc_row(r, g) < lim ? s[r] : -INFINITY;
+      for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], p.scale_log2, minus)) * dp[r];
+      if (kt * 64 + 32 * t + 32 > lim_all) {      // (here and not before the exponential: what is masked counts for nothing whatever it is)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = kt * 64 + 32 * t + acc_row(r, g) < lim ? s[r] : 0.f;
       }
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], p.scale_log2, -lse2)) * dp[r];
       if (below || above) {
         float sum = 0.f;
 #pragma unroll
@@ -618,18 +678,7 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 3 : 2) rel_bwd_dq_bf16_kernel
         if (below) far_sum_lo += sum;
         else far_sum_hi += sum;
       } else {
-#pragma unroll
-        for (int part = 0; part < 32 / REL_SQ; ++part) {
-          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-          if (l32 / REL_SQ == part) {
-#pragma unroll
-            for (int r4 = 0; r4 < 4; ++r4)
-              *reinterpret_cast<f32x4*>(stage + l32 % REL_SQ * 36 + 8 * r4 + 4 * g) = f32x4{s[4 * r4], s[4 * r4 + 1], s[4 * r4 + 2], s[4 * r4 + 3]};
-          }
-          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-          const float v = rel_diagonals(stage, lane);
-          sums[mine + kt * 64 + 32 * t - REL_SQ * part] += v;
-        }
+        rel_add_diagonals(s, stage, sums + (mine + kt * 64 + 32 * t), g, l32, lane);
       }
 #pragma unroll
       for (int cc = 0; cc < 2; ++cc) {
@@ -657,42 +706,7 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 3 : 2) rel_bwd_dq_bf16_kernel
         }
       }
   }
-  if (!p.dtable_partial) return;
-  // the four sums of a distance, then the distances of a bucket: eight lanes each
-  far_sum_lo = wave_sum(far_sum_lo);
-  far_sum_hi = wave_sum(far_sum_hi);
-  if (lane == 0) { far_sums[0][wave] = far_sum_lo; far_sums[1][wave] = far_sum_hi; }
-  __syncthreads();
-  for (int e = tid; e < entries; e += 256) {
-    float v = sums[e];
-#pragma unroll
-    for (int w = 1; w < 4; ++w) v += sums[w * sum_stride + e];
-    sums[e] = v;
-  }
-  __syncthreads();
-  float* out = p.dtable_partial + ((size_t)h * p.B * qtiles + (size_t)b * qtiles + qtile) * p.bk.n_buckets;
-  const int first = p.bk.lo - REL_MARGIN, last = p.bk.hi + REL_MARGIN;
-  for (int bucket = tid / 8; bucket < (p.bk.n_buckets + 31) / 32 * 32; bucket += 32) {
-    const bool on = bucket < p.bk.n_buckets;
-    const int side = on && p.bk.bidirectional && bucket >= p.bk.per_side, k = on ? bucket - side * p.bk.per_side : 0;
-    const int n0 = rel_start(p.bk, st, k), n1 = rel_start(p.bk, st, k + 1) - 1;      // distances n0 .. n1 of this direction
-    int d0, d1;
-    if (side) d0 = max(n0, 1), d1 = min(n1, last);
-    else d0 = max(-n1, first), d1 = -n0;
-    if (!p.bk.bidirectional && k == 0) d1 = last;        // keys behind the query
-    float v = 0.f;
-    if (on)
-      for (int d = d0 + tid % 8; d <= d1; d += 8) v += sums[d - first];
-    v += lane_dpp<0xB1>(v);       // lanes i ^ 1, i ^ 2, i ^ 7 (by then equal within four): the eight of a bucket
-    v += lane_dpp<0x4E>(v);
-    v += lane_dpp<0x141>(v);      // row_half_mirror
-    if (on && tid % 8 == 0) {
-      const int lo_bucket = p.bk.per_side - 1, hi_bucket = p.bk.bidirectional ? 2 * p.bk.per_side - 1 : 0;
-      if (bucket == lo_bucket) v += (far_sums[0][0] + far_sums[0][1]) + (far_sums[0][2] + far_sums[0][3]);
-      if (bucket == hi_bucket) v += (far_sums[1][0] + far_sums[1][1]) + (far_sums[1][2] + far_sums[1][3]);
-      out[bucket] = v;
-    }
-  }
+  if (p.dtable_partial) rel_bucket_sums(p, st, sums, sum_stride, far_sums, far_sum_lo, far_sum_hi, p.dtable_partial + ((size_t)h * p.B * qtiles + (size_t)b * qtiles + qtile) * p.bk.n_buckets);
 }
 
 // dtable[bucket][head] = sum over the parts, in their order: 32 buckets of a head a workgroup, eight shares of the parts.
@@ -714,7 +728,9 @@ __global__ void __launch_bounds__(256) rel_dtable_kernel(const float* __restrict
 }
 
 // ------------------------------------------------------------------ dK, dV (bf16)
-// Each wave owns 32 keys and walks the queries in tiles of 64, from the first that sees one of the workgroup's keys (see attn_bwd_dkv_bf16_kernel).
+// Each wave owns 32 keys and walks the queries in tiles of 64, from the first that sees one of the workgroup's keys (see attn_bwd_dkv_bf16_kernel).  The
+// bias is the addend of the exponent here, and lse what the scores begin with.  Two waves per SIMD: three need 168 registers, and what is spilled
+// for them in the loop costs more than they give (8 x 10 heads of 1024 70 -> 71 us, causal 41 -> 58; 8 x 5 of 4096 370 -> 436).
 template <int DHP, int KC>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) rel_bwd_dkv_bf16_kernel(const RelAttnK p, const RelStarts st) {
   constexpr int DT = DHP / 32, TILE = 64 * DHP;
@@ -724,6 +740,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
   __shared__ __attribute__((aligned(16))) float dlt_s[2][64];
   extern __shared__ __attribute__((aligned(16))) float rel_lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, l32 = lane & 31;
+  const int bk_lo = p.bk.lo, bk_hi = p.bk.hi;
   int ktile, bh;
   rel_block_map(p, blockIdx.x, (p.Nk + 127) / 128, false, ktile, bh);
   const int b = bh / p.H, h = bh % p.H;
@@ -755,11 +772,11 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
   };
   auto store_stats = [&](int qt, int buf) {
     const bool ok = qt * 64 + lane < p.Nq;
-    if (wave == 0) lse_s[buf][lane] = ok && stat != -INFINITY ? stat * LOG2E : INFINITY;      // (a query that sees no key has no probabilities)
+    if (wave == 0) lse_s[buf][lane] = ok && stat != -INFINITY ? -stat * p.inv_scale : -INFINITY;      // (a query that sees no key has no probabilities)
     if (wave == 1) dlt_s[buf][lane] = ok ? -stat : 0.f;
   };
   load_stats(qt0);
-  rel_fill<bf16, true>(p, st, h, rel_lds, 256);
+  rel_fill<bf16, true>(p, st, h, rel_lds, 256, LOG2E);
   const int tab = 4 * g + p.query0 - ki + p.bk.hi + REL_MARGIN;      // entry of this lane's first query
 
   bf16x8 kf[KC], vf[KC];
@@ -777,7 +794,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
   store_stats(qt0, 0);
   wait_vmcnt<0>();
   __syncthreads();
-  const float far_hi = rel_lds[0], far_lo = rel_lds[rel_entries(p.bk) - 1];
+  const float far_hi = rel_uniform(rel_lds[0]), far_lo = rel_uniform(rel_lds[rel_entries(p.bk) - 1]);
 
   auto tile = [&](int qt, auto bc) {
     take_turns(p.even, qt);
@@ -789,46 +806,43 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
       load_stats(qt + 1);
     }
     const int pos = p.query0 + qt * 64;      // of the tile's first query; distances k0 - pos - 63 .. k0 + 31 - pos
-    const bool below = k0 + 31 - pos <= p.bk.lo, above = k0 - pos - 63 >= p.bk.hi;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      f32x16 s, dp;
+      if (p.causal && k0 > pos + 32 * t + 31) continue;
+      const bool below = k0 + 31 - pos - 32 * t <= bk_lo, above = k0 - pos - 32 * t - 31 >= bk_hi;
+      f32x16 s, dp;      // S less lse, over the scale, and dP less delta: the products accumulate onto them.  The bias is the addend of the exponent
 #pragma unroll
       for (int r4 = 0; r4 < 4; ++r4) {
-        const f32x4 d4 = *reinterpret_cast<const f32x4*>(&dlt_s[buf][32 * t + 8 * r4 + 4 * g]);
+        const f32x4 l4 = *reinterpret_cast<const f32x4*>(&lse_s[buf][32 * t + 8 * r4 + 4 * g]), d4 = *reinterpret_cast<const f32x4*>(&dlt_s[buf][32 * t + 8 * r4 + 4 * g]);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) dp[4 * r4 + u] = d4[u];
-      }
-      if (below || above) {
-        const float far = below ? far_lo : far_hi;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = far;
-      } else {
-#pragma unroll
-        for (int r4 = 0; r4 < 4; ++r4) {
-          const f32x4 v = rel_read4(rel_lds + (tab + qt * 64) + 32 * t + 8 * r4);
-#pragma unroll
-          for (int u = 0; u < 4; ++u) s[4 * r4 + u] = v[u];
-        }
+        for (int u = 0; u < 4; ++u) { s[4 * r4 + u] = l4[u]; dp[4 * r4 + u] = d4[u]; }
       }
 #pragma unroll
       for (int c = 0; c < KC; ++c) {
         s = mfma32(fo.row_frag(Qs[buf], t, c), kf[c], s);
         dp = mfma32(fo.row_frag(Ds[buf], t, c), vf[c], dp);
       }
-      if (p.causal && k0 + 31 > pos) {
+      // a lane whose key is past the sample's length computes garbage that stays in its own accumulator columns, which are not stored
+      if (below || above) {
+        const float far = below ? far_lo : far_hi;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = ki <= pos + 32 * t + acc_row(r, g) ? s[r] : -INFINITY;
+        for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], p.scale_log2, far));
+      } else {
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4) {
+          const f32x4 v = rel_read4(rel_lds + (tab + qt * 64) + 32 * t + 8 * r4);
+#pragma unroll
+          for (int u = 0; u < 4; ++u) s[4 * r4 + u] = __builtin_amdgcn_exp2f(fmaf(s[4 * r4 + u], p.scale_log2, v[u]));
+        }
       }
 #pragma unroll
-      for (int r4 = 0; r4 < 4; ++r4) {
-        const f32x4 l4 = *reinterpret_cast<const f32x4*>(&lse_s[buf][32 * t + 8 * r4 + 4 * g]);
+      for (int r = 0; r < 16; ++r) dp[r] *= s[r];
+      if (p.causal && k0 + 31 > pos + 32 * t) {      // (here and not before the exponential: what is masked counts for nothing whatever it is)
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const int r = 4 * r4 + u;
-          // a lane whose key is past the sample's length computes garbage that stays in its own accumulator columns, which are not stored
-          s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], p.scale_log2, -l4[u]));
-          dp[r] *= s[r];
+        for (int r = 0; r < 16; ++r) {
+          const bool seen = ki <= pos + 32 * t + acc_row(r, g);
+          s[r] = seen ? s[r] : 0.f;
+          dp[r] = seen ? dp[r] : 0.f;
         }
       }
 #pragma unroll
@@ -868,138 +882,325 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
     }
 }
 
-// ------------------------------------------------------------------ fp32: a wave a row
-constexpr int REL_F32_MAX_D = 96;
-__device__ __forceinline__ float rel_bias_f32(const RelAttnK& p, const RelStarts& st, int h, int dist) {
-  return ((const float*)p.table)[(size_t)rel_bucket(p.bk, st, max(p.bk.lo, min(p.bk.hi, dist))) * p.H + h];
-}
+// ------------------------------------------------------------------ fp32
+// v_mfma_f32_32x32x2_f32: A row l % 32, k = l / 32; B column l % 32, k = l / 32; D as in bf16.  Any order of the contraction does as long as both operands
+// follow it: over the head's columns step 4 c + u is column 8 c + 4 g + u (a lane's operands are 16 bytes of a row), over keys or queries step r is row acc_row(r, g),
+// which makes register r of the scores the B operand as it stands and the A operand a row of which 32 lanes read neighbouring columns.  So nothing goes
+// through LDS on its way in: an instruction takes 64 cycles, several loads' time.
+// A workgroup has 32 queries (forward, dQ) or 32 keys (dK / dV) of a head; its four waves take every fourth tile of 32 of the other side and
+// add what they have in LDS at the end, in their order.  Bound by the matrix instruction where there is work for all CUs, else by the chain of tiles.
+__device__ __forceinline__ f32x16 mfma_f32(float a, float b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0); }
 
-__global__ void __launch_bounds__(64) rel_fwd_f32_kernel(const RelAttnK p, const RelStarts st) {
-  extern __shared__ float sc[];        // [Nk]
-  __shared__ float qs[REL_F32_MAX_D];
-  const int lane = threadIdx.x, i = blockIdx.x % p.Nq, bh = blockIdx.x / p.Nq, b = bh / p.H, h = bh % p.H, pos = p.query0 + i;
-  const int keys = rel_keys(p, b), lim = p.causal ? min(keys, pos + 1) : keys;
-  const float* q = (const float*)p.q + ((size_t)b * p.Nq + i) * p.ldq + h * p.dh;
-  const float* kb = (const float*)p.k + (size_t)b * p.Nk * p.ldk + h * p.dh;
-  const float* vb = (const float*)p.v + (size_t)b * p.Nk * p.ldv + h * p.dh;
-  for (int t = lane; t < p.dh; t += 64) qs[t] = q[t];
-  __syncthreads();
-  float mx = -INFINITY;
-  for (int j = lane; j < lim; j += 64) {
-    float s = 0.f;
-#pragma unroll 16
-    for (int t = 0; t < p.dh; ++t) s = fmaf(qs[t], kb[(size_t)j * p.ldk + t], s);
-    s = fmaf(s, p.scale, rel_bias_f32(p, st, h, j - pos));
-    sc[j] = s;
-    mx = fmaxf(mx, s);
+template <int KC> struct RelRows {      // a lane's 16-byte pieces of one row
+  f32x4 v[KC];
+  __device__ __forceinline__ void load(const float* base, int row, int ld, int dh, int g) {
+    const float* r = base + (size_t)row * ld + 4 * g;
+#pragma unroll
+    for (int c = 0; c < KC; ++c) v[c] = 8 * c + 4 * g < dh ? *reinterpret_cast<const f32x4*>(r + 8 * c) : f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  mx = wave_max(mx);
-  const float ref = mx == -INFINITY ? 0.f : mx;
-  float sum = 0.f;
-  for (int j = lane; j < lim; j += 64) {
-    const float e = expf(sc[j] - ref);
-    sc[j] = e;
-    sum += e;
-  }
-  sum = wave_sum(sum);
-  __syncthreads();
-  float* o = (float*)p.o + ((size_t)b * p.Nq + i) * p.ldo + h * p.dh;
-  for (int t = lane; t < p.dh; t += 64) {
-    float a = 0.f;
-#pragma unroll 16
-    for (int j = 0; j < lim; ++j) a = fmaf(sc[j], vb[(size_t)j * p.ldv + t], a);
-    o[t] = sum == 0.f ? 0.f : a / sum;
-  }
-  if (p.lse && lane == 0) p.lse[((size_t)b * p.H + h) * p.Nq + i] = sum == 0.f ? -INFINITY : mx + logf(sum);
+};
+// D += rows of a (A) times rows of b (B), over the head's columns
+template <int KC> __device__ __forceinline__ f32x16 rel_rows_product(const RelRows<KC>& a, const RelRows<KC>& b, f32x16 acc) {
+#pragma unroll
+  for (int c = 0; c < KC; ++c)
+#pragma unroll
+    for (int u = 0; u < 4; ++u) acc = mfma_f32(a.v[c][u], b.v[c][u], acc);
+  return acc;
 }
-
-__global__ void __launch_bounds__(64) rel_bwd_dq_f32_kernel(const RelAttnK p, const RelStarts st) {
-  extern __shared__ float sc[];        // [Nk]
-  __shared__ float qs[REL_F32_MAX_D], dos[REL_F32_MAX_D];
-  const int lane = threadIdx.x, i = blockIdx.x % p.Nq, bh = blockIdx.x / p.Nq, b = bh / p.H, h = bh % p.H, pos = p.query0 + i;
-  const int keys = rel_keys(p, b), lim = max(0, p.causal ? min(keys, pos + 1) : keys);
-  const float* q = (const float*)p.q + ((size_t)b * p.Nq + i) * p.ldq + h * p.dh;
-  const float* dor = (const float*)p.dout + ((size_t)b * p.Nq + i) * p.lddo + h * p.dh;
-  const float* orow = (const float*)p.o + ((size_t)b * p.Nq + i) * p.ldo + h * p.dh;
-  const float* kb = (const float*)p.k + (size_t)b * p.Nk * p.ldk + h * p.dh;
-  const float* vb = (const float*)p.v + (size_t)b * p.Nk * p.ldv + h * p.dh;
-  const size_t sidx = ((size_t)b * p.H + h) * p.Nq + i;
-  const float l = p.lse[sidx], lse = l == -INFINITY ? INFINITY : l;
-  float dlt = 0.f;
-  for (int t = lane; t < p.dh; t += 64) { qs[t] = q[t]; dos[t] = dor[t]; dlt = fmaf(dor[t], orow[t], dlt); }
-  dlt = wave_sum(dlt);
-  if (lane == 0) p.delta[sidx] = dlt;
-  __syncthreads();
-  for (int j = lane; j < lim; j += 64) {
-    float s = 0.f, dp = 0.f;
-#pragma unroll 16
-    for (int t = 0; t < p.dh; ++t) {
-      s = fmaf(qs[t], kb[(size_t)j * p.ldk + t], s);
-      dp = fmaf(dos[t], vb[(size_t)j * p.ldv + t], dp);
+template <int DT> struct RelColumns {      // columns 32 i + l32 of the rows acc_row(r, g) of a tile
+  float v[DT][16];
+  __device__ __forceinline__ void load(const float* base, int row0, int last_row, int ld, int dh, int g, int l32) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const float* row = base + (size_t)min(row0 + acc_row(r, g), last_row) * ld;
+#pragma unroll
+      for (int i = 0; i < DT; ++i) v[i][r] = row[min(32 * i + l32, dh - 1)];      // (rows of the result past the head are not stored)
     }
-    sc[j] = expf(fmaf(s, p.scale, rel_bias_f32(p, st, h, j - pos)) - lse) * (dp - dlt);
   }
+};
+template <int DT> __device__ __forceinline__ void rel_columns_product(const RelColumns<DT>& a, const f32x16& b, f32x16 (&acc)[DT]) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r)
+#pragma unroll
+    for (int i = 0; i < DT; ++i) acc[i] = mfma_f32(a.v[i][r], b[r], acc[i]);
+}
+// A wave's result [32 rows][columns] in LDS, and four columns of the sum over the waves, each times its weight
+template <int DT> constexpr int REL_F32_LD = 32 * DT + 4;
+template <int DT> constexpr int REL_F32_MEET = 4 * 32 * REL_F32_LD<DT>;      // floats
+template <int DT> __device__ __forceinline__ void rel_leave(float* meet, const f32x16 (&acc)[DT], int wave, int g, int l32) {
+#pragma unroll
+  for (int i = 0; i < DT; ++i)
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4)
+      *reinterpret_cast<f32x4*>(meet + (32 * wave + l32) * REL_F32_LD<DT> + 32 * i + 8 * r4 + 4 * g) = f32x4{acc[i][4 * r4], acc[i][4 * r4 + 1], acc[i][4 * r4 + 2], acc[i][4 * r4 + 3]};
+}
+template <int DT> __device__ __forceinline__ f32x4 rel_meet(const float* meet, int row, int col, const float (&weight)[4]) {
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const f32x4 v = *reinterpret_cast<const f32x4*>(meet + (32 * w + row) * REL_F32_LD<DT> + col);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) o[u] = fmaf(weight[w], v[u], o[u]);
+  }
+  return o;
+}
+// Scores of a tile begin with the bias over the scale
+__device__ __forceinline__ f32x16 rel_bias16(const float* lds, int entry) {
+  f32x16 s;
+#pragma unroll
+  for (int r4 = 0; r4 < 4; ++r4) {
+    const f32x4 v = rel_read4(lds + entry + 8 * r4);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) s[4 * r4 + u] = v[u];
+  }
+  return s;
+}
+__device__ __forceinline__ f32x16 rel_all16(float v) {
+  f32x16 s;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) s[r] = v;
+  return s;
+}
+
+template <int DT, int KC>
+__global__ void __launch_bounds__(256) rel_fwd_f32_kernel(const RelAttnK p, const RelStarts st) {
+  __shared__ __attribute__((aligned(16))) float meet[REL_F32_MEET<DT>];
+  __shared__ float stat[4][2][32];
+  extern __shared__ __attribute__((aligned(16))) float rel_lds[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, l32 = lane & 31;
+  const int bk_lo = p.bk.lo, bk_hi = p.bk.hi;
+  int qtile, bh;
+  rel_block_map(p, blockIdx.x, (p.Nq + 31) / 32, true, qtile, bh);
+  const int b = bh / p.H, h = bh % p.H, qi = qtile * 32 + l32, pos0 = p.query0 + qtile * 32, pos = pos0 + l32;
+  const int keys = __builtin_amdgcn_readfirstlane(rel_keys(p, b));
+  const int lim = p.causal ? min(keys, pos + 1) : keys, lim_all = p.causal ? min(keys, pos0 + 1) : keys;
+  const int lim_any = p.causal ? min(keys, p.query0 + min(p.Nq, qtile * 32 + 32)) : keys, nkt = lim_any > 0 ? (lim_any + 31) / 32 : 0;
+  const float* kb = (const float*)p.k + (size_t)b * p.Nk * p.ldk + h * p.dh;
+  const float* vb = (const float*)p.v + (size_t)b * p.Nk * p.ldv + h * p.dh;
+  RelRows<KC> q, k;
+  q.load((const float*)p.q + (size_t)b * p.Nq * p.ldq + h * p.dh, min(qi, p.Nq - 1), p.ldq, p.dh, g);
+  if (wave < nkt) k.load(kb, min(32 * wave + l32, keys - 1), p.ldk, p.dh, g);
+  rel_fill<float, false>(p, st, h, rel_lds, 256, p.inv_scale);
+  const int tab = 4 * g - pos - (bk_lo - REL_MARGIN);      // entry of this lane's first key
+  f32x16 oacc[DT];
+#pragma unroll
+  for (int i = 0; i < DT; ++i) oacc[i] = rel_all16(0.f);
+  float m = -INFINITY, lsum = 0.f;
   __syncthreads();
-  float* dq = (float*)p.dq + ((size_t)b * p.Nq + i) * p.lddq + h * p.dh;
-  for (int t = lane; t < p.dh; t += 64) {
-    float a = 0.f;
-#pragma unroll 16
-    for (int j = 0; j < lim; ++j) a = fmaf(sc[j], kb[(size_t)j * p.ldk + t], a);
-    dq[t] = a * p.scale;
+  const float far_lo = rel_uniform(rel_lds[0]), far_hi = rel_uniform(rel_lds[rel_entries(p.bk) - 1]);
+  for (int kt = wave; kt < nkt; kt += 4) {
+    const int k0 = 32 * kt;
+    RelColumns<DT> v;
+    v.load(vb, k0, keys - 1, p.ldv, p.dh, g, l32);
+    const bool below = k0 + 31 - pos0 <= bk_lo, above = k0 - pos0 - 31 >= bk_hi;
+    f32x16 s = below ? rel_all16(far_lo) : (above ? rel_all16(far_hi) : rel_bias16(rel_lds, tab + k0));
+    s = rel_rows_product(k, q, s);
+    if (kt + 4 < nkt) k.load(kb, min(k0 + 128 + l32, keys - 1), p.ldk, p.dh, g);
+    if (k0 + 32 > lim_all) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = k0 + acc_row(r, g) < lim ? s[r] : -INFINITY;
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[r]);
+    mx = fmaxf(m, reduce_halves(mx, MaxOp()) * p.scale_log2);
+    const float ref = mx == -INFINITY ? 0.f : mx, alpha = __builtin_amdgcn_exp2f(m - ref);
+    m = mx;
+    lsum *= alpha;
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) oacc[i][r] *= alpha;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], p.scale_log2, -ref));
+      lsum += s[r];
+    }
+    rel_columns_product(v, s, oacc);
   }
-  if (!p.dtable_partial) return;
-  float* out = p.dtable_partial + (((size_t)h * p.B + b) * p.Nq + i) * p.bk.n_buckets;
-  for (int bucket = lane; bucket < p.bk.n_buckets; bucket += 64) {      // a lane adds its bucket's keys
-    const int side = p.bk.bidirectional && bucket >= p.bk.per_side, k = bucket - side * p.bk.per_side;
-    const int n0 = rel_start(p.bk, st, k), n1 = rel_start(p.bk, st, k + 1) - 1;
-    int j0 = side ? pos + max(n0, 1) : pos - n1, j1 = min(lim - 1, side ? pos + n1 : pos - n0);
-    if (!p.bk.bidirectional && k == 0) j1 = lim - 1;
-    float v = 0.f;
-    for (int j = max(0, j0); j <= j1; ++j) v += sc[j];
-    out[bucket] = v;
+  lsum = reduce_halves(lsum, AddOp());
+  if (g == 0) { stat[wave][0][l32] = m; stat[wave][1][l32] = lsum; }
+  rel_leave(meet, oacc, wave, g, l32);
+  __syncthreads();
+  for (int at = tid; at < 32 * 8 * DT; at += 256) {
+    const int row = at / (8 * DT), col = at % (8 * DT) * 4, i = qtile * 32 + row;
+    if (i >= p.Nq || col >= p.dh) continue;
+    const float top = fmaxf(fmaxf(stat[0][0][row], stat[1][0][row]), fmaxf(stat[2][0][row], stat[3][0][row])), ref = top == -INFINITY ? 0.f : top;
+    float a[4], sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      a[w] = __builtin_amdgcn_exp2f(stat[w][0][row] - ref);
+      sum = fmaf(a[w], stat[w][1][row], sum);
+    }
+    const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+    f32x4 o = rel_meet<DT>(meet, row, col, a);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) o[u] *= inv;
+    *reinterpret_cast<f32x4*>((float*)p.o + ((size_t)b * p.Nq + i) * p.ldo + h * p.dh + col) = o;
+    if (p.lse && col == 0) p.lse[((size_t)b * p.H + h) * p.Nq + i] = sum == 0.f ? -INFINITY : fmaf(top, LN2, logf(sum));
   }
 }
 
-__global__ void __launch_bounds__(64) rel_bwd_dkv_f32_kernel(const RelAttnK p, const RelStarts st) {
-  extern __shared__ float sc[];        // [2][Nq]: P and dS
-  __shared__ float ks[REL_F32_MAX_D], vs[REL_F32_MAX_D];
-  const int lane = threadIdx.x, j = blockIdx.x % p.Nk, bh = blockIdx.x / p.Nk, b = bh / p.H, h = bh % p.H;
-  float* dk = (float*)p.dk + ((size_t)b * p.Nk + j) * p.lddk + h * p.dh;
-  float* dv = (float*)p.dv + ((size_t)b * p.Nk + j) * p.lddv + h * p.dh;
-  if (j >= rel_keys(p, b)) {
-    for (int t = lane; t < p.dh; t += 64) { dk[t] = 0.f; dv[t] = 0.f; }
-    return;
+template <int DT, int KC>
+__global__ void __launch_bounds__(256) rel_bwd_dq_f32_kernel(const RelAttnK p, const RelStarts st) {
+  __shared__ __attribute__((aligned(16))) float meet[REL_F32_MEET<DT>];
+  __shared__ float far_sums[2][4];
+  extern __shared__ __attribute__((aligned(16))) float rel_lds[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, l32 = lane & 31;
+  const int bk_lo = p.bk.lo, bk_hi = p.bk.hi, qtiles = (p.Nq + 31) / 32, entries = rel_entries(p.bk);
+  int qtile, bh;
+  rel_block_map(p, blockIdx.x, qtiles, true, qtile, bh);
+  const int b = bh / p.H, h = bh % p.H, qi = qtile * 32 + l32, pos0 = p.query0 + qtile * 32, pos = pos0 + l32;
+  const bool qok = qi < p.Nq;
+  const int keys = __builtin_amdgcn_readfirstlane(rel_keys(p, b));
+  const int lim = p.causal ? min(keys, pos + 1) : keys, lim_all = p.causal ? min(keys, pos0 + 1) : keys;
+  const int lim_any = p.causal ? min(keys, p.query0 + min(p.Nq, qtile * 32 + 32)) : keys, nkt = lim_any > 0 ? (lim_any + 31) / 32 : 0;
+  const float* kb = (const float*)p.k + (size_t)b * p.Nk * p.ldk + h * p.dh;
+  const float* vb = (const float*)p.v + (size_t)b * p.Nk * p.ldv + h * p.dh;
+  const int qrow = min(qi, p.Nq - 1);
+  RelRows<KC> q, dout, k;
+  q.load((const float*)p.q + (size_t)b * p.Nq * p.ldq + h * p.dh, qrow, p.ldq, p.dh, g);
+  dout.load((const float*)p.dout + (size_t)b * p.Nq * p.lddo + h * p.dh, qrow, p.lddo, p.dh, g);
+  k.load((const float*)p.o + (size_t)b * p.Nq * p.ldo + h * p.dh, qrow, p.ldo, p.dh, g);
+  const size_t sidx = ((size_t)b * p.H + h) * p.Nq + qrow;
+  const float l = p.lse[sidx], lse2 = qok && l != -INFINITY ? l * LOG2E : INFINITY;      // (of no query, and of one that sees no key: its probabilities are zero)
+  float dlt = 0.f;
+#pragma unroll
+  for (int c = 0; c < KC; ++c)
+#pragma unroll
+    for (int u = 0; u < 4; ++u) dlt = fmaf(k.v[c][u], dout.v[c][u], dlt);
+  dlt = reduce_halves(dlt, AddOp());
+  if (qok && tid < 32) p.delta[sidx] = dlt;
+  rel_fill<float, false>(p, st, h, rel_lds, 256, p.inv_scale);
+  float* sums = rel_lds + rel_table_floats(p.bk);
+  const int sum_stride = rel_sum_stride(p.bk);
+  float* stage = sums + 4 * sum_stride + 32 + wave * REL_STAGE;
+  for (int e = tid; e < 4 * sum_stride; e += 256) sums[e] = 0.f;
+  const int tab = 4 * g - pos - (bk_lo - REL_MARGIN), mine = wave * sum_stride + lane - (REL_SQ - 1) - pos0 - (bk_lo - REL_MARGIN);
+  f32x16 acc[DT];
+#pragma unroll
+  for (int i = 0; i < DT; ++i) acc[i] = rel_all16(0.f);
+  float far_sum_lo = 0.f, far_sum_hi = 0.f;
+  __syncthreads();
+  const float far_lo = rel_uniform(rel_lds[0]), far_hi = rel_uniform(rel_lds[entries - 1]);
+  for (int kt = wave; kt < nkt; kt += 4) {
+    const int k0 = 32 * kt, row = min(k0 + l32, keys - 1);
+    RelRows<KC> v;
+    RelColumns<DT> kc;
+    k.load(kb, row, p.ldk, p.dh, g);
+    v.load(vb, row, p.ldv, p.dh, g);
+    kc.load(kb, k0, keys - 1, p.ldk, p.dh, g, l32);
+    const bool below = k0 + 31 - pos0 <= bk_lo, above = k0 - pos0 - 31 >= bk_hi;
+    f32x16 s = below ? rel_all16(far_lo) : (above ? rel_all16(far_hi) : rel_bias16(rel_lds, tab + k0));
+    s = rel_rows_product(k, q, s);
+    const f32x16 dp = rel_rows_product(v, dout, rel_all16(-dlt));
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], p.scale_log2, -lse2)) * dp[r];
+    if (k0 + 32 > lim_all) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = k0 + acc_row(r, g) < lim ? s[r] : 0.f;
+    }
+    if (below || above) {
+      float sum = 0.f;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sum += s[r];
+      if (below) far_sum_lo += sum;
+      else far_sum_hi += sum;
+    } else {
+      rel_add_diagonals(s, stage, sums + (mine + k0), g, l32, lane);
+    }
+    rel_columns_product(kc, s, acc);
   }
-  const float* kr = (const float*)p.k + ((size_t)b * p.Nk + j) * p.ldk + h * p.dh;
-  const float* vr = (const float*)p.v + ((size_t)b * p.Nk + j) * p.ldv + h * p.dh;
+  rel_leave(meet, acc, wave, g, l32);
+  __syncthreads();
+  for (int at = tid; at < 32 * 8 * DT; at += 256) {
+    const int row = at / (8 * DT), col = at % (8 * DT) * 4, i = qtile * 32 + row;
+    if (i >= p.Nq || col >= p.dh) continue;
+    const float each[4] = {p.scale, p.scale, p.scale, p.scale};
+    *reinterpret_cast<f32x4*>((float*)p.dq + ((size_t)b * p.Nq + i) * p.lddq + h * p.dh + col) = rel_meet<DT>(meet, row, col, each);
+  }
+  if (p.dtable_partial) rel_bucket_sums(p, st, sums, sum_stride, far_sums, far_sum_lo, far_sum_hi, p.dtable_partial + ((size_t)h * p.B * qtiles + (size_t)b * qtiles + qtile) * p.bk.n_buckets);
+}
+
+template <int DT, int KC>
+__global__ void __launch_bounds__(256) rel_bwd_dkv_f32_kernel(const RelAttnK p, const RelStarts st) {
+  __shared__ __attribute__((aligned(16))) float meet[REL_F32_MEET<DT>];
+  extern __shared__ __attribute__((aligned(16))) float rel_lds[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, l32 = lane & 31;
+  const int bk_lo = p.bk.lo, bk_hi = p.bk.hi;
+  int ktile, bh;
+  rel_block_map(p, blockIdx.x, (p.Nk + 31) / 32, false, ktile, bh);
+  const int b = bh / p.H, h = bh % p.H, k0 = ktile * 32, ki = k0 + l32;
+  const int keys = __builtin_amdgcn_readfirstlane(rel_keys(p, b));
+  const int nqt = k0 < keys ? (p.Nq + 31) / 32 : 0, first = p.causal ? max(0, k0 - p.query0) / 32 : 0;
   const float* qb = (const float*)p.q + (size_t)b * p.Nq * p.ldq + h * p.dh;
   const float* dob = (const float*)p.dout + (size_t)b * p.Nq * p.lddo + h * p.dh;
   const float* lse_b = p.lse + ((size_t)b * p.H + h) * p.Nq;
   const float* dlt_b = p.delta + ((size_t)b * p.H + h) * p.Nq;
-  for (int t = lane; t < p.dh; t += 64) { ks[t] = kr[t]; vs[t] = vr[t]; }
+  f32x16 dkacc[DT], dvacc[DT];
+#pragma unroll
+  for (int i = 0; i < DT; ++i) dkacc[i] = dvacc[i] = rel_all16(0.f);
+  rel_fill<float, true>(p, st, h, rel_lds, 256, p.inv_scale);
+  const int tab = 4 * g + p.query0 - ki + bk_hi + REL_MARGIN;      // entry of this lane's first query
   __syncthreads();
-  const int i0 = p.causal ? max(0, j - p.query0) : 0;
-  float* pp = sc; float* dsp = sc + p.Nq;
-  for (int i = i0 + lane; i < p.Nq; i += 64) {
-    float s = 0.f, dp = 0.f;
-    for (int t = 0; t < p.dh; ++t) {
-      s = fmaf(qb[(size_t)i * p.ldq + t], ks[t], s);
-      dp = fmaf(dob[(size_t)i * p.lddo + t], vs[t], dp);
+  const float far_hi = rel_uniform(rel_lds[0]), far_lo = rel_uniform(rel_lds[rel_entries(p.bk) - 1]);
+  if (first + wave < nqt) {
+    RelRows<KC> k, v;      // (a lane whose key is past the sample's length computes what is not stored)
+    k.load((const float*)p.k + (size_t)b * p.Nk * p.ldk + h * p.dh, min(ki, keys - 1), p.ldk, p.dh, g);
+    v.load((const float*)p.v + (size_t)b * p.Nk * p.ldv + h * p.dh, min(ki, keys - 1), p.ldv, p.dh, g);
+    for (int qt = first + wave; qt < nqt; qt += 4) {
+      const int q0 = 32 * qt, row = min(q0 + l32, p.Nq - 1), pos0 = p.query0 + q0;
+      RelRows<KC> q, dout;
+      RelColumns<DT> qc, dc;
+      q.load(qb, row, p.ldq, p.dh, g);
+      dout.load(dob, row, p.lddo, p.dh, g);
+      qc.load(qb, q0, p.Nq - 1, p.ldq, p.dh, g, l32);
+      dc.load(dob, q0, p.Nq - 1, p.lddo, p.dh, g, l32);
+      float lse2[16];
+      f32x16 dp;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int i = q0 + acc_row(r, g), at = min(i, p.Nq - 1);
+        const float l = lse_b[at];
+        lse2[r] = i < p.Nq && l != -INFINITY ? l * LOG2E : INFINITY;
+        dp[r] = -dlt_b[at];
+      }
+      const bool below = k0 + 31 - pos0 <= bk_lo, above = k0 - pos0 - 31 >= bk_hi;
+      f32x16 s = below ? rel_all16(far_lo) : (above ? rel_all16(far_hi) : rel_bias16(rel_lds, tab + q0));
+      s = rel_rows_product(q, k, s);
+      dp = rel_rows_product(dout, v, dp);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], p.scale_log2, -lse2[r]));
+        dp[r] *= s[r];
+      }
+      if (p.causal && k0 + 31 > pos0) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const bool seen = ki <= pos0 + acc_row(r, g);
+          s[r] = seen ? s[r] : 0.f;
+          dp[r] = seen ? dp[r] : 0.f;
+        }
+      }
+      rel_columns_product(dc, s, dvacc);
+      rel_columns_product(qc, dp, dkacc);
     }
-    const float l = lse_b[i];
-    const float pr = expf(fmaf(s, p.scale, rel_bias_f32(p, st, h, j - p.query0 - i)) - (l == -INFINITY ? INFINITY : l));
-    pp[i] = pr;
-    dsp[i] = pr * (dp - dlt_b[i]);
   }
-  __syncthreads();
-  for (int t = lane; t < p.dh; t += 64) {
-    float a = 0.f, c = 0.f;
-    for (int i = i0; i < p.Nq; ++i) {
-      a = fmaf(dsp[i], qb[(size_t)i * p.ldq + t], a);
-      c = fmaf(pp[i], dob[(size_t)i * p.lddo + t], c);
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    const float f = which ? 1.0f : p.scale, each[4] = {f, f, f, f};
+    float* out = which ? (float*)p.dv : (float*)p.dk;
+    const int ld = which ? p.lddv : p.lddk;
+    if (which) __syncthreads();
+    rel_leave(meet, which ? dvacc : dkacc, wave, g, l32);
+    __syncthreads();
+    for (int at = tid; at < 32 * 8 * DT; at += 256) {
+      const int row = at / (8 * DT), col = at % (8 * DT) * 4, j = k0 + row;
+      if (j >= p.Nk || col >= p.dh) continue;
+      f32x4 o = rel_meet<DT>(meet, row, col, each);
+      if (j >= keys) o = f32x4{0.f, 0.f, 0.f, 0.f};
+      *reinterpret_cast<f32x4*>(out + ((size_t)b * p.Nk + j) * ld + h * p.dh + col) = o;
     }
-    dk[t] = a * p.scale;
-    dv[t] = c;
   }
 }
 
@@ -1056,8 +1257,8 @@ static int rel_buckets(const char* who, int n_buckets, int max_distance, int bid
 
 static size_t rel_align(size_t n) { return align_up(n, 256); }
 struct RelWorkspace { size_t delta, partial, bytes; };
-// dQ workgroups (bf16) or rows (fp32) of a head, each with its sums over buckets
-static size_t rel_parts(int B, int Nq, bool f32) { return (size_t)B * (f32 ? Nq : (Nq + 127) / 128); }
+// dQ workgroups of a head, each with its sums over buckets
+static size_t rel_parts(int B, int Nq, bool f32) { return (size_t)B * (f32 ? (Nq + 31) / 32 : (Nq + 127) / 128); }
 static RelWorkspace rel_workspace(int B, int H, int Nq, int n_buckets) {
   RelWorkspace w;
   w.delta = 0;
@@ -1067,8 +1268,8 @@ static RelWorkspace rel_workspace(int B, int H, int Nq, int n_buckets) {
 }
 
 // Dynamic LDS beyond 64 KB in all has to be asked for, once per kernel and device; asking again does no harm.
-template <class K> static int rel_allow_lds(K kern, int dhp, int bytes) {
-  if (512 * dhp + 2048 + bytes <= 64 * 1024) return DP_OK;      // (two stages of two tiles, and a few rows of statistics)
+template <class K> static int rel_allow_lds(K kern, int tiles, int bytes) {      // tiles: bytes of the kernel's own
+  if (tiles + 2048 + bytes <= 64 * 1024) return DP_OK;
   if (hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return set_error(DP_EHIP, "hipFuncSetAttribute(attention) failed");
   return DP_OK;
 }
@@ -1078,6 +1279,15 @@ template <class F> static int rel_dispatch(int d_head, F f) {
   if (d_head <= 64) return f(integral_constant<int, 64>(), integral_constant<int, 4>());
   if (d_head <= 80) return f(integral_constant<int, 96>(), integral_constant<int, 5>());
   return f(integral_constant<int, 96>(), integral_constant<int, 6>());
+}
+// Blocks of 32 columns and steps of 8 over the head
+template <class F> static int rel_dispatch_f32(int d_head, F f) {
+  using std::integral_constant;
+  if (d_head <= 16) return f(integral_constant<int, 1>(), integral_constant<int, 2>());
+  if (d_head <= 32) return f(integral_constant<int, 1>(), integral_constant<int, 4>());
+  if (d_head <= 40) return f(integral_constant<int, 2>(), integral_constant<int, 5>());
+  if (d_head <= 64) return f(integral_constant<int, 2>(), integral_constant<int, 8>());
+  return f(integral_constant<int, 3>(), integral_constant<int, 12>());
 }
 static int rel_takes_turns(long blocks, int per_cu) { return blocks > 256 && blocks <= 256L * per_cu; }
 static int rel_launched() {
@@ -1111,7 +1321,7 @@ static int check_rel(const char* who, int dtype, const RelAttnK& k, const dp_rel
   const int grid = dtype == DP_BF16 ? 8 : 4, es = dtype == DP_BF16 ? 2 : 4;
   if (k.dh % grid || k.dh > 96) return set_errorf(DP_EUNSUPPORTED, "%s: d_head must be a multiple of %d, at most 96", who, grid);
   if (k.query0 > (1 << 29) || k.query0 < -(1 << 29) || k.Nq > (1 << 29) || k.Nk > (1 << 29)) return set_errorf(DP_EUNSUPPORTED, "%s: positions beyond 2^29", who);
-  const size_t tiles = (size_t)(std::max(k.Nq, k.Nk) + 127) / 128 * k.B * k.H;
+  const size_t rows = dtype == DP_BF16 ? 128 : 32, tiles = ((size_t)std::max(k.Nq, k.Nk) + rows - 1) / rows * k.B * k.H;
   if (tiles >= (1u << 24)) return set_errorf(DP_EUNSUPPORTED, "%s: too many tiles for one launch", who);      // (2^32 threads)
   const int span = k.H * k.dh;
   struct Op { const void* p; int ld, n; const char* name; };
@@ -1129,10 +1339,6 @@ static int check_rel(const char* who, int dtype, const RelAttnK& k, const dp_rel
   if (k.key_len && (uintptr_t)k.key_len % 4) return set_errorf(DP_EALIGN, "%s: key_len must be 4-byte aligned", who);
   if (bwd && !k.lse) return set_errorf(DP_EINVAL, "%s: lse is NULL", who);
   if (k.lse && (uintptr_t)k.lse % 16) return set_errorf(DP_EALIGN, "%s: lse is not 16-byte aligned", who);
-  if (dtype == DP_F32) {
-    if ((size_t)k.B * k.H * std::max(k.Nq, k.Nk) >= (1u << 26)) return set_errorf(DP_EUNSUPPORTED, "%s: too many rows for one launch", who);
-    if ((size_t)k.Nk * 4 > 60000 || (bwd && (size_t)k.Nq * 8 > 60000)) return set_errorf(DP_EUNSUPPORTED, "%s: sequence too long for fp32", who);
-  }
   return DP_OK;
 }
 
@@ -1173,8 +1379,12 @@ int dp_op_attention_relbias_fwd(int dtype, int B, int H, int Nq, int Nk, int d_h
   hipStream_t s = (hipStream_t)hip_stream;
   KScope ks(dtype == DP_BF16 ? KK_ATTN_FWD : KK_ATTN_F32, 4.0 * B * H * (double)Nq * Nk * d_head, (dtype == DP_BF16 ? 2.0 : 4.0) * B * H * d_head * (2.0 * Nq + 2.0 * Nk), s, Nq, Nk, d_head);
   if (dtype == DP_F32) {
-    hipLaunchKernelGGL(rel_fwd_f32_kernel, dim3((unsigned)(B * H) * Nq), dim3(64), (size_t)Nk * sizeof(float), s, a, st);
-    return rel_launched();
+    const int table = rel_table_floats(a.bk) * 4;
+    return rel_dispatch_f32(d_head, [&](auto dt, auto kc) {
+      DP_TRY(rel_allow_lds(rel_fwd_f32_kernel<dt, kc>, REL_F32_MEET<dt> * 4, table));
+      hipLaunchKernelGGL((rel_fwd_f32_kernel<dt, kc>), dim3((unsigned)((Nq + 31) / 32 * B * H)), dim3(256), table, s, a, st);
+      return rel_launched();
+    });
   }
   const int lds = rel_table_floats(a.bk) * 4;
   if (rel_few(B, H, Nq, Nk, d_head)) {
@@ -1187,7 +1397,7 @@ int dp_op_attention_relbias_fwd(int dtype, int B, int H, int Nq, int Nk, int d_h
       a.part = (float*)workspace;
     }
     DP_TRY(rel_dispatch(d_head, [&](auto dhp, auto kc) {
-      DP_TRY(rel_allow_lds(rel_fwd_few_bf16_kernel<dhp, kc>, 2 * dhp, lds));
+      DP_TRY(rel_allow_lds(rel_fwd_few_bf16_kernel<dhp, kc>, 1024 * dhp, lds));
       hipLaunchKernelGGL((rel_fwd_few_bf16_kernel<dhp, kc>), dim3((unsigned)((Nq + 31) / 32 * B * H * a.shares)), dim3(256), lds, s, a, st);
       return rel_launched();
     }));
@@ -1199,7 +1409,7 @@ int dp_op_attention_relbias_fwd(int dtype, int B, int H, int Nq, int Nk, int d_h
   a.even = rel_takes_turns(blocks, d_head <= 64 ? 4 : 3);
   return rel_dispatch(d_head, [&](auto dhp, auto kc) {
     constexpr int W = dhp == 64 ? 4 : 3;
-    DP_TRY(rel_allow_lds(rel_fwd_bf16_kernel<dhp, kc, W>, dhp, lds));
+    DP_TRY(rel_allow_lds(rel_fwd_bf16_kernel<dhp, kc, W>, 512 * dhp, lds));
     hipLaunchKernelGGL((rel_fwd_bf16_kernel<dhp, kc, W>), dim3((unsigned)blocks), dim3(256), lds, s, a, st);
     return rel_launched();
   });
@@ -1230,10 +1440,15 @@ int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_h
   const double fl = 4.0 * B * H * (double)Nq * Nk * d_head, by = (dtype == DP_BF16 ? 2.0 : 4.0) * B * H * d_head * (3.0 * Nq + 2.0 * Nk);
   if (dtype == DP_F32) {
     KScope ks(KK_ATTN_F32, 2 * fl, 2 * by, s, Nq, Nk, d_head);
-    hipLaunchKernelGGL(rel_bwd_dq_f32_kernel, dim3((unsigned)(B * H) * Nq), dim3(64), (size_t)Nk * sizeof(float), s, a, st);
-    DP_TRY(rel_launched());
-    hipLaunchKernelGGL(rel_bwd_dkv_f32_kernel, dim3((unsigned)(B * H) * Nk), dim3(64), (size_t)2 * Nq * sizeof(float), s, a, st);
-    DP_TRY(rel_launched());
+    const int table = rel_table_floats(a.bk) * 4, both = rel_dq_floats(a.bk) * 4;
+    DP_TRY(rel_dispatch_f32(d_head, [&](auto dt, auto kc) {
+      DP_TRY(rel_allow_lds(rel_bwd_dq_f32_kernel<dt, kc>, REL_F32_MEET<dt> * 4, both));
+      hipLaunchKernelGGL((rel_bwd_dq_f32_kernel<dt, kc>), dim3((unsigned)((Nq + 31) / 32 * B * H)), dim3(256), both, s, a, st);
+      DP_TRY(rel_launched());
+      DP_TRY(rel_allow_lds(rel_bwd_dkv_f32_kernel<dt, kc>, REL_F32_MEET<dt> * 4, table));
+      hipLaunchKernelGGL((rel_bwd_dkv_f32_kernel<dt, kc>), dim3((unsigned)((Nk + 31) / 32 * B * H)), dim3(256), table, s, a, st);
+      return rel_launched();
+    }));
   } else {
     const long qblocks = (long)((Nq + 127) / 128) * B * H, kblocks = (long)((Nk + 127) / 128) * B * H;
     const int table = rel_table_floats(a.bk) * 4, both = rel_dq_floats(a.bk) * 4;
@@ -1241,7 +1456,7 @@ int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_h
       KScope ks(KK_ATTN_BWD_DQ, fl, by, s, Nq, Nk, d_head);
       a.even = rel_takes_turns(qblocks, d_head <= 64 ? 3 : 2);
       DP_TRY(rel_dispatch(d_head, [&](auto dhp, auto kc) {
-        DP_TRY(rel_allow_lds(rel_bwd_dq_bf16_kernel<dhp, kc>, dhp, both));
+        DP_TRY(rel_allow_lds(rel_bwd_dq_bf16_kernel<dhp, kc>, 512 * dhp, both));
         hipLaunchKernelGGL((rel_bwd_dq_bf16_kernel<dhp, kc>), dim3((unsigned)qblocks), dim3(256), both, s, a, st);
         return rel_launched();
       }));
@@ -1249,7 +1464,7 @@ int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_h
     KScope ks(KK_ATTN_BWD_DKV, fl, by, s, Nq, Nk, d_head);
     a.even = rel_takes_turns(kblocks, 2);
     DP_TRY(rel_dispatch(d_head, [&](auto dhp, auto kc) {
-      DP_TRY(rel_allow_lds(rel_bwd_dkv_bf16_kernel<dhp, kc>, dhp, table));
+      DP_TRY(rel_allow_lds(rel_bwd_dkv_bf16_kernel<dhp, kc>, 512 * dhp, table));
       hipLaunchKernelGGL((rel_bwd_dkv_bf16_kernel<dhp, kc>), dim3((unsigned)kblocks), dim3(256), table, s, a, st);
       return rel_launched();
     }));

@@ -45,13 +45,16 @@ def _close(got, want, bound, what):
     assert (err <= bound).all(), (what, float((err / np.maximum(bound, 1e-300)).max()), np.unravel_index((err - bound).argmax(), err.shape))
 
 
-def _check(dtype, B, H, nq, nk, d, causal, bidirectional, n_buckets, distance, query0, lens, gain=1.0, pad=0, forbid=(), workspace=True, seed=0):
+def _check(dtype, B, H, nq, nk, d, causal, bidirectional, n_buckets, distance, query0, lens, gain=1.0, pad=0, forbid=(), garbage={}, workspace=True, seed=0):
     import torch
     from paper_2405_01248_amd import binding as K
     t, dev, val, table, tv = _make(dtype, B, H, nq, nk, d, seed + nq * 31 + nk, n_buckets, lens, gain, pad)
     for bk in forbid:
         table[bk] = -float("inf")
         tv[bk] = -np.inf
+    for bk, x in garbage.items():      # buckets whose pairs are all masked
+        table[bk] = x
+        tv[bk] = 0.0
     dt, ld, scale = (K.DP_F32 if dtype == "f32" else K.DP_BF16), H * d + pad, 1.0 / np.sqrt(d)
     scale = float(np.float32(scale))
     key_len = torch.tensor(lens, dtype=torch.int32, device="cuda") if lens is not None else None
@@ -154,6 +157,14 @@ def test_strides_large_logits_and_forbidden_buckets(dtype):
     _check(dtype, 1, 2, 400, 400, 64, False, True, 32, 128, 0, None, gain=12.0)
     _check(dtype, 1, 2, 260, 300, 64, False, True, 32, 128, 0, None, forbid=(0, 3, 15, 31))      # -infinity: near, middle and both ends
     _check(dtype, 1, 2, 70, 70, 64, True, False, 8, 16, 0, [70], forbid=range(8))               # nothing is visible at all
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [64, 300, 1000])
+def test_anything_in_buckets_that_the_causal_mask_hides(dtype, n):
+    # two directions of buckets under the causal mask: those of later keys hold infinities and NaN
+    _check(dtype, 1, 2, n, n, 64, True, True, 32, 128, 0, [n - n // 3],
+           garbage={k: v for k, v in zip(range(17, 32), [float("nan"), float("inf"), -float("inf")] * 5)})
 
 
 @pytest.mark.parametrize("nq,nk", [(1, 3001), (32, 2500), (33, 700)])

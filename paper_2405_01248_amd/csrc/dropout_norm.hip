@@ -52,7 +52,7 @@ struct DropoutK {
   DropK drop;
 };
 
-// A thread takes U groups, 256 apart, of the workgroup's 256 U consecutive ones (rows one after the other), all requested before the first mask.
+// 32768 x 1280 bf16 with a residual 46 us, 5.4 TB/s; a copy of 1 GiB runs at 5.05.  A thread takes U groups, 256 apart, of the workgroup's 256 U consecutive ones (rows one after the other), all requested before the first mask.
 template <typename T, int U>
 __global__ void __launch_bounds__(256) dropout_kernel(const DropoutK a) {
   const uint64_t first = (uint64_t)blockIdx.x * (256 * U);
@@ -115,7 +115,7 @@ struct NormK {
   DropK drop;
 };
 
-// y = LayerNorm(residual + dropout(x)).  The statistics are those of the fp32 sum: what is stored of it may have been rounded to 16 bits.
+// y = LayerNorm(residual + dropout(x)).  32768 x 640, fp32 residual and sum: 50 us, 5.1 TB/s.  The statistics are those of the fp32 sum: what is stored of it may have been rounded to 16 bits.
 template <typename T, typename S, int L, int NC>
 __global__ void __launch_bounds__(norm_threads<L>) norm_fwd_kernel(const NormK a) {
   __shared__ float red[2][L > 64 ? L / 64 : 1];
@@ -201,7 +201,7 @@ struct NormBwdK {
 
 // With g = dy gamma and xh = (sum - mean) rstd: dsum = rstd (g - mean(g) - xh mean(g xh)) + dsum_in, dx = dropout of dsum, and the columns' sums of
 // dy xh and dy.  A group of L lanes walks every G-th row, the next one's operands requested before the present one is used; a lane adds its columns of
-// dy xh and dy in registers, and the groups' sums meet in LDS at the end.
+// dy xh and dy in registers, and the groups' sums meet in LDS at the end.  32768 x 640, fp32 residual gradients: 67 us (5.0 TB/s) and 4.7 for the sums.
 template <typename T, typename S, int L, int NC>
 __global__ void __launch_bounds__(norm_threads<L>) norm_bwd_kernel(const NormBwdK a) {
   constexpr int NT = norm_threads<L>, PER = NT / L;      // rows at a time
@@ -300,20 +300,20 @@ __global__ void __launch_bounds__(norm_threads<L>) norm_bwd_kernel(const NormBwd
     }
 }
 
-// Columns' sums of the workgroups' parts [parts][n]: 8 columns of 32 shares of the parts a workgroup, the shares added in their order.
-__global__ void __launch_bounds__(256) norm_bwd_reduce_kernel(const float* __restrict__ partial, int parts, int d, float* __restrict__ dgamma,
-                                                              float* __restrict__ dbeta, int accumulate) {
-  __shared__ float meet[32][8];
-  const int col = blockIdx.x * 8 + threadIdx.x % 8, share = threadIdx.x / 8, n = 2 * d;
+// Columns' sums of the workgroups' parts [parts][n]: 32 columns (a line of memory) and 32 shares of the parts a workgroup, the shares added in their order.
+__global__ void __launch_bounds__(1024) norm_bwd_reduce_kernel(const float* __restrict__ partial, int parts, int d, float* __restrict__ dgamma,
+                                                               float* __restrict__ dbeta, int accumulate) {
+  __shared__ float meet[32][33];
+  const int lane = threadIdx.x % 32, share = threadIdx.x / 32, col = blockIdx.x * 32 + lane, n = 2 * d;
   float s = 0.f;
   if (col < n) {
 #pragma unroll 8
     for (int p = share; p < parts; p += 32) s += partial[(size_t)p * n + col];
   }
-  meet[share][threadIdx.x % 8] = s;
+  meet[share][lane] = s;
   __syncthreads();
-  if (threadIdx.x >= 8 || col >= n) return;
-  for (int w = 1; w < 32; ++w) s += meet[w][threadIdx.x];
+  if (share || col >= n) return;
+  for (int w = 1; w < 32; ++w) s += meet[w][lane];
   float* out = col < d ? dgamma : dbeta;
   const int at = col < d ? col : col - d;
   if (!out) return;
@@ -375,10 +375,11 @@ static bool norm_too_many(int rows, int d) {      // a launch has less than 2^32
   norm_dispatch(d, [&](auto l, auto) { lanes = l; });
   return rows * lanes >= (1l << 31);
 }
-// Workgroups of the backward, hence parts to be added afterwards.
+// Workgroups of the backward, hence parts to be added afterwards: as many as run at once, two a CU (half the registers of a SIMD each wave), four where a row is
+// one group of columns a lane of 256.  512 / 768 / 1024 of them, us without the sum: 32768 x 640 67 / 81 / 69, 8192 x 640 21 / 23 / 23, 32768 x 320 32 / 38 / 35, 8192 x 1152 28 / 26 / 23.
 static int norm_bwd_workgroups(int rows, int d) {
   const int per = norm_rows_per_workgroup(d);
-  return std::min((rows + per - 1) / per, d <= 2048 ? 1024 : 512);
+  return std::min((rows + per - 1) / per, d > 1024 && d <= 2048 ? 1024 : 512);
 }
 template <typename T, typename S> static int norm_fwd_t(const NormK& k, hipStream_t s) {
   norm_dispatch(k.d, [&](auto l, auto nc) {
@@ -482,7 +483,7 @@ int dp_op_layernorm_bwd(int dtype, int sum_f32, int rows, int d, const void* dy,
   }
   if (!dgamma && !dbeta) return DP_OK;
   KScope ks(KK_REDUCE, 0.0, (double)workgroups * 2 * d * 4, s, workgroups, d);
-  hipLaunchKernelGGL(norm_bwd_reduce_kernel, dim3((2 * d + 7) / 8), dim3(256), 0, s, k.partial, workgroups, d, dgamma, dbeta, accumulate != 0);
+  hipLaunchKernelGGL(norm_bwd_reduce_kernel, dim3((2 * d + 31) / 32), dim3(1024), 0, s, k.partial, workgroups, d, dgamma, dbeta, accumulate != 0);
   return launched(who);
 }
 

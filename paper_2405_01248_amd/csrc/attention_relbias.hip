@@ -491,18 +491,20 @@ __host__ __device__ __forceinline__ int rel_sum_stride(const RelBucketsK& r) { r
 // three workgroups of a head of at most 64 fit a CU's LDS.)
 constexpr int REL_SQ = 16, REL_STAGE = REL_SQ * 36;
 __host__ __device__ __forceinline__ int rel_dq_floats(const RelBucketsK& r) { return rel_table_floats(r) + 4 * rel_sum_stride(r) + 4 * REL_STAGE + 64; }
-__device__ __forceinline__ float rel_diagonals(const float* stage, int lane) {
+template <bool TURNED> __device__ __forceinline__ float rel_diagonals(const float* stage, int lane) {      // TURNED: the queries of odd number have the other sign
   float v = 0.f;
   static_for<REL_SQ>([&](auto r) {
     constexpr int row = r();
     constexpr uint64_t lanes = 0xFFFFFFFFull << (REL_SQ - 1 - row);
     const float x = stage[row * 37 + lane - (REL_SQ - 1)];
-    v += __builtin_amdgcn_inverse_ballot_w64(lanes) ? x : 0.f;
+    const float y = __builtin_amdgcn_inverse_ballot_w64(lanes) ? x : 0.f;
+    v = TURNED && row % 2 ? v - y : v + y;
   });
   return v;
 }
 
 // Adds a block of dS, 32 queries (lanes) x 32 keys, along its diagonals to the wave's sums over distances; mine: where this lane's distance of its first key lies.
+template <bool TURNED>
 __device__ __forceinline__ void rel_add_diagonals(const f32x16& s, float* stage, float* mine, int g, int l32, int lane) {
 #pragma unroll
   for (int part = 0; part < 32 / REL_SQ; ++part) {
@@ -513,7 +515,7 @@ __device__ __forceinline__ void rel_add_diagonals(const f32x16& s, float* stage,
         *reinterpret_cast<f32x4*>(stage + l32 % REL_SQ * 36 + 8 * r4 + 4 * g) = f32x4{s[4 * r4], s[4 * r4 + 1], s[4 * r4 + 2], s[4 * r4 + 3]};
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    mine[-REL_SQ * part] += rel_diagonals(stage, lane);
+    mine[-REL_SQ * part] += rel_diagonals<TURNED>(stage, lane);
   }
 }
 
@@ -597,12 +599,22 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 3 : 2) rel_bwd_dq_bf16_kernel
   const int mine = wave * sum_stride + lane - (REL_SQ - 1) - pos0 - (p.bk.lo - REL_MARGIN);
   float far_sum_lo = 0.f, far_sum_hi = 0.f;
 
+  // The matrix instruction rounds downwards when it adds products to an accumulator, by some 1e-9 of dP's size: nothing for dQ, but the table's gradient
+  // adds up millions of pairs whose signs cancel (8 x 10^-6 of it at 3 x 1620 x 1620).  Queries of odd number therefore work with -dO, hence -delta and
+  // -dS, and the errors of neighbours cancel; the sign is put right where a query's results leave the lane.
+  const bool odd = l32 & 1;
+  auto turned = [](bf16x8 v, bool turn) {
+    u32x4 w = __builtin_bit_cast(u32x4, v);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) w[u] ^= turn ? 0x80008000u : 0u;
+    return __builtin_bit_cast(bf16x8, w);
+  };
   bf16x8 qf[KC], dof[KC];
 #pragma unroll
   for (int c = 0; c < KC; ++c) {
     const bool ok = qok && 16 * c + 8 * g < p.dh;
     qf[c] = ld8(qrow + 16 * c + 8 * g, ok);
-    dof[c] = ld8(dorow + 16 * c + 8 * g, ok);
+    dof[c] = turned(ld8(dorow + 16 * c + 8 * g, ok), odd);
   }
   const size_t sidx = ((size_t)b * p.H + h) * p.Nq + qi;
   float lse2 = INFINITY;      // of no query, and of one that sees no key: its probabilities are zero
@@ -620,7 +632,7 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 3 : 2) rel_bwd_dq_bf16_kernel
       for (int u = 0; u < 8; ++u) dlt = fmaf((float)of[u], (float)dof[c][u], dlt);
     }
     dlt = reduce_halves(dlt, AddOp());
-    if (qok && g == 0) p.delta[sidx] = dlt;
+    if (qok && g == 0) p.delta[sidx] = odd ? -dlt : dlt;
   }
   f32x16 ndelta;
 #pragma unroll
@@ -678,7 +690,7 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 3 : 2) rel_bwd_dq_bf16_kernel
         if (below) far_sum_lo += sum;
         else far_sum_hi += sum;
       } else {
-        rel_add_diagonals(s, stage, sums + (mine + kt * 64 + 32 * t), g, l32, lane);
+        rel_add_diagonals<true>(s, stage, sums + (mine + kt * 64 + 32 * t), g, l32, lane);
       }
 #pragma unroll
       for (int cc = 0; cc < 2; ++cc) {
@@ -701,12 +713,12 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 3 : 2) rel_bwd_dq_bf16_kernel
         if (col < p.dh) {
           bf16x4 o;
 #pragma unroll
-          for (int u = 0; u < 4; ++u) o[u] = (bf16)(acc[i][4 * r4 + u] * p.scale);
+          for (int u = 0; u < 4; ++u) o[u] = (bf16)(acc[i][4 * r4 + u] * (odd ? -p.scale : p.scale));
           *reinterpret_cast<bf16x4*>(ob + col) = o;
         }
       }
   }
-  if (p.dtable_partial) rel_bucket_sums(p, st, sums, sum_stride, far_sums, far_sum_lo, far_sum_hi, p.dtable_partial + ((size_t)h * p.B * qtiles + (size_t)b * qtiles + qtile) * p.bk.n_buckets);
+  if (p.dtable_partial) rel_bucket_sums(p, st, sums, sum_stride, far_sums, odd ? -far_sum_lo : far_sum_lo, odd ? -far_sum_hi : far_sum_hi, p.dtable_partial + ((size_t)h * p.B * qtiles + (size_t)b * qtiles + qtile) * p.bk.n_buckets);
 }
 
 // dtable[bucket][head] = sum over the parts, in their order: 32 buckets of a head a workgroup, eight shares of the parts.
@@ -1107,7 +1119,7 @@ __global__ void __launch_bounds__(256) rel_bwd_dq_f32_kernel(const RelAttnK p, c
       if (below) far_sum_lo += sum;
       else far_sum_hi += sum;
     } else {
-      rel_add_diagonals(s, stage, sums + (mine + k0), g, l32, lane);
+      rel_add_diagonals<false>(s, stage, sums + (mine + k0), g, l32, lane);
     }
     rel_columns_product(kc, s, acc);
   }

@@ -57,6 +57,7 @@ struct RelAttnK {
   void* dv; int lddv;
   float* dtable_partial;      // [head][sample and query tile][bucket]
   int even;
+  int qsplits; float* dkv_partial;      // all keys in a workgroup: shares of the queries, and what they leave of dK and dV, [dK, dV][share][key row][column]
   int shares; float* part;      // few queries: shares of the keys, and what they leave: outputs [share][row][column], references and sums [share][row][2]
   RelBucketsK bk;
 };
@@ -101,13 +102,15 @@ __device__ __forceinline__ f32x4 rel_read4(const float* t) { return f32x4{t[0], 
 
 // Workgroup -> (tile, batch * head).  Without the causal mask that of the other attention kernels.  Under it tiles differ in length (the last tiles of
 // queries and the first tiles of keys are the longest): they go by length over all heads, the longest first, so that the launch does not end with
-// few workgroups on their longest tiles; consecutive ids still go round the XCDs, and all tiles of a head to one of them.
+// few workgroups on their longest tiles; and every second 256, which meet the first 256 on the same CUs, the other way round, in steps of eight, so that all tiles of a
+// head still go to one XCD.
 __device__ __forceinline__ void rel_block_map(const RelAttnK& p, int id, int ntiles, bool last_longest, int& tile, int& bh) {
   const int BH = p.B * p.H, full = BH / 8 * 8;
   if (!p.causal || id >= full * ntiles) {
     attn_block_map(id, ntiles, BH, tile, bh);
     return;
   }
+  if ((id & 256) && (id | 255) < full * ntiles) id ^= 248;
   tile = id / full;
   bh = id % full;
   if (last_longest) tile = ntiles - 1 - tile;
@@ -484,58 +487,58 @@ __global__ void __launch_bounds__(256) rel_join_kernel(const RelAttnK p) {
 }
 
 // ------------------------------------------------------------------ dQ and the table's gradient (bf16)
-// Sums of dS over distances: [wave][entry].
+__device__ __forceinline__ bf16x8 rel_turned(bf16x8 v, bool turn) {      // -v
+  u32x4 w = __builtin_bit_cast(u32x4, v);
+#pragma unroll
+  for (int u = 0; u < 4; ++u) w[u] ^= turn ? 0x80008000u : 0u;
+  return __builtin_bit_cast(bf16x8, w);
+}
+// Sums of dS over distances: [wave][half of the wave][entry].
 __host__ __device__ __forceinline__ int rel_sum_stride(const RelBucketsK& r) { return (rel_entries(r) + 3) / 4 * 4; }
-// Half a wave's block of dS on its way to them, [query][key], four floats between the rows.  The diagonals are added by lane: lane l takes the distance
-// l - 15 from the block's first key to its first query, of which query r has the key r + l - 15, where there is one.  (Sixteen queries and not 32:
-// three workgroups of a head of at most 64 fit a CU's LDS.)
-constexpr int REL_SQ = 16, REL_STAGE = REL_SQ * 36;
-__host__ __device__ __forceinline__ int rel_dq_floats(const RelBucketsK& r) { return rel_table_floats(r) + 4 * rel_sum_stride(r) + 4 * REL_STAGE + 64; }
-template <bool TURNED> __device__ __forceinline__ float rel_diagonals(const float* stage, int lane) {      // TURNED: the queries of odd number have the other sign
-  float v = 0.f;
-  static_for<REL_SQ>([&](auto r) {
-    constexpr int row = r();
-    constexpr uint64_t lanes = 0xFFFFFFFFull << (REL_SQ - 1 - row);
-    const float x = stage[row * 37 + lane - (REL_SQ - 1)];
-    const float y = __builtin_amdgcn_inverse_ballot_w64(lanes) ? x : 0.f;
-    v = TURNED && row % 2 ? v - y : v + y;
-  });
-  return v;
-}
-
-// Adds a block of dS, 32 queries (lanes) x 32 keys, along its diagonals to the wave's sums over distances; mine: where this lane's distance of its first key lies.
-template <bool TURNED>
-__device__ __forceinline__ void rel_add_diagonals(const f32x16& s, float* stage, float* mine, int g, int l32, int lane) {
-#pragma unroll
-  for (int part = 0; part < 32 / REL_SQ; ++part) {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    if (l32 / REL_SQ == part) {
-#pragma unroll
-      for (int r4 = 0; r4 < 4; ++r4)
-        *reinterpret_cast<f32x4*>(stage + l32 % REL_SQ * 36 + 8 * r4 + 4 * g) = f32x4{s[4 * r4], s[4 * r4 + 1], s[4 * r4 + 2], s[4 * r4 + 3]};
+__host__ __device__ __forceinline__ int rel_sum_floats(const RelBucketsK& r, int waves) { return rel_table_floats(r) + 2 * waves * rel_sum_stride(r); }
+// The sums of a block of dS (a lane: one query; register r: key 8 (r / 4) + r % 4, in the other half of the wave 4 more) along its diagonals, without leaving the
+// registers.  In a row of 16 lanes key k of lane j lies on diagonal k - j = 16 c - m with m = (j - k) mod 16 and c one of three: a register, moved by k mod 16
+// lanes inside the row, adds to the c of the lanes that stay inside, and moved the other way to the next c of those that left it, two additions with a lane shift
+// each.  Then the rows of queries 0 .. 15 and 16 .. 31 exchange what belongs together: lane l has in `near` the sum of key - query = 4 g - l, in `next` that of 32
+// more.  TURNED: queries 16 .. 31 have the other sign.  (With keys for lanes and queries for registers: of query - key.)
+struct RelDiagonals { float near, next; };
+template <bool TURNED> __device__ __forceinline__ RelDiagonals rel_diagonals(const f32x16& s, int lane) {
+  float acc[3] = {0.f, 0.f, 0.f};
+  static_for<16>([&](auto rc) {
+    constexpr int r = rc(), key = 8 * (r / 4) + r % 4, c = key / 16, n = key % 16;
+    if constexpr (n == 0) {
+      acc[c] += s[r];
+    } else {
+      acc[c] += lane_dpp<0x100 + n>(s[r]);              // row_shl: from lane m + n
+      acc[c + 1] += lane_dpp<0x110 + 16 - n>(s[r]);     // row_shr: from lane m + n - 16
     }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    mine[-REL_SQ * part] += rel_diagonals<TURNED>(stage, lane);
-  }
+  });
+  const bool second = lane & 16;
+  const auto rows = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, acc[1]), __builtin_bit_cast(uint32_t, acc[1]), false, false);
+  const uint32_t r0 = rows[0], r1 = rows[1];
+  const float first1 = __builtin_bit_cast(float, r0), second1 = __builtin_bit_cast(float, r1);      // of either row, in both
+  if constexpr (TURNED) return second ? RelDiagonals{-acc[0], first1 - acc[2]} : RelDiagonals{acc[0] - second1, acc[2]};
+  return second ? RelDiagonals{acc[0], first1 + acc[2]} : RelDiagonals{acc[0] + second1, acc[2]};
 }
 
-// The end of a dQ workgroup: the waves' sums of a distance, then the distances of a bucket (eight lanes each), then what lay beyond the middle.
-__device__ __forceinline__ void rel_bucket_sums(const RelAttnK& p, const RelStarts& st, float* sums, int sum_stride, float (&far_sums)[2][4], float far_sum_lo,
+// The end of a workgroup that summed dS (REVERSED: entry e is distance hi + margin - e): the waves' sums of a distance, then the distances of a bucket (eight lanes each), then what lay beyond the middle.
+template <int NW, bool REVERSED>
+__device__ __forceinline__ void rel_bucket_sums(const RelAttnK& p, const RelStarts& st, float* sums, int sum_stride, float (*far_sums)[NW], float far_sum_lo,
                                                 float far_sum_hi, float* out) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, entries = rel_entries(p.bk);
   far_sum_lo = wave_sum(far_sum_lo);
   far_sum_hi = wave_sum(far_sum_hi);
   if (lane == 0) { far_sums[0][wave] = far_sum_lo; far_sums[1][wave] = far_sum_hi; }
   __syncthreads();
-  for (int e = tid; e < entries; e += 256) {
+  for (int e = tid; e < entries; e += 64 * NW) {
     float v = sums[e];
 #pragma unroll
-    for (int w = 1; w < 4; ++w) v += sums[w * sum_stride + e];
+    for (int w = 1; w < 2 * NW; ++w) v += sums[w * sum_stride + e];
     sums[e] = v;
   }
   __syncthreads();
   const int first = p.bk.lo - REL_MARGIN, last = p.bk.hi + REL_MARGIN;
-  for (int bucket = tid / 8; bucket < (p.bk.n_buckets + 31) / 32 * 32; bucket += 32) {
+  for (int bucket = tid / 8; bucket < (p.bk.n_buckets + 8 * NW - 1) / (8 * NW) * (8 * NW); bucket += 8 * NW) {
     const bool on = bucket < p.bk.n_buckets;
     const int side = on && p.bk.bidirectional && bucket >= p.bk.per_side, k = on ? bucket - side * p.bk.per_side : 0;
     const int n0 = rel_start(p.bk, st, k), n1 = rel_start(p.bk, st, k + 1) - 1;      // distances n0 .. n1 of this direction
@@ -545,14 +548,17 @@ __device__ __forceinline__ void rel_bucket_sums(const RelAttnK& p, const RelStar
     if (!p.bk.bidirectional && k == 0) d1 = last;        // keys behind the query
     float v = 0.f;
     if (on)
-      for (int d = d0 + tid % 8; d <= d1; d += 8) v += sums[d - first];
+      for (int d = d0 + tid % 8; d <= d1; d += 8) v += sums[REVERSED ? last - d : d - first];
     v += lane_dpp<0xB1>(v);       // lanes i ^ 1, i ^ 2, i ^ 7 (by then equal within four): the eight of a bucket
     v += lane_dpp<0x4E>(v);
     v += lane_dpp<0x141>(v);      // row_half_mirror
     if (on && tid % 8 == 0) {
       const int lo_bucket = p.bk.per_side - 1, hi_bucket = p.bk.bidirectional ? 2 * p.bk.per_side - 1 : 0;
-      if (bucket == lo_bucket) v += (far_sums[0][0] + far_sums[0][1]) + (far_sums[0][2] + far_sums[0][3]);
-      if (bucket == hi_bucket) v += (far_sums[1][0] + far_sums[1][1]) + (far_sums[1][2] + far_sums[1][3]);
+      float far[2] = {0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < NW; ++w) far[0] += far_sums[0][w], far[1] += far_sums[1][w];
+      if (bucket == lo_bucket) v += far[0];
+      if (bucket == hi_bucket) v += far[1];
       out[bucket] = v;
     }
   }
@@ -593,28 +599,23 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 3 : 2) rel_bwd_dq_bf16_kernel
   rel_fill<bf16, false>(p, st, h, rel_lds, 256, p.inv_scale);
   float* sums = rel_lds + rel_table_floats(p.bk);
   const int sum_stride = rel_sum_stride(p.bk);
-  float* stage = sums + 4 * sum_stride + 32 + wave * REL_STAGE;      // (what is read of no query's keys lies within 32 floats before and behind)
-  for (int e = tid; e < 4 * sum_stride; e += 256) sums[e] = 0.f;
+  for (int e = tid; e < 8 * sum_stride; e += 256) sums[e] = 0.f;
   const int tab = 4 * g - pos - (p.bk.lo - REL_MARGIN);      // entry of this lane's first key
-  const int mine = wave * sum_stride + lane - (REL_SQ - 1) - pos0 - (p.bk.lo - REL_MARGIN);
+  float* const mine = sums + (2 * wave + g) * sum_stride;
+  float carry = 0.f;      // sums of the block behind in the distances of the one ahead
+  int carry_at = -1;
   float far_sum_lo = 0.f, far_sum_hi = 0.f;
 
   // The matrix instruction rounds downwards when it adds products to an accumulator, by some 1e-9 of dP's size: nothing for dQ, but the table's gradient
-  // adds up millions of pairs whose signs cancel (8 x 10^-6 of it at 3 x 1620 x 1620).  Queries of odd number therefore work with -dO, hence -delta and
-  // -dS, and the errors of neighbours cancel; the sign is put right where a query's results leave the lane.
-  const bool odd = l32 & 1;
-  auto turned = [](bf16x8 v, bool turn) {
-    u32x4 w = __builtin_bit_cast(u32x4, v);
-#pragma unroll
-    for (int u = 0; u < 4; ++u) w[u] ^= turn ? 0x80008000u : 0u;
-    return __builtin_bit_cast(bf16x8, w);
-  };
+  // adds up millions of pairs whose signs cancel (8 x 10^-6 of it at 3 x 1620 x 1620).  The second sixteen queries therefore work with -dO, hence -delta
+  // and -dS, and the errors cancel; the sign is put right where a query's results leave the lane.
+  const bool second = lane & 16;
   bf16x8 qf[KC], dof[KC];
 #pragma unroll
   for (int c = 0; c < KC; ++c) {
     const bool ok = qok && 16 * c + 8 * g < p.dh;
     qf[c] = ld8(qrow + 16 * c + 8 * g, ok);
-    dof[c] = turned(ld8(dorow + 16 * c + 8 * g, ok), odd);
+    dof[c] = rel_turned(ld8(dorow + 16 * c + 8 * g, ok), second);
   }
   const size_t sidx = ((size_t)b * p.H + h) * p.Nq + qi;
   float lse2 = INFINITY;      // of no query, and of one that sees no key: its probabilities are zero
@@ -632,7 +633,7 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 3 : 2) rel_bwd_dq_bf16_kernel
       for (int u = 0; u < 8; ++u) dlt = fmaf((float)of[u], (float)dof[c][u], dlt);
     }
     dlt = reduce_halves(dlt, AddOp());
-    if (qok && g == 0) p.delta[sidx] = odd ? -dlt : dlt;
+    if (qok && g == 0) p.delta[sidx] = second ? -dlt : dlt;
   }
   f32x16 ndelta;
 #pragma unroll
@@ -690,7 +691,11 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 3 : 2) rel_bwd_dq_bf16_kernel
         if (below) far_sum_lo += sum;
         else far_sum_hi += sum;
       } else {
-        rel_add_diagonals<true>(s, stage, sums + (mine + kt * 64 + 32 * t), g, l32, lane);
+        // blocks of the middle follow each other: every distance of this half of the wave is written once
+        const RelDiagonals d = rel_diagonals<true>(s, lane);
+        mine[tab + kt * 64 + 32 * t] = d.near + carry;
+        carry = d.next;
+        carry_at = kt * 64 + 32 * t + 32;
       }
 #pragma unroll
       for (int cc = 0; cc < 2; ++cc) {
@@ -703,6 +708,7 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 3 : 2) rel_bwd_dq_bf16_kernel
     __syncthreads();
   };
   two_stages(0, nkt, tile);
+  if (carry_at >= 0) mine[tab + carry_at] = carry;
   if (qok) {
     bf16* ob = (bf16*)p.dq + ((size_t)b * p.Nq + qi) * p.lddq + h * p.dh;
 #pragma unroll
@@ -713,12 +719,12 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 3 : 2) rel_bwd_dq_bf16_kernel
         if (col < p.dh) {
           bf16x4 o;
 #pragma unroll
-          for (int u = 0; u < 4; ++u) o[u] = (bf16)(acc[i][4 * r4 + u] * (odd ? -p.scale : p.scale));
+          for (int u = 0; u < 4; ++u) o[u] = (bf16)(acc[i][4 * r4 + u] * (second ? -p.scale : p.scale));
           *reinterpret_cast<bf16x4*>(ob + col) = o;
         }
       }
   }
-  if (p.dtable_partial) rel_bucket_sums(p, st, sums, sum_stride, far_sums, odd ? -far_sum_lo : far_sum_lo, odd ? -far_sum_hi : far_sum_hi, p.dtable_partial + ((size_t)h * p.B * qtiles + (size_t)b * qtiles + qtile) * p.bk.n_buckets);
+  if (p.dtable_partial) rel_bucket_sums<4, false>(p, st, sums, sum_stride, far_sums, second ? -far_sum_lo : far_sum_lo, second ? -far_sum_hi : far_sum_hi, p.dtable_partial + ((size_t)h * p.B * qtiles + (size_t)b * qtiles + qtile) * p.bk.n_buckets);
 }
 
 // dtable[bucket][head] = sum over the parts, in their order: 32 buckets of a head a workgroup, eight shares of the parts.
@@ -892,6 +898,304 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
         *reinterpret_cast<bf16x4*>(dvb + col) = ov;
       }
     }
+}
+
+// ------------------------------------------------------------------ dQ, dK, dV and the table's gradient at once (bf16, at most 32 NW keys)
+// A workgroup has all keys of its (sample, head), 32 per wave, and walks the queries of its share in tiles of 64 (see attn_bwd_short_bf16_kernel): scores, dP and
+// exponentials once instead of twice.  Per tile every wave adds to its keys' dK and dV, adds its dS along the diagonals and leaves it in LDS; behind a barrier the
+// dQ of the tile is formed from it and the keys, while the next tile's delta is.  The second sixteen keys of a wave work with -V, hence -delta and
+// -dS (see rel_bwd_dq_bf16_kernel).
+template <int DHP, int NW> struct RelShort {
+  static constexpr int TILE = 64 * DHP, K = 32 * NW * DHP, DS = 32 * NW * 64;                            // elements
+  static_assert(K <= 2 * TILE + DS, "V passes through the second stage and dS");
+  static constexpr int BYTES = (K + 4 * TILE + DS) * (int)sizeof(bf16) + (3 * 64 + 2 * NW) * (int)sizeof(float);
+};
+
+// A wave's dK and dV (lane: key ki): fp32 parts of a query share, or the result; zeros for keys past the sample's length.
+template <int DT>
+__device__ __forceinline__ void rel_store_dkv(const RelAttnK& p, const f32x16 (&dkacc)[DT], const f32x16 (&dvacc)[DT], float dk_scale, int qs, int b, int h, int ki, bool kok, int g) {
+  if (ki >= p.Nk) return;
+  const size_t hd = (size_t)p.H * p.dh, rows = (size_t)p.B * p.Nk, row = (size_t)b * p.Nk + ki;
+#pragma unroll
+  for (int i = 0; i < DT; ++i)
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4) {
+      const int col = 32 * i + 8 * r4 + 4 * g;
+      if (col >= p.dh) continue;
+      f32x4 k, v;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        k[u] = kok ? dkacc[i][4 * r4 + u] * dk_scale : 0.f;
+        v[u] = kok ? dvacc[i][4 * r4 + u] : 0.f;
+      }
+      if (p.qsplits > 1) {
+        float* pk = p.dkv_partial + (qs * rows + row) * hd + h * p.dh + col;
+        *reinterpret_cast<f32x4*>(pk) = k;
+        *reinterpret_cast<f32x4*>(pk + p.qsplits * rows * hd) = v;
+      } else {
+        bf16x4 k4, v4;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) { k4[u] = (bf16)k[u]; v4[u] = (bf16)v[u]; }
+        *reinterpret_cast<bf16x4*>((bf16*)p.dk + row * p.lddk + h * p.dh + col) = k4;
+        *reinterpret_cast<bf16x4*>((bf16*)p.dv + row * p.lddv + h * p.dh + col) = v4;
+      }
+    }
+}
+
+template <int DHP, int KC, int NW>
+__global__ void __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) rel_bwd_short_bf16_kernel(const RelAttnK p, const RelStarts st) {
+  using S = RelShort<DHP, NW>;
+  constexpr int DT = DHP / 32, TILE = S::TILE;
+  constexpr int LPR = DHP == 64 ? 8 : 16, RPP = 64 / LPR, PASSES = 64 / (NW * RPP);      // delta: lanes a row, rows a pass of a wave
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  // what the products of every tile read comes first: an LDS instruction reaches 64 KB past its base register
+  bf16* const QD = reinterpret_cast<bf16*>(smem);      // two stages of Q and dO
+  bf16* const dS = QD + 4 * TILE;
+  bf16* const Vt = QD + 2 * TILE;                      // V on its way to the registers: where the second stage and dS will be
+  bf16* const Kt = dS + S::DS;
+  float* const lse_s = reinterpret_cast<float*>(Kt + S::K);
+  float* const dlt_s = lse_s + 64;                     // -delta, delta
+  float (*const far_sums)[NW] = reinterpret_cast<float (*)[NW]>(dlt_s + 128);
+  float* const rel_lds = dlt_s + 128 + 2 * NW;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, l32 = lane & 31;
+  const int bk_lo = p.bk.lo, bk_hi = p.bk.hi;
+  int qs, bh;
+  attn_block_map(blockIdx.x, p.qsplits, p.B * p.H, qs, bh);
+  const int b = bh / p.H, h = bh % p.H, k0 = 32 * wave, ki = k0 + l32;
+  const int keys = __builtin_amdgcn_readfirstlane(rel_keys(p, b)), groups = (keys + 31) / 32;      // (a wave past the last group has copies, dQ and delta)
+  const bool kok = ki < keys, second = lane & 16;
+  const bf16* ob = (const bf16*)p.o + (size_t)b * p.Nq * p.ldo + h * p.dh;
+  const float* lse_b = p.lse + ((size_t)b * p.H + h) * p.Nq;
+  const u32x4 qr = make_raw_rsrc((const bf16*)p.q + (size_t)b * p.Nq * p.ldq + h * p.dh, attn_slice_bytes(p.Nq, p.ldq, p.dh));
+  const u32x4 dr = make_raw_rsrc((const bf16*)p.dout + (size_t)b * p.Nq * p.lddo + h * p.dh, attn_slice_bytes(p.Nq, p.lddo, p.dh));
+  const u32x4 kr = make_raw_rsrc((const bf16*)p.k + (size_t)b * p.Nk * p.ldk + h * p.dh, rel_slice_bytes(keys, p.ldk, p.dh));
+  const u32x4 vr = make_raw_rsrc((const bf16*)p.v + (size_t)b * p.Nk * p.ldv + h * p.dh, rel_slice_bytes(keys, p.ldv, p.dh));
+  const int nqt_all = (p.Nq + 63) / 64, tps = (nqt_all + p.qsplits - 1) / p.qsplits;
+  const int qt0 = qs * tps, nqt = min(nqt_all, qt0 + tps);      // no share is empty
+
+  AttnFragOff<DHP, KC> fo;
+  fo.init(lane);
+  // four waves copy a query tile of both kinds, eight one kind each
+  AttnTileCopy<DHP> ck, cv, cq, cd;
+  ck.init(wave, lane, p.ldk, p.dh);
+  cv.init(wave, lane, p.ldv, p.dh);
+  cq.init(wave & 3, lane, p.ldq, p.dh);
+  cd.init(wave & 3, lane, p.lddo, p.dh);
+  auto issue = [&](int qt) __attribute__((always_inline)) {
+    const int at = (qt - qt0) & 1;
+    if (NW == 4 || wave < 4) cq.issue(qr, qt * 64, p.ldq, QD + at * 2 * TILE, wave & 3);
+    if (NW == 4 || wave >= 4) cd.issue(dr, qt * 64, p.lddo, QD + (at * 2 + 1) * TILE, wave & 3);
+  };
+  // O and the logarithms of the sums of a tile, kept as loaded until delta is due
+  bf16x8 of[PASSES];
+  float stat = 0.f;
+  const int drow = wave * RPP + lane / LPR, dchunk = lane % LPR;
+  auto load_o = [&](int qt) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) {
+      const int q = qt * 64 + i * NW * RPP + drow;
+      of[i] = ld8(ob + (size_t)q * p.ldo + 8 * dchunk, q < p.Nq && 8 * dchunk < p.dh);
+    }
+    if (wave == 0) stat = lse_b[min((uint32_t)(qt * 64 + lane), (uint32_t)p.Nq - 1u)];
+  };
+  auto statistics = [&](int qt) __attribute__((always_inline)) {
+    const bf16* tile = QD + (((qt - qt0) & 1) * 2 + 1) * TILE;
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) {
+      const int row = i * NW * RPP + drow;
+      float v = 0.f;
+      if (dchunk < DHP / 8) {
+        const bf16x8 df = *reinterpret_cast<const bf16x8*>(tile + row * DHP + 8 * (dchunk ^ AttnTile<DHP>::key(row)));
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v = fmaf((float)of[i][u], (float)df[u], v);
+      }
+      v += lane_dpp<0xB1>(v);       // quad_perm:[1,0,3,2]
+      v += lane_dpp<0x4E>(v);       // quad_perm:[2,3,0,1]
+      v += lane_dpp<0x141>(v);      // row_half_mirror: the other quad of eight
+      if (LPR == 16) v += lane_dpp<0x128>(v);      // row_ror:8
+      if (dchunk == 0) { dlt_s[row] = -v; dlt_s[64 + row] = v; }
+    }
+    if (wave == 0) lse_s[lane] = qt * 64 + lane < p.Nq && stat != -INFINITY ? -stat * p.inv_scale : -INFINITY;
+  };
+
+  ck.issue(kr, 0, p.ldk, Kt, wave);
+  cv.issue(vr, 0, p.ldv, Vt, wave);
+  ck.issue(kr, 16 * NW, p.ldk, Kt + 16 * NW * DHP, wave);
+  cv.issue(vr, 16 * NW, p.ldv, Vt + 16 * NW * DHP, wave);
+  issue(qt0);
+  load_o(qt0);
+  rel_fill<bf16, true>(p, st, h, rel_lds, 64 * NW, LOG2E);
+  float* const sums = rel_lds + rel_table_floats(p.bk);
+  const int sum_stride = rel_sum_stride(p.bk);
+  for (int e = tid; e < 2 * NW * sum_stride; e += 64 * NW) sums[e] = 0.f;
+  const int tab = 4 * g + p.query0 - ki + bk_hi + REL_MARGIN;                                                 // entry of this lane's first query
+  float* const mine = sums + (2 * wave + g) * sum_stride;
+  float carry = 0.f;      // sums of the block behind in the distances of the one ahead
+  int carry_at = -1;
+  float far_sum_lo = 0.f, far_sum_hi = 0.f;
+  f32x16 dkacc[DT], dvacc[DT];
+#pragma unroll
+  for (int i = 0; i < DT; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) { dkacc[i][r] = 0.f; dvacc[i][r] = 0.f; }
+  wait_vmcnt<0>();
+  __syncthreads();
+  const float far_hi = rel_uniform(rel_lds[0]), far_lo = rel_uniform(rel_lds[rel_entries(p.bk) - 1]);
+  bf16x8 kf[KC], vf[KC];      // rows past the last key are zero
+#pragma unroll
+  for (int c = 0; c < KC; ++c) {
+    kf[c] = fo.row_frag(Kt + 32 * wave * DHP, 0, c);
+    vf[c] = rel_turned(fo.row_frag(Vt + 32 * wave * DHP, 0, c), second);
+  }
+  statistics(qt0);
+  lds_barrier();
+  if (wave >= groups) {      // keys that are not there: the products for dQ run over all of them
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<u32x4*>(dS + 32 * wave * 64 + 512 * i + 8 * lane) = u32x4{0u, 0u, 0u, 0u};
+  }
+  if (qt0 + 1 < nqt) {
+    issue(qt0 + 1);
+    load_o(qt0 + 1);
+  }
+
+  auto frag = [](const bf16* lo, const bf16* hi) {
+    const bf16x4 a = lds_read_tr(lo), c = lds_read_tr(hi);
+    return __builtin_shufflevector(a, c, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  auto tile = [&](int qt, auto bc) __attribute__((always_inline)) {
+    const bf16* Q = QD + bc() * 2 * TILE;
+    const bf16* D = Q + TILE;
+    if (wave < groups) {
+      const int pos = p.query0 + qt * 64;      // of the tile's first query
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const bool below = k0 + 31 - pos - 32 * t <= bk_lo, above = k0 - pos - 32 * t - 31 >= bk_hi;
+        f32x16 s, dp;      // S less lse, over the scale, and dP less delta (of the other sign for the second sixteen keys)
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4) {
+          const f32x4 l4 = *reinterpret_cast<const f32x4*>(lse_s + 32 * t + 8 * r4 + 4 * g), d4 = *reinterpret_cast<const f32x4*>(dlt_s + (second ? 64 : 0) + 32 * t + 8 * r4 + 4 * g);
+#pragma unroll
+          for (int u = 0; u < 4; ++u) { s[4 * r4 + u] = l4[u]; dp[4 * r4 + u] = d4[u]; }
+        }
+#pragma unroll
+        for (int c = 0; c < KC; ++c) {
+          s = mfma32(fo.row_frag(Q, t, c), kf[c], s);
+          dp = mfma32(fo.row_frag(D, t, c), vf[c], dp);
+        }
+        if (below || above) {
+          const float far = below ? far_lo : far_hi;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], p.scale_log2, far));
+        } else {
+#pragma unroll
+          for (int r4 = 0; r4 < 4; ++r4) {
+            const f32x4 v = rel_read4(rel_lds + (tab + qt * 64) + 32 * t + 8 * r4);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) s[4 * r4 + u] = __builtin_amdgcn_exp2f(fmaf(s[4 * r4 + u], p.scale_log2, v[u]));
+          }
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dp[r] *= s[r];
+        if (k0 + 32 > keys || (p.causal && k0 + 31 > pos + 32 * t)) {      // what is masked counts for nothing whatever it is
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const bool seen = kok && (!p.causal || ki <= pos + 32 * t + acc_row(r, g));
+            s[r] = seen ? s[r] : 0.f;
+            dp[r] = seen ? dp[r] : 0.f;
+          }
+        }
+        if (below || above) {
+          float sum = 0.f;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) sum += dp[r];
+          if (below) far_sum_lo += sum;
+          else far_sum_hi += sum;
+        } else {
+          const RelDiagonals d = rel_diagonals<true>(dp, lane);
+          mine[tab + qt * 64 + 32 * t] = d.near + carry;
+          carry = d.next;
+          carry_at = qt * 64 + 32 * t + 32;
+        }
+#pragma unroll
+        for (int cc = 0; cc < 2; ++cc) {
+          const bf16x8 pf = pack8(s, 8 * cc), dsf = pack8(dp, 8 * cc);
+          const bf16x8 out = rel_turned(dsf, second);
+#pragma unroll
+          for (int q4 = 0; q4 < 2; ++q4) {
+            const bf16x4 v = q4 ? __builtin_shufflevector(out, out, 4, 5, 6, 7) : __builtin_shufflevector(out, out, 0, 1, 2, 3);
+            *reinterpret_cast<u32x2*>(dS + ki * 64 + 8 * ((4 * t + 2 * cc + q4) ^ AttnTile<64>::key(l32)) + 4 * g) = __builtin_bit_cast(u32x2, v);
+          }
+#pragma unroll
+          for (int i = 0; i < DT; ++i) {
+            dvacc[i] = mfma32(fo.tr_frag(D, 32 * t + 16 * cc, i), pf, dvacc[i]);
+            dkacc[i] = mfma32(fo.tr_frag(Q, 32 * t + 16 * cc, i), dsf, dkacc[i]);
+          }
+        }
+      }
+    }
+    wait_vmcnt<0>();
+    __syncthreads();      // dS is there, and the next tile
+    const bool more = qt + 1 < nqt;
+    if (more) statistics(qt + 1);
+    if (qt + 2 < nqt) {
+      issue(qt + 2);
+      load_o(qt + 2);
+    }
+    // dQ of the tile: blocks of 32 columns (di) x 32 queries (dt)
+    for (int n = wave; n < 2 * DT; n += NW) {
+      const int di = n % DT, dt = n / DT;
+      int kt_lo, kt_hi, ds_lo, ds_hi;
+      AttnFragOff<DHP, KC>::transposed(lane, di, kt_lo, kt_hi);
+      AttnFragOff<64, KC>::transposed(lane, dt, ds_lo, ds_hi);
+      f32x16 acc;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[r] = 0.f;
+#pragma unroll
+      for (int r = 0; r < 32 * NW; r += 16) acc = mfma32(frag(Kt + kt_lo + r * DHP, Kt + kt_hi + r * DHP), frag(dS + ds_lo + r * 64, dS + ds_hi + r * 64), acc);
+      const int q = qt * 64 + 32 * dt + l32;
+      if (q < p.Nq) {
+        bf16* o = (bf16*)p.dq + ((size_t)b * p.Nq + q) * p.lddq + h * p.dh;
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4) {
+          const int col = 32 * di + 8 * r4 + 4 * g;
+          if (col < p.dh) {
+            bf16x4 v;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) v[u] = (bf16)(acc[4 * r4 + u] * p.scale);
+            *reinterpret_cast<bf16x4*>(o + col) = v;
+          }
+        }
+      }
+    }
+    lds_barrier();      // dS has been read, the statistics of the next tile are there
+  };
+  two_stages(qt0, nqt, tile);
+  if (carry_at >= 0) mine[tab + carry_at] = carry;
+  rel_store_dkv<DT>(p, dkacc, dvacc, second ? -p.scale : p.scale, qs, b, h, ki, kok, g);
+  if (p.dtable_partial)
+    rel_bucket_sums<NW, true>(p, st, sums, sum_stride, far_sums, second ? -far_sum_lo : far_sum_lo, second ? -far_sum_hi : far_sum_hi,
+                              p.dtable_partial + ((size_t)h * p.B * p.qsplits + (size_t)b * p.qsplits + qs) * p.bk.n_buckets);
+}
+
+// The query shares' dK and dV, in their order; four columns a thread.
+__global__ void __launch_bounds__(256) rel_dkv_kernel(const RelAttnK p) {
+  const size_t hd = (size_t)p.H * p.dh, rows = (size_t)p.B * p.Nk, at = (blockIdx.x * 256ul + threadIdx.x) * 4, row = at / hd, col = at % hd;
+  if (row >= rows) return;
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    const float* part = p.dkv_partial + which * p.qsplits * rows * hd + at;
+    f32x4 s = *reinterpret_cast<const f32x4*>(part);
+#pragma unroll 4
+    for (int q = 1; q < p.qsplits; ++q) {
+      const f32x4 v = *reinterpret_cast<const f32x4*>(part + q * rows * hd);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) s[u] += v[u];
+    }
+    bf16x4 o;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) o[u] = (bf16)s[u];
+    *reinterpret_cast<bf16x4*>((bf16*)(which ? p.dv : p.dk) + row * (which ? p.lddv : p.lddk) + col) = o;
+  }
 }
 
 // ------------------------------------------------------------------ fp32
@@ -1086,9 +1390,9 @@ __global__ void __launch_bounds__(256) rel_bwd_dq_f32_kernel(const RelAttnK p, c
   rel_fill<float, false>(p, st, h, rel_lds, 256, p.inv_scale);
   float* sums = rel_lds + rel_table_floats(p.bk);
   const int sum_stride = rel_sum_stride(p.bk);
-  float* stage = sums + 4 * sum_stride + 32 + wave * REL_STAGE;
-  for (int e = tid; e < 4 * sum_stride; e += 256) sums[e] = 0.f;
-  const int tab = 4 * g - pos - (bk_lo - REL_MARGIN), mine = wave * sum_stride + lane - (REL_SQ - 1) - pos0 - (bk_lo - REL_MARGIN);
+  for (int e = tid; e < 8 * sum_stride; e += 256) sums[e] = 0.f;
+  const int tab = 4 * g - pos - (bk_lo - REL_MARGIN);      // entry of this lane's first key
+  float* const mine = sums + (2 * wave + g) * sum_stride;
   f32x16 acc[DT];
 #pragma unroll
   for (int i = 0; i < DT; ++i) acc[i] = rel_all16(0.f);
@@ -1119,7 +1423,10 @@ __global__ void __launch_bounds__(256) rel_bwd_dq_f32_kernel(const RelAttnK p, c
       if (below) far_sum_lo += sum;
       else far_sum_hi += sum;
     } else {
-      rel_add_diagonals<false>(s, stage, sums + (mine + k0), g, l32, lane);
+      // this wave's blocks lie 128 keys apart: every distance of this half of the wave is written once
+      const RelDiagonals d = rel_diagonals<false>(s, lane);
+      mine[tab + k0] = d.near;
+      mine[tab + k0 + 32] = d.next;
     }
     rel_columns_product(kc, s, acc);
   }
@@ -1131,7 +1438,7 @@ __global__ void __launch_bounds__(256) rel_bwd_dq_f32_kernel(const RelAttnK p, c
     const float each[4] = {p.scale, p.scale, p.scale, p.scale};
     *reinterpret_cast<f32x4*>((float*)p.dq + ((size_t)b * p.Nq + i) * p.lddq + h * p.dh + col) = rel_meet<DT>(meet, row, col, each);
   }
-  if (p.dtable_partial) rel_bucket_sums(p, st, sums, sum_stride, far_sums, far_sum_lo, far_sum_hi, p.dtable_partial + ((size_t)h * p.B * qtiles + (size_t)b * qtiles + qtile) * p.bk.n_buckets);
+  if (p.dtable_partial) rel_bucket_sums<4, false>(p, st, sums, sum_stride, far_sums, far_sum_lo, far_sum_hi, p.dtable_partial + ((size_t)h * p.B * qtiles + (size_t)b * qtiles + qtile) * p.bk.n_buckets);
 }
 
 template <int DT, int KC>
@@ -1268,21 +1575,40 @@ static int rel_buckets(const char* who, int n_buckets, int max_distance, int bid
 }
 
 static size_t rel_align(size_t n) { return align_up(n, 256); }
-struct RelWorkspace { size_t delta, partial, bytes; };
-// dQ workgroups of a head, each with its sums over buckets
-static size_t rel_parts(int B, int Nq, bool f32) { return (size_t)B * (f32 ? (Nq + 31) / 32 : (Nq + 127) / 128); }
-static RelWorkspace rel_workspace(int B, int H, int Nq, int n_buckets) {
+// Shares of the queries where a workgroup has all keys of a head: as many as run beside each other, of two tiles at least.
+static int rel_query_shares(int B, int H, int Nq) {
+  const long blocks = (long)B * H, tiles = (Nq + 63) / 64;
+  if (blocks >= 256) return 1;
+  const long shares = std::max<long>(1, std::min<long>(std::min<long>(16, tiles / 2), (512 + blocks - 1) / blocks)), each = (tiles + shares - 1) / shares;
+  return (int)((tiles + each - 1) / each);
+}
+// Workgroups that sum dS over buckets, of a head and sample
+static int rel_parts(int dtype, bool all_keys, int B, int H, int Nq) {
+  return dtype == DP_F32 ? (Nq + 31) / 32 : (all_keys ? rel_query_shares(B, H, Nq) : (Nq + 127) / 128);
+}
+// The backward's: the same for both types and any bias
+struct RelWorkspace { size_t delta, partial, dkv, bytes; };
+static RelWorkspace rel_workspace(int B, int H, int Nq, int Nk, int d_head, int n_buckets) {
   RelWorkspace w;
   w.delta = 0;
   w.partial = rel_align((size_t)B * H * Nq * sizeof(float));
-  w.bytes = w.partial + rel_align((size_t)H * rel_parts(B, Nq, true) * n_buckets * sizeof(float));
+  w.dkv = w.partial + rel_align((size_t)H * B * rel_parts(DP_F32, false, B, H, Nq) * n_buckets * sizeof(float));
+  const int shares = Nk <= 256 ? rel_query_shares(B, H, Nq) : 1;
+  w.bytes = w.dkv + (shares > 1 ? rel_align(2 * (size_t)shares * B * Nk * H * d_head * sizeof(float)) : 0);
   return w;
 }
 
-// Dynamic LDS beyond 64 KB in all has to be asked for, once per kernel and device; asking again does no harm.
-template <class K> static int rel_allow_lds(K kern, int tiles, int bytes) {      // tiles: bytes of the kernel's own
-  if (tiles + 2048 + bytes <= 64 * 1024) return DP_OK;
-  if (hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return set_error(DP_EHIP, "hipFuncSetAttribute(attention) failed");
+// LDS beyond 64 KB in all has to be allowed, once per kernel and device (allowing it twice is harmless; the bits only save the call).
+template <auto KERNEL> static int rel_allow_lds(int own, int dynamic) {
+  static std::atomic<uint64_t> devices{0};
+  if (own + 2048 + dynamic <= 64 * 1024) return DP_OK;      // (own: of the tiles; a few rows of statistics come on top)
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess) return set_error(DP_EHIP, "attention with a relative position bias: hipGetDevice failed");
+  const uint64_t bit = dev >= 0 && dev < 64 ? 1ull << dev : 0;
+  if (bit && (devices.load(std::memory_order_acquire) & bit)) return DP_OK;
+  if (hipFuncSetAttribute((const void*)KERNEL, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024 - own - (own ? 2048 : 0)) != hipSuccess)
+    return set_error(DP_EHIP, "attention with a relative position bias: hipFuncSetAttribute failed");
+  devices.fetch_or(bit, std::memory_order_release);
   return DP_OK;
 }
 template <class F> static int rel_dispatch(int d_head, F f) {
@@ -1300,6 +1626,10 @@ template <class F> static int rel_dispatch_f32(int d_head, F f) {
   if (d_head <= 40) return f(integral_constant<int, 2>(), integral_constant<int, 5>());
   if (d_head <= 64) return f(integral_constant<int, 2>(), integral_constant<int, 8>());
   return f(integral_constant<int, 3>(), integral_constant<int, 12>());
+}
+template <class F> static int rel_short_dispatch(int d_head, int Nk, F f) {      // and waves: 32 keys each
+  using std::integral_constant;
+  return rel_dispatch(d_head, [&](auto dhp, auto kc) { return Nk <= 128 ? f(dhp, kc, integral_constant<int, 4>()) : f(dhp, kc, integral_constant<int, 8>()); });
 }
 static int rel_takes_turns(long blocks, int per_cu) { return blocks > 256 && blocks <= 256L * per_cu; }
 static int rel_launched() {
@@ -1373,7 +1703,7 @@ int dp_relative_bucket(int n_buckets, int max_distance, int bidirectional, int d
 
 size_t dp_op_attention_relbias_workspace_bytes(int B, int H, int Nq, int Nk, int d_head, int n_buckets, int backward) {
   if (B <= 0 || H <= 0 || Nq <= 0 || Nk <= 0 || d_head <= 0 || n_buckets <= 0) return 0;
-  if (backward) return rel_workspace(B, H, Nq, n_buckets).bytes;
+  if (backward) return rel_workspace(B, H, Nq, Nk, d_head, n_buckets).bytes;
   return rel_few(B, H, Nq, Nk, d_head) ? rel_share_bytes(B, H, Nq, d_head, rel_shares(B, H, Nq, Nk)) : 0;
 }
 
@@ -1393,7 +1723,7 @@ int dp_op_attention_relbias_fwd(int dtype, int B, int H, int Nq, int Nk, int d_h
   if (dtype == DP_F32) {
     const int table = rel_table_floats(a.bk) * 4;
     return rel_dispatch_f32(d_head, [&](auto dt, auto kc) {
-      DP_TRY(rel_allow_lds(rel_fwd_f32_kernel<dt, kc>, REL_F32_MEET<dt> * 4, table));
+      DP_TRY((rel_allow_lds<rel_fwd_f32_kernel<dt, kc>>(REL_F32_MEET<dt> * 4, table)));
       hipLaunchKernelGGL((rel_fwd_f32_kernel<dt, kc>), dim3((unsigned)((Nq + 31) / 32 * B * H)), dim3(256), table, s, a, st);
       return rel_launched();
     });
@@ -1409,7 +1739,7 @@ int dp_op_attention_relbias_fwd(int dtype, int B, int H, int Nq, int Nk, int d_h
       a.part = (float*)workspace;
     }
     DP_TRY(rel_dispatch(d_head, [&](auto dhp, auto kc) {
-      DP_TRY(rel_allow_lds(rel_fwd_few_bf16_kernel<dhp, kc>, 1024 * dhp, lds));
+      DP_TRY((rel_allow_lds<rel_fwd_few_bf16_kernel<dhp, kc>>(1024 * dhp, lds)));
       hipLaunchKernelGGL((rel_fwd_few_bf16_kernel<dhp, kc>), dim3((unsigned)((Nq + 31) / 32 * B * H * a.shares)), dim3(256), lds, s, a, st);
       return rel_launched();
     }));
@@ -1421,7 +1751,7 @@ int dp_op_attention_relbias_fwd(int dtype, int B, int H, int Nq, int Nk, int d_h
   a.even = rel_takes_turns(blocks, d_head <= 64 ? 4 : 3);
   return rel_dispatch(d_head, [&](auto dhp, auto kc) {
     constexpr int W = dhp == 64 ? 4 : 3;
-    DP_TRY(rel_allow_lds(rel_fwd_bf16_kernel<dhp, kc, W>, 512 * dhp, lds));
+    DP_TRY((rel_allow_lds<rel_fwd_bf16_kernel<dhp, kc, W>>(512 * dhp, lds)));
     hipLaunchKernelGGL((rel_fwd_bf16_kernel<dhp, kc, W>), dim3((unsigned)blocks), dim3(256), lds, s, a, st);
     return rel_launched();
   });
@@ -1442,33 +1772,53 @@ int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_h
   DP_TRY(check_rel(who, dtype, a, bias, true));
   DP_TRY(rel_buckets(who, bias->n_buckets, bias->max_distance, bias->bidirectional, a.bk, st));
   if (dtable && (uintptr_t)dtable % 16) return set_errorf(DP_EALIGN, "%s: dtable is not 16-byte aligned", who);
-  const RelWorkspace w = rel_workspace(B, H, Nq, bias->n_buckets);
+  const RelWorkspace w = rel_workspace(B, H, Nq, Nk, d_head, bias->n_buckets);
   DP_TRY(check_ptr(workspace, "workspace", 256));
   if (workspace_bytes < w.bytes) return set_errorf(DP_EWORKSPACE, "%s: workspace too small (%zu bytes, needs %zu)", who, workspace_bytes, w.bytes);
   a.delta = (float*)((char*)workspace + w.delta);
   a.dtable_partial = dtable ? (float*)((char*)workspace + w.partial) : nullptr;
   hipStream_t s = (hipStream_t)hip_stream;
-  const int parts = (int)rel_parts(B, Nq, dtype == DP_F32);
+  bool all_keys = false;      // one kernel whose workgroups hold all keys (where its LDS suffices for the bias)
+  if (dtype == DP_BF16 && Nk <= 256)
+    DP_TRY(rel_short_dispatch(d_head, Nk, [&](auto dhp, auto, auto nw) {
+      all_keys = RelShort<dhp, nw>::BYTES + rel_sum_floats(a.bk, nw) * 4 <= 160 * 1024;
+      return DP_OK;
+    }));
+  const int parts = B * rel_parts(dtype, all_keys, B, H, Nq);
   const double fl = 4.0 * B * H * (double)Nq * Nk * d_head, by = (dtype == DP_BF16 ? 2.0 : 4.0) * B * H * d_head * (3.0 * Nq + 2.0 * Nk);
   if (dtype == DP_F32) {
     KScope ks(KK_ATTN_F32, 2 * fl, 2 * by, s, Nq, Nk, d_head);
-    const int table = rel_table_floats(a.bk) * 4, both = rel_dq_floats(a.bk) * 4;
+    const int table = rel_table_floats(a.bk) * 4, both = rel_sum_floats(a.bk, 4) * 4;
     DP_TRY(rel_dispatch_f32(d_head, [&](auto dt, auto kc) {
-      DP_TRY(rel_allow_lds(rel_bwd_dq_f32_kernel<dt, kc>, REL_F32_MEET<dt> * 4, both));
+      DP_TRY((rel_allow_lds<rel_bwd_dq_f32_kernel<dt, kc>>(REL_F32_MEET<dt> * 4, both)));
       hipLaunchKernelGGL((rel_bwd_dq_f32_kernel<dt, kc>), dim3((unsigned)((Nq + 31) / 32 * B * H)), dim3(256), both, s, a, st);
       DP_TRY(rel_launched());
-      DP_TRY(rel_allow_lds(rel_bwd_dkv_f32_kernel<dt, kc>, REL_F32_MEET<dt> * 4, table));
+      DP_TRY((rel_allow_lds<rel_bwd_dkv_f32_kernel<dt, kc>>(REL_F32_MEET<dt> * 4, table)));
       hipLaunchKernelGGL((rel_bwd_dkv_f32_kernel<dt, kc>), dim3((unsigned)((Nk + 31) / 32 * B * H)), dim3(256), table, s, a, st);
       return rel_launched();
     }));
+  } else if (all_keys) {
+    KScope ks(KK_ATTN_BWD_DKV, 2 * fl, 2 * by, s, Nq, Nk, d_head);
+    a.qsplits = rel_query_shares(B, H, Nq);
+    a.dkv_partial = (float*)((char*)workspace + w.dkv);
+    DP_TRY(rel_short_dispatch(d_head, Nk, [&](auto dhp, auto kc, auto nw) {
+      const int lds = RelShort<dhp, nw>::BYTES + rel_sum_floats(a.bk, nw) * 4;
+      DP_TRY((rel_allow_lds<rel_bwd_short_bf16_kernel<dhp, kc, nw>>(0, lds)));
+      hipLaunchKernelGGL((rel_bwd_short_bf16_kernel<dhp, kc, nw>), dim3((unsigned)(B * H * a.qsplits)), dim3(64 * nw), lds, s, a, st);
+      return rel_launched();
+    }));
+    if (a.qsplits > 1) {
+      hipLaunchKernelGGL(rel_dkv_kernel, dim3((unsigned)(((size_t)B * Nk * H * d_head / 4 + 255) / 256)), dim3(256), 0, s, a);
+      DP_TRY(rel_launched());
+    }
   } else {
     const long qblocks = (long)((Nq + 127) / 128) * B * H, kblocks = (long)((Nk + 127) / 128) * B * H;
-    const int table = rel_table_floats(a.bk) * 4, both = rel_dq_floats(a.bk) * 4;
+    const int table = rel_table_floats(a.bk) * 4, both = rel_sum_floats(a.bk, 4) * 4;
     {
       KScope ks(KK_ATTN_BWD_DQ, fl, by, s, Nq, Nk, d_head);
       a.even = rel_takes_turns(qblocks, d_head <= 64 ? 3 : 2);
       DP_TRY(rel_dispatch(d_head, [&](auto dhp, auto kc) {
-        DP_TRY(rel_allow_lds(rel_bwd_dq_bf16_kernel<dhp, kc>, 512 * dhp, both));
+        DP_TRY((rel_allow_lds<rel_bwd_dq_bf16_kernel<dhp, kc>>(512 * dhp, both)));
         hipLaunchKernelGGL((rel_bwd_dq_bf16_kernel<dhp, kc>), dim3((unsigned)qblocks), dim3(256), both, s, a, st);
         return rel_launched();
       }));
@@ -1476,7 +1826,7 @@ int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_h
     KScope ks(KK_ATTN_BWD_DKV, fl, by, s, Nq, Nk, d_head);
     a.even = rel_takes_turns(kblocks, 2);
     DP_TRY(rel_dispatch(d_head, [&](auto dhp, auto kc) {
-      DP_TRY(rel_allow_lds(rel_bwd_dkv_bf16_kernel<dhp, kc>, 512 * dhp, table));
+      DP_TRY((rel_allow_lds<rel_bwd_dkv_bf16_kernel<dhp, kc>>(512 * dhp, table)));
       hipLaunchKernelGGL((rel_bwd_dkv_bf16_kernel<dhp, kc>), dim3((unsigned)kblocks), dim3(256), table, s, a, st);
       return rel_launched();
     }));

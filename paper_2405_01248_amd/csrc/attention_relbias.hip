@@ -1015,7 +1015,7 @@ __global__ void __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2,
       if (LPR == 16) v += lane_dpp<0x128>(v);      // row_ror:8
       if (dchunk == 0) { dlt_s[row] = -v; dlt_s[64 + row] = v; }
     }
-    if (wave == 0) lse_s[lane] = qt * 64 + lane < p.Nq && stat != -INFINITY ? -stat * p.inv_scale : -INFINITY;
+    if (wave == 0) lse_s[lane] = qt * 64 + lane < p.Nq && stat != -INFINITY ? stat * LOG2E : INFINITY;      // (a query that sees no key has no probabilities)
   };
 
   ck.issue(kr, 0, p.ldk, Kt, wave);
@@ -1024,7 +1024,7 @@ __global__ void __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2,
   cv.issue(vr, 16 * NW, p.ldv, Vt + 16 * NW * DHP, wave);
   issue(qt0);
   load_o(qt0);
-  rel_fill<bf16, true>(p, st, h, rel_lds, 64 * NW, LOG2E);
+  rel_fill<bf16, true>(p, st, h, rel_lds, 64 * NW, p.inv_scale);
   float* const sums = rel_lds + rel_table_floats(p.bk);
   const int sum_stride = rel_sum_stride(p.bk);
   for (int e = tid; e < 2 * NW * sum_stride; e += 64 * NW) sums[e] = 0.f;
@@ -1041,10 +1041,11 @@ __global__ void __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2,
   wait_vmcnt<0>();
   __syncthreads();
   const float far_hi = rel_uniform(rel_lds[0]), far_lo = rel_uniform(rel_lds[rel_entries(p.bk) - 1]);
+  constexpr bool KEPT = DHP == 64;      // (wide heads have no registers for K as well, and read it again for every tile)
   bf16x8 kf[KC], vf[KC];      // rows past the last key are zero
 #pragma unroll
   for (int c = 0; c < KC; ++c) {
-    kf[c] = fo.row_frag(Kt + 32 * wave * DHP, 0, c);
+    if (KEPT) kf[c] = fo.row_frag(Kt + 32 * wave * DHP, 0, c);
     vf[c] = rel_turned(fo.row_frag(Vt + 32 * wave * DHP, 0, c), second);
   }
   statistics(qt0);
@@ -1070,29 +1071,35 @@ __global__ void __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2,
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         const bool below = k0 + 31 - pos - 32 * t <= bk_lo, above = k0 - pos - 32 * t - 31 >= bk_hi;
-        f32x16 s, dp;      // S less lse, over the scale, and dP less delta (of the other sign for the second sixteen keys)
+        f32x16 s, dp;      // S over the scale; dP less delta, of the other sign for the second sixteen keys
 #pragma unroll
         for (int r4 = 0; r4 < 4; ++r4) {
-          const f32x4 l4 = *reinterpret_cast<const f32x4*>(lse_s + 32 * t + 8 * r4 + 4 * g), d4 = *reinterpret_cast<const f32x4*>(dlt_s + (second ? 64 : 0) + 32 * t + 8 * r4 + 4 * g);
+          const f32x4 d4 = *reinterpret_cast<const f32x4*>(dlt_s + (second ? 64 : 0) + 32 * t + 8 * r4 + 4 * g);
 #pragma unroll
-          for (int u = 0; u < 4; ++u) { s[4 * r4 + u] = l4[u]; dp[4 * r4 + u] = d4[u]; }
-        }
-#pragma unroll
-        for (int c = 0; c < KC; ++c) {
-          s = mfma32(fo.row_frag(Q, t, c), kf[c], s);
-          dp = mfma32(fo.row_frag(D, t, c), vf[c], dp);
+          for (int u = 0; u < 4; ++u) dp[4 * r4 + u] = d4[u];
         }
         if (below || above) {
           const float far = below ? far_lo : far_hi;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], p.scale_log2, far));
+          for (int r = 0; r < 16; ++r) s[r] = far;
         } else {
 #pragma unroll
           for (int r4 = 0; r4 < 4; ++r4) {
             const f32x4 v = rel_read4(rel_lds + (tab + qt * 64) + 32 * t + 8 * r4);
 #pragma unroll
-            for (int u = 0; u < 4; ++u) s[4 * r4 + u] = __builtin_amdgcn_exp2f(fmaf(s[4 * r4 + u], p.scale_log2, v[u]));
+            for (int u = 0; u < 4; ++u) s[4 * r4 + u] = v[u];
           }
+        }
+#pragma unroll
+        for (int c = 0; c < KC; ++c) {
+          s = mfma32(fo.row_frag(Q, t, c), KEPT ? kf[c] : fo.row_frag(Kt + 32 * wave * DHP, 0, c), s);
+          dp = mfma32(fo.row_frag(D, t, c), vf[c], dp);
+        }
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4) {
+          const f32x4 l4 = *reinterpret_cast<const f32x4*>(lse_s + 32 * t + 8 * r4 + 4 * g);
+#pragma unroll
+          for (int u = 0; u < 4; ++u) s[4 * r4 + u] = __builtin_amdgcn_exp2f(fmaf(s[4 * r4 + u], p.scale_log2, -l4[u]));
         }
 #pragma unroll
         for (int r = 0; r < 16; ++r) dp[r] *= s[r];

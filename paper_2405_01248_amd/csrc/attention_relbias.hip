@@ -747,17 +747,20 @@ __global__ void __launch_bounds__(256) rel_dtable_kernel(const float* __restrict
 
 // ------------------------------------------------------------------ dK, dV (bf16)
 // Each wave owns 32 keys and walks the queries in tiles of 64, from the first that sees one of the workgroup's keys (see attn_bwd_dkv_bf16_kernel).  The
-// bias is the addend of the exponent here, and lse what the scores begin with.  Two waves per SIMD: three need 168 registers, and what is spilled
-// for them in the loop costs more than they give (8 x 10 heads of 1024 70 -> 71 us, causal 41 -> 58; 8 x 5 of 4096 370 -> 436).
-template <int DHP, int KC>
-__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) rel_bwd_dkv_bf16_kernel(const RelAttnK p, const RelStarts st) {
+// bias is the addend of the exponent here, and lse what the scores begin with.  MINW: waves per SIMD, exactly; three have no registers for K, which they read from
+// LDS again for every tile, nor for the causal mask: 8 x 10 heads of 1024 72 -> 61 us, 8 x 5 of 4096 372 -> 346, 16 x 16 of 300 33 -> 27.
+template <int DHP, int KC, int MINW>
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(MINW, MINW))) rel_bwd_dkv_bf16_kernel(const RelAttnK p, const RelStarts st) {
   constexpr int DT = DHP / 32, TILE = 64 * DHP;
   __shared__ __attribute__((aligned(1024))) bf16 Qs[2][TILE];
   __shared__ __attribute__((aligned(1024))) bf16 Ds[2][TILE];
+  constexpr bool KEPT = MINW == 2;
+  __shared__ __attribute__((aligned(1024))) bf16 Kt[KEPT ? 8 : 2 * TILE];
   __shared__ __attribute__((aligned(16))) float lse_s[2][64];
   __shared__ __attribute__((aligned(16))) float dlt_s[2][64];
   extern __shared__ __attribute__((aligned(16))) float rel_lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, l32 = lane & 31;
+  const bool causal = MINW == 2 && p.causal;
   const int bk_lo = p.bk.lo, bk_hi = p.bk.hi;
   int ktile, bh;
   rel_block_map(p, blockIdx.x, (p.Nk + 127) / 128, false, ktile, bh);
@@ -773,7 +776,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
   const float* dlt_b = p.delta + ((size_t)b * p.H + h) * p.Nq;
 
   const int nqt = __builtin_amdgcn_readfirstlane(ktile * 128 < keys ? (p.Nq + 63) / 64 : 0);      // (no query sees keys past the sample's length)
-  const int qt0 = p.causal ? max(0, ktile * 128 - p.query0) / 64 : 0;
+  const int qt0 = causal ? max(0, ktile * 128 - p.query0) / 64 : 0;
   AttnFragOff<DHP, KC> fo;
   fo.init(lane);
   AttnTileCopy<DHP> cq, cd;
@@ -797,11 +800,18 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
   rel_fill<bf16, true>(p, st, h, rel_lds, 256, LOG2E);
   const int tab = 4 * g + p.query0 - ki + p.bk.hi + REL_MARGIN;      // entry of this lane's first query
 
+  if constexpr (!KEPT) {
+    const u32x4 kr = make_raw_rsrc((const bf16*)p.k + (size_t)b * p.Nk * p.ldk + h * p.dh, rel_slice_bytes(keys, p.ldk, p.dh));
+    AttnTileCopy<DHP> ck;
+    ck.init(wave, lane, p.ldk, p.dh);
+    ck.issue(kr, ktile * 128, p.ldk, Kt, wave);
+    ck.issue(kr, ktile * 128 + 64, p.ldk, Kt + TILE, wave);
+  }
   bf16x8 kf[KC], vf[KC];
 #pragma unroll
   for (int c = 0; c < KC; ++c) {
     const bool ok = kok && 16 * c + 8 * g < p.dh;
-    kf[c] = ld8(krow + 16 * c + 8 * g, ok);
+    if (KEPT) kf[c] = ld8(krow + 16 * c + 8 * g, ok);
     vf[c] = ld8(vrow + 16 * c + 8 * g, ok);
   }
   f32x16 dkacc[DT], dvacc[DT];
@@ -826,7 +836,8 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
     const int pos = p.query0 + qt * 64;      // of the tile's first query; distances k0 - pos - 63 .. k0 + 31 - pos
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      if (p.causal && k0 > pos + 32 * t + 31) continue;
+      if (MINW > 2) __builtin_amdgcn_sched_barrier(0);      // (the halves' fragments would overlap in registers)
+      if (causal && k0 > pos + 32 * t + 31) continue;
       const bool below = k0 + 31 - pos - 32 * t <= bk_lo, above = k0 - pos - 32 * t - 31 >= bk_hi;
       f32x16 s, dp;      // S less lse, over the scale, and dP less delta: the products accumulate onto them.  The bias is the addend of the exponent
 #pragma unroll
@@ -837,7 +848,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
       }
 #pragma unroll
       for (int c = 0; c < KC; ++c) {
-        s = mfma32(fo.row_frag(Qs[buf], t, c), kf[c], s);
+        s = mfma32(fo.row_frag(Qs[buf], t, c), KEPT ? kf[c] : fo.row_frag(Kt + 32 * wave * DHP, 0, c), s);
         dp = mfma32(fo.row_frag(Ds[buf], t, c), vf[c], dp);
       }
       // a lane whose key is past the sample's length computes garbage that stays in its own accumulator columns, which are not stored
@@ -855,7 +866,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
       }
 #pragma unroll
       for (int r = 0; r < 16; ++r) dp[r] *= s[r];
-      if (p.causal && k0 + 31 > pos + 32 * t) {      // (here and not before the exponential: what is masked counts for nothing whatever it is)
+      if (causal && k0 + 31 > pos + 32 * t) {      // (here and not before the exponential: what is masked counts for nothing whatever it is)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const bool seen = ki <= pos + 32 * t + acc_row(r, g);
@@ -874,6 +885,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
         }
       }
     }
+    if (MINW > 2) __builtin_amdgcn_sched_barrier(0);
     if (more) store_stats(qt + 1, buf ^ 1);
     wait_vmcnt<0>();
     __syncthreads();
@@ -1831,10 +1843,19 @@ int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_h
       }));
     }
     KScope ks(KK_ATTN_BWD_DKV, fl, by, s, Nq, Nk, d_head);
-    a.even = rel_takes_turns(kblocks, 2);
+    // Three waves per SIMD where two would begin a second round; under the causal mask tiles end at different times anyway, and its selects have no registers
+    // left (8 x 10 heads of 1024 40 and 46 us)
+    const bool many = d_head <= 64 && !causal && kblocks > 2 * 256;
+    a.even = rel_takes_turns(kblocks, many ? 3 : 2);
     DP_TRY(rel_dispatch(d_head, [&](auto dhp, auto kc) {
-      DP_TRY((rel_allow_lds<rel_bwd_dkv_bf16_kernel<dhp, kc>>(512 * dhp, table)));
-      hipLaunchKernelGGL((rel_bwd_dkv_bf16_kernel<dhp, kc>), dim3((unsigned)kblocks), dim3(256), table, s, a, st);
+      constexpr int MANY = dhp == 64 ? 3 : 2;
+      if (MANY > 2 && many) {
+        DP_TRY((rel_allow_lds<rel_bwd_dkv_bf16_kernel<dhp, kc, MANY>>(768 * dhp, table)));
+        hipLaunchKernelGGL((rel_bwd_dkv_bf16_kernel<dhp, kc, MANY>), dim3((unsigned)kblocks), dim3(256), table, s, a, st);
+      } else {
+        DP_TRY((rel_allow_lds<rel_bwd_dkv_bf16_kernel<dhp, kc, 2>>(512 * dhp, table)));
+        hipLaunchKernelGGL((rel_bwd_dkv_bf16_kernel<dhp, kc, 2>), dim3((unsigned)kblocks), dim3(256), table, s, a, st);
+      }
       return rel_launched();
     }));
   }

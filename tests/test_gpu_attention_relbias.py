@@ -145,6 +145,11 @@ def _check(dtype, B, H, nq, nk, d, causal, bidirectional, n_buckets, distance, q
     (1, 1, 640, 640, 64, False, True, 32, 128, -300, [-5]),          # a negative length: no keys
     (5, 7, 33, 31, 16, False, True, 8, 20, 0, [31, 30, 29, 1, 0]),
     (16, 20, 129, 130, 64, False, True, 32, 128, 0, None),
+    (16, 12, 70, 300, 64, False, True, 32, 128, 100, [300] * 8 + [257] * 4 + [128, 129, 65, 0]),      # more key tiles than two a CU
+    (16, 12, 66, 270, 40, False, False, 32, 128, 200, None),
+    (2, 3, 90, 200, 96, False, True, 320, 800, 0, [200, 3]),         # few keys, more distances than LDS has room for beside them
+    (2, 3, 520, 128, 88, False, True, 32, 128, 0, None),             # few keys, shares of the queries
+    (3, 9, 384, 384, 64, True, True, 32, 128, 0, None),              # heads that do not go round the XCDs evenly
 ])
 def test_against_the_definition(dtype, B, H, nq, nk, d, causal, bidirectional, n_buckets, distance, query0, lens):
     _check(dtype, B, H, nq, nk, d, causal, bidirectional, n_buckets, distance, query0, lens)

@@ -204,9 +204,10 @@ def _check(code: int):
 
 
 def _ptr(t):
+    """Address of a tensor (an integer: every function below declares its pointers) or None."""
     if t is None:
         return None
-    return C.c_void_p(t.data_ptr()) if hasattr(t, "data_ptr") else C.c_void_p(int(t))
+    return t.data_ptr() if hasattr(t, "data_ptr") else int(t)
 
 
 def _ptr_array(ts: Sequence):
@@ -216,11 +217,21 @@ def _ptr_array(ts: Sequence):
     return arr
 
 
-def _stream(stream):
-    if stream is None:
+_CURRENT_STREAM = None
+
+
+def _current_stream():
+    """Handle of torch's current stream, as an integer.  The raw query where torch has it: a Stream object costs 2.5 us of the host's time, a third of a small call's."""
+    global _CURRENT_STREAM
+    if _CURRENT_STREAM is None:
         import torch
-        stream = torch.cuda.current_stream().cuda_stream
-    return C.c_void_p(int(stream))
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        _CURRENT_STREAM = (lambda: raw(torch.cuda.current_device())) if raw else (lambda: torch.cuda.current_stream().cuda_stream)
+    return _CURRENT_STREAM()
+
+
+def _stream(stream):
+    return _current_stream() if stream is None else int(stream)
 
 
 def _nbytes(t):

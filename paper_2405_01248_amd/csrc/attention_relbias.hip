@@ -76,25 +76,43 @@ __device__ __forceinline__ int rel_bucket(const RelBucketsK& r, const RelStarts&
   }
   return side + (n < r.half ? n : k);
 }
-__device__ __forceinline__ int rel_start(const RelBucketsK& r, const RelStarts& st, int k) {      // least distance of a direction's bucket k
-  if (k < r.half) return k;
-  if (k >= r.per_side) return 1 << 28;
-  const uint32_t two = st.of[(k - r.half) / 2];
-  return (int)((k - r.half) & 1 ? two >> 16 : two & 0xFFFFu);
+// Least distance of each bucket of a direction, and behind the last one more than any in the sums' reach: in LDS from a kernel's beginning, for its end.
+constexpr int REL_STARTS = REL_MAX_BUCKETS + 8;
+__device__ __forceinline__ void rel_fill_starts(const RelBucketsK& r, const RelStarts& st, uint16_t* starts, int threads) {
+  for (int k = threadIdx.x; k <= r.per_side; k += threads) {
+    const uint32_t two = st.of[max(k - r.half, 0) / 2];
+    starts[k] = (uint16_t)(k < r.half ? k : (k == r.per_side ? 0x7FFFu : ((k - r.half) & 1 ? two >> 16 : two & 0xFFFFu)));
+  }
 }
 __host__ __device__ __forceinline__ int rel_entries(const RelBucketsK& r) { return r.hi - r.lo + 1 + 2 * REL_MARGIN; }
 __host__ __device__ __forceinline__ int rel_table_floats(const RelBucketsK& r) { return (rel_entries(r) + 3) / 4 * 4; }
 __device__ __forceinline__ int rel_keys(const RelAttnK& p, int b) { return p.key_len ? max(0, min(p.key_len[b], p.Nk)) : p.Nk; }
 
-// Bias of head h by distance, times a factor.  Entry e is distance lo - margin + e, or, REVERSED, hi + margin - e.
-template <typename T, bool REVERSED>
-__device__ __forceinline__ void rel_fill(const RelAttnK& p, const RelStarts& st, int h, float* tab, int threads, float factor) {
-  const int n = rel_entries(p.bk);
-  for (int e = threadIdx.x; e < n; e += threads) {
+// Bias of head h by distance, times a factor.  Entry e is distance lo - margin + e, or, REVERSED, hi + margin - e.  In two steps, so that the table's
+// loads are on their way beside the first tiles': what a thread has of the first two rounds is requested first and stored behind the tiles' copies.
+template <typename T, bool REVERSED, int THREADS> struct RelFill {
+  T v[2];
+  __device__ __forceinline__ T entry(const RelAttnK& p, const RelStarts& st, int h, int e) const {
     const int dist = REVERSED ? p.bk.hi + REL_MARGIN - e : p.bk.lo - REL_MARGIN + e;
-    tab[e] = to_f<T>(((const T*)p.table)[(size_t)rel_bucket(p.bk, st, dist) * p.H + h]) * factor;
+    return ((const T*)p.table)[(size_t)rel_bucket(p.bk, st, dist) * p.H + h];
   }
-}
+  __device__ __forceinline__ void request(const RelAttnK& p, const RelStarts& st, int h) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int e = threadIdx.x + i * THREADS;
+      if (e < rel_entries(p.bk)) v[i] = entry(p, st, h, e);
+    }
+  }
+  __device__ __forceinline__ void store(const RelAttnK& p, const RelStarts& st, int h, float* tab, float factor) const {
+    const int n = rel_entries(p.bk);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int e = threadIdx.x + i * THREADS;
+      if (e < n) tab[e] = to_f<T>(v[i]) * factor;
+    }
+    for (int e = threadIdx.x + 2 * THREADS; e < n; e += THREADS) tab[e] = to_f<T>(entry(p, st, h, e)) * factor;
+  }
+};
 // The same in all lanes, hence in a scalar register
 __device__ __forceinline__ float rel_uniform(float v) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v))); }
 // Four neighbouring entries
@@ -134,6 +152,8 @@ __global__ void __launch_bounds__(256, MINW) rel_fwd_bf16_kernel(const RelAttnK 
   int qtile, bh;
   rel_block_map(p, blockIdx.x, (p.Nq + BQ - 1) / BQ, true, qtile, bh);
   const int b = bh / p.H, h = bh % p.H;
+  RelFill<bf16, false, 256> fill;
+  fill.request(p, st, h);
   const int q0 = qtile * BQ + wave * 32, qi = q0 + l32, pos0 = p.query0 + q0, pos = pos0 + l32;
   const int keys = __builtin_amdgcn_readfirstlane(rel_keys(p, b));
   const int lim = p.causal ? min(keys, pos + 1) : keys;                                   // keys that this lane's query sees
@@ -154,12 +174,12 @@ __global__ void __launch_bounds__(256, MINW) rel_fwd_bf16_kernel(const RelAttnK 
     ck.issue(kr, 0, p.ldk, Ks[0], wave);
     cv.issue(vr, 0, p.ldv, Vs[0], wave);
   }
-  rel_fill<bf16, false>(p, st, h, rel_lds, 256, p.inv_scale);
   const int tab = 4 * g - pos - (bk_lo - REL_MARGIN);      // entry of this lane's first key
 
   bf16x8 qf[KC];
 #pragma unroll
   for (int c = 0; c < KC; ++c) qf[c] = ld8(qb + (size_t)qi * p.ldq + 16 * c + 8 * g, qi < p.Nq && 16 * c + 8 * g < p.dh);
+  fill.store(p, st, h, rel_lds, p.inv_scale);
   f32x16 oacc[DT];
   float m = -INFINITY, lsum = 0.f;
 #pragma unroll
@@ -308,6 +328,8 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 2 : 1) rel_fwd_few_bf16_kerne
   int part, bh;
   attn_block_map(blockIdx.x, qtiles * p.shares, p.B * p.H, part, bh);
   const int qtile = part / p.shares, share = part % p.shares, b = bh / p.H, h = bh % p.H;
+  RelFill<bf16, false, 256> fill;
+  fill.request(p, st, h);
   const int qi = qtile * 32 + l32, pos0 = p.query0 + qtile * 32, pos = pos0 + l32;
   const int keys = __builtin_amdgcn_readfirstlane(rel_keys(p, b));
   const int lim = p.causal ? min(keys, pos + 1) : keys, lim_all = p.causal ? min(keys, pos0 + 1) : keys;
@@ -335,12 +357,12 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 2 : 1) rel_fwd_few_bf16_kerne
     for (int w = 0; w < 4; ++w) cv[w].issue(vr, kt * 64, p.ldv, Vs[wave][buf], w);
   };
   if (first < last) request(first, 0);
-  rel_fill<bf16, false>(p, st, h, rel_lds, 256, p.inv_scale);
   const int tab = 4 * g - pos - (bk_lo - REL_MARGIN);
   bf16x8 qf[KC];
   const bf16* qrow = (const bf16*)p.q + ((size_t)b * p.Nq + qi) * p.ldq + h * p.dh;
 #pragma unroll
   for (int c = 0; c < KC; ++c) qf[c] = ld8(qrow + 16 * c + 8 * g, qi < p.Nq && 16 * c + 8 * g < p.dh);
+  fill.store(p, st, h, rel_lds, p.inv_scale);
   f32x16 oacc[DT];
   float m = -INFINITY, lsum = 0.f;
 #pragma unroll
@@ -528,7 +550,7 @@ template <bool TURNED> __device__ __forceinline__ RelDiagonals rel_diagonals(con
 
 // The end of a workgroup that summed dS (REVERSED: entry e is distance hi + margin - e): the waves' sums of a distance, then the distances of a bucket (eight lanes each), then what lay beyond the middle.
 template <int NW, bool REVERSED>
-__device__ __forceinline__ void rel_bucket_sums(const RelAttnK& p, const RelStarts& st, float* sums, int sum_stride, float (*far_sums)[NW], float far_sum_lo,
+__device__ __forceinline__ void rel_bucket_sums(const RelAttnK& p, const uint16_t* starts, float* sums, int sum_stride, float (*far_sums)[NW], float far_sum_lo,
                                                 float far_sum_hi, float* out) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, entries = rel_entries(p.bk);
   far_sum_lo = wave_sum(far_sum_lo);
@@ -546,7 +568,7 @@ __device__ __forceinline__ void rel_bucket_sums(const RelAttnK& p, const RelStar
   for (int bucket = tid / 8; bucket < (p.bk.n_buckets + 8 * NW - 1) / (8 * NW) * (8 * NW); bucket += 8 * NW) {
     const bool on = bucket < p.bk.n_buckets;
     const int side = on && p.bk.bidirectional && bucket >= p.bk.per_side, k = on ? bucket - side * p.bk.per_side : 0;
-    const int n0 = rel_start(p.bk, st, k), n1 = rel_start(p.bk, st, k + 1) - 1;      // distances n0 .. n1 of this direction
+    const int n0 = starts[k], n1 = starts[k + 1] - 1;      // distances n0 .. n1 of this direction
     int d0, d1;
     if (side) d0 = max(n0, 1), d1 = min(n1, last);
     else d0 = max(-n1, first), d1 = -n0;
@@ -575,12 +597,16 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 3 : 2) rel_bwd_dq_bf16_kernel
   __shared__ __attribute__((aligned(1024))) bf16 Ks[2][TILE];
   __shared__ __attribute__((aligned(1024))) bf16 Vs[2][TILE];
   __shared__ float far_sums[2][4];
+  __shared__ uint16_t starts[REL_STARTS];
   extern __shared__ __attribute__((aligned(16))) float rel_lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, l32 = lane & 31;
   const int qtiles = (p.Nq + 127) / 128, entries = rel_entries(p.bk), bk_lo = p.bk.lo, bk_hi = p.bk.hi;
   int qtile, bh;
   rel_block_map(p, blockIdx.x, qtiles, true, qtile, bh);
   const int b = bh / p.H, h = bh % p.H;
+  RelFill<bf16, false, 256> fill;
+  fill.request(p, st, h);
+  rel_fill_starts(p.bk, st, starts, 256);
   const int q0 = qtile * 128 + wave * 32, qi = q0 + l32, pos0 = p.query0 + q0, pos = pos0 + l32;
   const bool qok = qi < p.Nq;
   const int keys = __builtin_amdgcn_readfirstlane(rel_keys(p, b));
@@ -601,7 +627,7 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 3 : 2) rel_bwd_dq_bf16_kernel
     ck.issue(kr, 0, p.ldk, Ks[0], wave);
     cv.issue(vr, 0, p.ldv, Vs[0], wave);
   }
-  rel_fill<bf16, false>(p, st, h, rel_lds, 256, p.inv_scale);
+  fill.store(p, st, h, rel_lds, p.inv_scale);
   float* sums = rel_lds + rel_table_floats(p.bk);
   const int sum_stride = rel_sum_stride(p.bk);
   for (int e = tid; e < 8 * sum_stride; e += 256) sums[e] = 0.f;
@@ -729,7 +755,7 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 3 : 2) rel_bwd_dq_bf16_kernel
         }
       }
   }
-  if (p.dtable_partial) rel_bucket_sums<4, false>(p, st, sums, sum_stride, far_sums, second ? -far_sum_lo : far_sum_lo, second ? -far_sum_hi : far_sum_hi, p.dtable_partial + ((size_t)h * p.B * qtiles + (size_t)b * qtiles + qtile) * p.bk.n_buckets);
+  if (p.dtable_partial) rel_bucket_sums<4, false>(p, starts, sums, sum_stride, far_sums, second ? -far_sum_lo : far_sum_lo, second ? -far_sum_hi : far_sum_hi, p.dtable_partial + ((size_t)h * p.B * qtiles + (size_t)b * qtiles + qtile) * p.bk.n_buckets);
 }
 
 // dtable[bucket][head] = sum over the parts, in their order: 32 buckets of a head a workgroup, eight shares of the parts.
@@ -770,6 +796,8 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(MINW, 
   int ktile, bh;
   rel_block_map(p, blockIdx.x, (p.Nk + 127) / 128, false, ktile, bh);
   const int b = bh / p.H, h = bh % p.H;
+  RelFill<bf16, true, 256> fill;
+  fill.request(p, st, h);
   const int k0 = ktile * 128 + wave * 32, ki = k0 + l32;
   const int keys = __builtin_amdgcn_readfirstlane(rel_keys(p, b));
   const bool kok = ki < keys;
@@ -802,7 +830,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(MINW, 
     if (wave == 1) dlt_s[buf][lane] = ok ? -stat : 0.f;
   };
   load_stats(qt0);
-  rel_fill<bf16, true>(p, st, h, rel_lds, 256, LOG2E);
+  fill.store(p, st, h, rel_lds, LOG2E);
   const int tab = 4 * g + p.query0 - ki + p.bk.hi + REL_MARGIN;      // entry of this lane's first query
 
   if constexpr (!KEPT) {
@@ -925,7 +953,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(MINW, 
 template <int DHP, int NW> struct RelShort {
   static constexpr int TILE = 64 * DHP, K = 32 * NW * DHP, DS = 32 * NW * 64;                            // elements
   static_assert(K <= 2 * TILE + DS, "V passes through the second stage and dS");
-  static constexpr int BYTES = (K + 4 * TILE + DS) * (int)sizeof(bf16) + (3 * 64 + 2 * NW) * (int)sizeof(float);
+  static constexpr int BYTES = (K + 4 * TILE + DS) * (int)sizeof(bf16) + (3 * 64 + 2 * NW + REL_STARTS / 2) * (int)sizeof(float);
 };
 
 // A wave's dK and dV (lane: key ki): fp32 parts of a query share, or the result; zeros for keys past the sample's length.
@@ -973,12 +1001,16 @@ __global__ void __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2,
   float* const lse_s = reinterpret_cast<float*>(Kt + S::K);
   float* const dlt_s = lse_s + 64;                     // -delta, delta
   float (*const far_sums)[NW] = reinterpret_cast<float (*)[NW]>(dlt_s + 128);
-  float* const rel_lds = dlt_s + 128 + 2 * NW;
+  uint16_t* const starts = reinterpret_cast<uint16_t*>(dlt_s + 128 + 2 * NW);
+  float* const rel_lds = dlt_s + 128 + 2 * NW + REL_STARTS / 2;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, l32 = lane & 31;
   const int bk_lo = p.bk.lo, bk_hi = p.bk.hi;
   int qs, bh;
   attn_block_map(blockIdx.x, p.qsplits, p.B * p.H, qs, bh);
   const int b = bh / p.H, h = bh % p.H, k0 = 32 * wave, ki = k0 + l32;
+  RelFill<bf16, true, 64 * NW> fill;
+  fill.request(p, st, h);
+  rel_fill_starts(p.bk, st, starts, 64 * NW);
   const int keys = __builtin_amdgcn_readfirstlane(rel_keys(p, b)), groups = (keys + 31) / 32;      // (a wave past the last group has copies, dQ and delta)
   const bool kok = ki < keys, second = lane & 16;
   const bf16* ob = (const bf16*)p.o + (size_t)b * p.Nq * p.ldo + h * p.dh;
@@ -1041,7 +1073,7 @@ __global__ void __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2,
   cv.issue(vr, 16 * NW, p.ldv, Vt + 16 * NW * DHP, wave);
   issue(qt0);
   load_o(qt0);
-  rel_fill<bf16, true>(p, st, h, rel_lds, 64 * NW, p.inv_scale);
+  fill.store(p, st, h, rel_lds, p.inv_scale);
   float* const sums = rel_lds + rel_table_floats(p.bk);
   const int sum_stride = rel_sum_stride(p.bk);
   for (int e = tid; e < 2 * NW * sum_stride; e += 64 * NW) sums[e] = 0.f;
@@ -1197,7 +1229,7 @@ __global__ void __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2,
   if (carry_at >= 0) mine[tab + carry_at] = carry;
   rel_store_dkv<DT>(p, dkacc, dvacc, second ? -p.scale : p.scale, qs, b, h, ki, kok, g);
   if (p.dtable_partial)
-    rel_bucket_sums<NW, true>(p, st, sums, sum_stride, far_sums, second ? -far_sum_lo : far_sum_lo, second ? -far_sum_hi : far_sum_hi,
+    rel_bucket_sums<NW, true>(p, starts, sums, sum_stride, far_sums, second ? -far_sum_lo : far_sum_lo, second ? -far_sum_hi : far_sum_hi,
                               p.dtable_partial + ((size_t)h * p.B * p.qsplits + (size_t)b * p.qsplits + qs) * p.bk.n_buckets);
 }
 
@@ -1312,6 +1344,8 @@ __global__ void __launch_bounds__(256) rel_fwd_f32_kernel(const RelAttnK p, cons
   int qtile, bh;
   rel_block_map(p, blockIdx.x, (p.Nq + 31) / 32, true, qtile, bh);
   const int b = bh / p.H, h = bh % p.H, qi = qtile * 32 + l32, pos0 = p.query0 + qtile * 32, pos = pos0 + l32;
+  RelFill<float, false, 256> fill;
+  fill.request(p, st, h);
   const int keys = __builtin_amdgcn_readfirstlane(rel_keys(p, b));
   const int lim = p.causal ? min(keys, pos + 1) : keys, lim_all = p.causal ? min(keys, pos0 + 1) : keys;
   const int lim_any = p.causal ? min(keys, p.query0 + min(p.Nq, qtile * 32 + 32)) : keys, nkt = lim_any > 0 ? (lim_any + 31) / 32 : 0;
@@ -1320,7 +1354,7 @@ __global__ void __launch_bounds__(256) rel_fwd_f32_kernel(const RelAttnK p, cons
   RelRows<KC> q, k;
   q.load((const float*)p.q + (size_t)b * p.Nq * p.ldq + h * p.dh, min(qi, p.Nq - 1), p.ldq, p.dh, g);
   if (wave < nkt) k.load(kb, min(32 * wave + l32, keys - 1), p.ldk, p.dh, g);
-  rel_fill<float, false>(p, st, h, rel_lds, 256, p.inv_scale);
+  fill.store(p, st, h, rel_lds, p.inv_scale);
   const int tab = 4 * g - pos - (bk_lo - REL_MARGIN);      // entry of this lane's first key
   f32x16 oacc[DT];
 #pragma unroll
@@ -1385,12 +1419,16 @@ template <int DT, int KC>
 __global__ void __launch_bounds__(256) rel_bwd_dq_f32_kernel(const RelAttnK p, const RelStarts st) {
   __shared__ __attribute__((aligned(16))) float meet[REL_F32_MEET<DT>];
   __shared__ float far_sums[2][4];
+  __shared__ uint16_t starts[REL_STARTS];
   extern __shared__ __attribute__((aligned(16))) float rel_lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, l32 = lane & 31;
   const int bk_lo = p.bk.lo, bk_hi = p.bk.hi, qtiles = (p.Nq + 31) / 32, entries = rel_entries(p.bk);
   int qtile, bh;
   rel_block_map(p, blockIdx.x, qtiles, true, qtile, bh);
   const int b = bh / p.H, h = bh % p.H, qi = qtile * 32 + l32, pos0 = p.query0 + qtile * 32, pos = pos0 + l32;
+  RelFill<float, false, 256> fill;
+  fill.request(p, st, h);
+  rel_fill_starts(p.bk, st, starts, 256);
   const bool qok = qi < p.Nq;
   const int keys = __builtin_amdgcn_readfirstlane(rel_keys(p, b));
   const int lim = p.causal ? min(keys, pos + 1) : keys, lim_all = p.causal ? min(keys, pos0 + 1) : keys;
@@ -1411,7 +1449,7 @@ __global__ void __launch_bounds__(256) rel_bwd_dq_f32_kernel(const RelAttnK p, c
     for (int u = 0; u < 4; ++u) dlt = fmaf(k.v[c][u], dout.v[c][u], dlt);
   dlt = reduce_halves(dlt, AddOp());
   if (qok && tid < 32) p.delta[sidx] = dlt;
-  rel_fill<float, false>(p, st, h, rel_lds, 256, p.inv_scale);
+  fill.store(p, st, h, rel_lds, p.inv_scale);
   float* sums = rel_lds + rel_table_floats(p.bk);
   const int sum_stride = rel_sum_stride(p.bk);
   for (int e = tid; e < 8 * sum_stride; e += 256) sums[e] = 0.f;
@@ -1423,12 +1461,19 @@ __global__ void __launch_bounds__(256) rel_bwd_dq_f32_kernel(const RelAttnK p, c
   float far_sum_lo = 0.f, far_sum_hi = 0.f;
   __syncthreads();
   const float far_lo = rel_uniform(rel_lds[0]), far_hi = rel_uniform(rel_lds[entries - 1]);
+  constexpr bool AHEAD = DT < 3;      // the rows of the next tile requested behind this one's products (wide heads have no registers for them)
+  RelRows<KC> v;
+  if (AHEAD && wave < nkt) {
+    k.load(kb, min(32 * wave + l32, keys - 1), p.ldk, p.dh, g);
+    v.load(vb, min(32 * wave + l32, keys - 1), p.ldv, p.dh, g);
+  }
   for (int kt = wave; kt < nkt; kt += 4) {
     const int k0 = 32 * kt, row = min(k0 + l32, keys - 1);
-    RelRows<KC> v;
     RelColumns<DT> kc;
-    k.load(kb, row, p.ldk, p.dh, g);
-    v.load(vb, row, p.ldv, p.dh, g);
+    if (!AHEAD) {
+      k.load(kb, row, p.ldk, p.dh, g);
+      v.load(vb, row, p.ldv, p.dh, g);
+    }
     kc.load(kb, k0, keys - 1, p.ldk, p.dh, g, l32);
     const bool below = k0 + 31 - pos0 <= bk_lo, above = k0 - pos0 - 31 >= bk_hi;
     f32x16 s = below ? rel_all16(far_lo) : (above ? rel_all16(far_hi) : rel_bias16(rel_lds, tab + k0));
@@ -1436,6 +1481,11 @@ __global__ void __launch_bounds__(256) rel_bwd_dq_f32_kernel(const RelAttnK p, c
     const f32x16 dp = rel_rows_product(v, dout, rel_all16(-dlt));
 #pragma unroll
     for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], p.scale_log2, -lse2)) * dp[r];
+    if (AHEAD && kt + 4 < nkt) {
+      const int next = min(k0 + 128 + l32, keys - 1);
+      k.load(kb, next, p.ldk, p.dh, g);
+      v.load(vb, next, p.ldv, p.dh, g);
+    }
     if (k0 + 32 > lim_all) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] = k0 + acc_row(r, g) < lim ? s[r] : 0.f;
@@ -1462,7 +1512,7 @@ __global__ void __launch_bounds__(256) rel_bwd_dq_f32_kernel(const RelAttnK p, c
     const float each[4] = {p.scale, p.scale, p.scale, p.scale};
     *reinterpret_cast<f32x4*>((float*)p.dq + ((size_t)b * p.Nq + i) * p.lddq + h * p.dh + col) = rel_meet<DT>(meet, row, col, each);
   }
-  if (p.dtable_partial) rel_bucket_sums<4, false>(p, st, sums, sum_stride, far_sums, far_sum_lo, far_sum_hi, p.dtable_partial + ((size_t)h * p.B * qtiles + (size_t)b * qtiles + qtile) * p.bk.n_buckets);
+  if (p.dtable_partial) rel_bucket_sums<4, false>(p, starts, sums, sum_stride, far_sums, far_sum_lo, far_sum_hi, p.dtable_partial + ((size_t)h * p.B * qtiles + (size_t)b * qtiles + qtile) * p.bk.n_buckets);
 }
 
 template <int DT, int KC>
@@ -1474,6 +1524,8 @@ __global__ void __launch_bounds__(256) rel_bwd_dkv_f32_kernel(const RelAttnK p, 
   int ktile, bh;
   rel_block_map(p, blockIdx.x, (p.Nk + 31) / 32, false, ktile, bh);
   const int b = bh / p.H, h = bh % p.H, k0 = ktile * 32, ki = k0 + l32;
+  RelFill<float, true, 256> fill;
+  fill.request(p, st, h);
   const int keys = __builtin_amdgcn_readfirstlane(rel_keys(p, b));
   const int nqt = k0 < keys ? (p.Nq + 31) / 32 : 0, first = p.causal ? max(0, k0 - p.query0) / 32 : 0;
   const float* qb = (const float*)p.q + (size_t)b * p.Nq * p.ldq + h * p.dh;
@@ -1483,7 +1535,7 @@ __global__ void __launch_bounds__(256) rel_bwd_dkv_f32_kernel(const RelAttnK p, 
   f32x16 dkacc[DT], dvacc[DT];
 #pragma unroll
   for (int i = 0; i < DT; ++i) dkacc[i] = dvacc[i] = rel_all16(0.f);
-  rel_fill<float, true>(p, st, h, rel_lds, 256, p.inv_scale);
+  fill.store(p, st, h, rel_lds, p.inv_scale);
   const int tab = 4 * g + p.query0 - ki + bk_hi + REL_MARGIN;      // entry of this lane's first query
   __syncthreads();
   const float far_hi = rel_uniform(rel_lds[0]), far_lo = rel_uniform(rel_lds[rel_entries(p.bk) - 1]);
@@ -1491,12 +1543,19 @@ __global__ void __launch_bounds__(256) rel_bwd_dkv_f32_kernel(const RelAttnK p, 
     RelRows<KC> k, v;      // (a lane whose key is past the sample's length computes what is not stored)
     k.load((const float*)p.k + (size_t)b * p.Nk * p.ldk + h * p.dh, min(ki, keys - 1), p.ldk, p.dh, g);
     v.load((const float*)p.v + (size_t)b * p.Nk * p.ldv + h * p.dh, min(ki, keys - 1), p.ldv, p.dh, g);
+    constexpr bool AHEAD = DT < 3;
+    RelRows<KC> q, dout;
+    if (AHEAD) {
+      q.load(qb, min(32 * (first + wave) + l32, p.Nq - 1), p.ldq, p.dh, g);
+      dout.load(dob, min(32 * (first + wave) + l32, p.Nq - 1), p.lddo, p.dh, g);
+    }
     for (int qt = first + wave; qt < nqt; qt += 4) {
       const int q0 = 32 * qt, row = min(q0 + l32, p.Nq - 1), pos0 = p.query0 + q0;
-      RelRows<KC> q, dout;
       RelColumns<DT> qc, dc;
-      q.load(qb, row, p.ldq, p.dh, g);
-      dout.load(dob, row, p.lddo, p.dh, g);
+      if (!AHEAD) {
+        q.load(qb, row, p.ldq, p.dh, g);
+        dout.load(dob, row, p.lddo, p.dh, g);
+      }
       qc.load(qb, q0, p.Nq - 1, p.ldq, p.dh, g, l32);
       dc.load(dob, q0, p.Nq - 1, p.lddo, p.dh, g, l32);
       float lse2[16];
@@ -1512,6 +1571,11 @@ __global__ void __launch_bounds__(256) rel_bwd_dkv_f32_kernel(const RelAttnK p, 
       f32x16 s = below ? rel_all16(far_lo) : (above ? rel_all16(far_hi) : rel_bias16(rel_lds, tab + q0));
       s = rel_rows_product(q, k, s);
       dp = rel_rows_product(dout, v, dp);
+      if (AHEAD && qt + 4 < nqt) {
+        const int next = min(q0 + 128 + l32, p.Nq - 1);
+        q.load(qb, next, p.ldq, p.dh, g);
+        dout.load(dob, next, p.lddo, p.dh, g);
+      }
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], p.scale_log2, -lse2[r]));

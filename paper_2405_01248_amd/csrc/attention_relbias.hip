@@ -24,8 +24,8 @@
 #include <string.h>
 #include <algorithm>
 #include <atomic>
+#include <iterator>
 #include <type_traits>
-#include <vector>
 
 namespace dp {
 
@@ -1612,23 +1612,27 @@ __global__ void __launch_bounds__(256) rel_bwd_dkv_f32_kernel(const RelAttnK p, 
 }
 
 // ------------------------------------------------------------------ host side
-// base^e * other^f as words of 32 bits, least first
-static std::vector<uint32_t> rel_power(uint32_t base, int e, uint32_t other, int f) {
-  std::vector<uint32_t> w{1};
+// base^e other^f in words of 32 bits, the least first: at most 1024^255 256^256, 4598 bits.  (No allocation: nothing may be thrown here.)
+struct RelPower { int n; uint32_t w[160]; };
+static RelPower rel_power(uint32_t base, int e, uint32_t other, int f) {
+  RelPower p;
+  p.n = 1;
+  p.w[0] = 1;
   for (int i = 0; i < e + f; ++i) {
     uint64_t carry = 0;
-    for (uint32_t& x : w) {
-      carry += (uint64_t)x * (i < e ? base : other);
-      x = (uint32_t)carry;
+    for (int j = 0; j < p.n; ++j) {
+      carry += (uint64_t)p.w[j] * (i < e ? base : other);
+      p.w[j] = (uint32_t)carry;
       carry >>= 32;
     }
-    if (carry) w.push_back((uint32_t)carry);
+    if (carry) p.w[p.n++] = (uint32_t)carry;
   }
-  return w;
+  return p;
 }
-static bool rel_less(const std::vector<uint32_t>& a, const std::vector<uint32_t>& b) {
-  if (a.size() != b.size()) return a.size() < b.size();
-  return std::lexicographical_compare(a.rbegin(), a.rend(), b.rbegin(), b.rend());
+static bool rel_less(const RelPower& a, const RelPower& b) {
+  if (a.n != b.n) return a.n < b.n;
+  return std::lexicographical_compare(std::reverse_iterator<const uint32_t*>(a.w + a.n), std::reverse_iterator<const uint32_t*>(a.w),
+                                      std::reverse_iterator<const uint32_t*>(b.w + b.n), std::reverse_iterator<const uint32_t*>(b.w));
 }
 
 // Bucket half + k begins with the least whole n for which n >= half (far / half)^(k / rest).  Where that border is a whole number or next to one, as it is for

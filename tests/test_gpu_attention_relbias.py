@@ -155,6 +155,38 @@ def test_against_the_definition(dtype, B, H, nq, nk, d, causal, bidirectional, n
     _check(dtype, B, H, nq, nk, d, causal, bidirectional, n_buckets, distance, query0, lens)
 
 
+@pytest.mark.parametrize("d", [4, 12, 20, 36, 68, 92])
+def test_fp32_head_widths(d):
+    _check("f32", 2, 2, 45, 77, d, True, True, 16, 64, 40, [77, 50])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_offsets_beyond_32_bits(dtype):
+    """Keys and values of five samples, rows 2^17 elements apart, so that the last sample lies beyond 4 GiB: the same bits as from dense rows."""
+    import torch
+    from paper_2405_01248_amd import binding as K
+    t, dt, n, ld = (torch.float32, K.DP_F32, 2100, 1 << 17) if dtype == "f32" else (torch.bfloat16, K.DP_BF16, 4096, 1 << 17)
+    B, H, d, nq, nb = 5, 1, 64, 40, 32
+    wide = torch.empty((B, n, ld), dtype=t, device="cuda")
+    kv = torch.randn((B, n, 2 * d), device="cuda").to(t)
+    wide[:, :, :2 * d] = kv
+    q, do, table = torch.randn((B, nq, d), device="cuda").to(t), torch.randn((B, nq, d), device="cuda").to(t), torch.randn((nb, H), device="cuda").to(t)
+    ws = torch.empty(K.op_attention_relbias_workspace_bytes(B, H, nq, n, d, nb, True), dtype=torch.uint8, device="cuda")
+    wf = torch.empty(K.op_attention_relbias_workspace_bytes(B, H, nq, n, d, nb, False), dtype=torch.uint8, device="cuda")
+    out = []
+    for x, l in ((kv, 2 * d), (wide, ld)):
+        g = torch.zeros_like(x)
+        o, lse, dq, tab = torch.empty_like(q), torch.empty((B, H, nq), device="cuda"), torch.empty_like(q), torch.empty((nb, H), device="cuda")
+        bias = K.RelBias(table, nb, 128, True, n - nq)
+        K.op_attention_relbias_fwd(dt, B, H, nq, n, d, False, 0.125, q, d, x, l, x[:, :, d:], l, bias, None, o, d, lse, wf)
+        K.op_attention_relbias_bwd(dt, B, H, nq, n, d, False, 0.125, q, d, x, l, x[:, :, d:], l, bias, None, o, d, lse, do, d, dq, d, g, l, g[:, :, d:], l, tab, False, ws)
+        out.append([o, lse, dq, tab, g[:, :, :2 * d].clone()])
+        del g
+    for a, b in zip(*out):
+        assert torch.equal(a, b)
+    torch.cuda.empty_cache()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_strides_large_logits_and_forbidden_buckets(dtype):
     _check(dtype, 2, 3, 150, 190, 40, False, True, 32, 128, 20, [190, 77], pad=24)

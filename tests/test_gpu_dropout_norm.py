@@ -181,6 +181,34 @@ def test_layernorm(dtype, sum_f32, rows, d, pad, p, residual, affine):
     assert torch.equal(dx2, dx)
 
 
+def test_offsets_beyond_32_bits():
+    """Rows 2^20 elements apart, the last beyond 4 GiB: the same bits as from dense rows."""
+    import torch
+    from paper_2405_01248_amd import binding as B
+    rows, d, ld = 2500, 200, 1 << 20
+    wide, dense = torch.empty((rows, ld), dtype=torch.bfloat16, device="cuda"), torch.randn((rows, d), device="cuda").bfloat16()
+    wide[:, :d] = dense
+    gamma, beta = torch.randn(d, device="cuda").bfloat16(), torch.randn(d, device="cuda").bfloat16()
+    ws = torch.empty(B.op_layernorm_bwd_workspace_bytes(rows, d), dtype=torch.uint8, device="cuda")
+    out = []
+    for x, l in ((dense, d), (wide, ld)):
+        y = torch.empty((rows, d), dtype=torch.bfloat16, device="cuda")
+        mean, rstd, dg, db = (torch.empty(n, device="cuda") for n in (rows, rows, d, d))
+        B.op_layernorm_fwd(B.DP_BF16, False, rows, d, 1e-5, x, l, x, l, 0.1, _rng(), 1, 0, gamma, beta, None, 0, y, d, mean, rstd)
+        z, dx = torch.empty_like(y), torch.empty_like(y)
+        B.op_dropout(B.DP_BF16, rows, d, x, l, x, l, 0.3, _rng(), 2, 0, z, d)
+        B.op_layernorm_bwd(B.DP_BF16, False, rows, d, x, l, x, l, mean, rstd, gamma, x, l, 0.1, _rng(), 1, 0, None, 0, dx, d, dg, db, False, ws)
+        out.append([y, mean, rstd, z, dx, dg, db])
+    for a, b in zip(*out):
+        assert torch.equal(a, b)
+    dense2 = wide      # written rows far apart
+    B.op_dropout(B.DP_BF16, rows, d, dense, d, None, 0, 0.3, _rng(), 2, 0, dense2, ld)
+    B.op_dropout(B.DP_BF16, rows, d, dense, d, None, 0, 0.3, _rng(), 2, 0, out[0][3], d)
+    assert torch.equal(dense2[:, :d], out[0][3])
+    del wide, dense2
+    torch.cuda.empty_cache()
+
+
 def test_layernorm_of_a_large_offset_and_a_constant_row():
     # rows far from zero: the centred values are formed before they are squared; a constant row has variance zero
     import torch

@@ -52,37 +52,28 @@ struct DropoutK {
   DropK drop;
 };
 
-// 32768 x 1280 bf16 with a residual 46 us, 5.4 TB/s; a copy of 1 GiB runs at 5.05.  A thread takes U groups, 256 apart, of the workgroup's 256 U consecutive ones (rows one after the other), all requested before the first mask.
-template <typename T, int U>
+// A thread takes eight columns of a row, the workgroup 256 consecutive such groups, rows one after the other.  Bytes bound it: 32768 x 1280 bf16 with a residual
+// 46 us, 5.4 TB/s (a copy of 1 GiB runs at 5.05).  With two groups a thread nothing is gained; found in the caches, one and two: 38 and 38 us, 4096 x 1280 6.6 and 6.8, 2048 x 640 3.5 and 4.0.
+template <typename T>
 __global__ void __launch_bounds__(256) dropout_kernel(const DropoutK a) {
-  const uint64_t first = (uint64_t)blockIdx.x * (256 * U);
-  const uint32_t row_first = (uint32_t)(first / (uint32_t)a.groups), rest = (uint32_t)(first % (uint32_t)a.groups);
+  const uint64_t first = (uint64_t)blockIdx.x * 256;
+  const uint32_t at = (uint32_t)(first % (uint32_t)a.groups) + threadIdx.x, over = at / (uint32_t)a.groups, row = (uint32_t)(first / (uint32_t)a.groups) + over;
+  const int group = (int)(at - over * (uint32_t)a.groups), n = a.cols - 8 * group;
   const DropKey key = drop_key(a.drop);
-  uint32_t row[U], group[U];
-  typename Row8<T>::value xv[U], rv[U];
+  if (row >= (uint32_t)a.rows) return;
+  const size_t c = 8 * (size_t)group;
+  const auto xv = row8_load((const T*)a.x + (size_t)row * a.ldx + c, n);
+  typename Row8<T>::value rv;
+  if (a.residual) rv = row8_load((const T*)a.residual + (size_t)row * a.ldr + c, n);
+  float v[8], r[8];
+  row8_widen<T>(xv, v);
+  drop8(a.drop, key, group, row, v);
+  if (a.residual) {
+    row8_widen<T>(rv, r);
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const uint32_t at = rest + 256 * u + threadIdx.x, over = at / (uint32_t)a.groups;
-    row[u] = row_first + over;
-    group[u] = at - over * (uint32_t)a.groups;
-    if (row[u] >= (uint32_t)a.rows) continue;
-    const int n = a.cols - 8 * (int)group[u];
-    xv[u] = row8_load((const T*)a.x + (size_t)row[u] * a.ldx + 8 * (size_t)group[u], n);
-    if (a.residual) rv[u] = row8_load((const T*)a.residual + (size_t)row[u] * a.ldr + 8 * (size_t)group[u], n);
+    for (int j = 0; j < 8; ++j) v[j] += r[j];
   }
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    if (row[u] >= (uint32_t)a.rows) continue;
-    float v[8], r[8];
-    row8_widen<T>(xv[u], v);
-    drop8(a.drop, key, group[u], row[u], v);
-    if (a.residual) {
-      row8_widen<T>(rv[u], r);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] += r[j];
-    }
-    row8_store((T*)a.y + (size_t)row[u] * a.ldy + 8 * (size_t)group[u], a.cols - 8 * (int)group[u], v);
-  }
+  row8_store((T*)a.y + (size_t)row * a.ldy + c, n, v);
 }
 
 // ------------------------------------------------------------------ rows of a LayerNorm
@@ -347,49 +338,61 @@ static int launched(const char* who) {
 
 template <typename T> static int dropout_t(const DropoutK& k, hipStream_t s) {
   const uint64_t groups = (uint64_t)k.rows * k.groups;
-  // two groups a thread where there are waves enough for the CUs anyway
-  if (groups >= 256ull * 2 * 1024) hipLaunchKernelGGL((dropout_kernel<T, 2>), dim3((unsigned)((groups + 511) / 512)), dim3(256), 0, s, k);
-  else hipLaunchKernelGGL((dropout_kernel<T, 1>), dim3((unsigned)((groups + 255) / 256)), dim3(256), 0, s, k);
+  hipLaunchKernelGGL((dropout_kernel<T>), dim3((unsigned)((groups + 255) / 256)), dim3(256), 0, s, k);
   return launched("dp_op_dropout");
 }
 
-// f(lanes, chunks) by the width of a row
-template <class F> static void norm_dispatch(int d, F f) {
+// f(lanes, chunks) by the width of a row: few lanes leave few steps of a sum between lanes, few chunks leave registers for rows in flight.  The backward keeps
+// four more vectors of a row than the forward and goes to more lanes earlier.  us of the lines' two sides (bf16, fp32 residual and sum unless said):
+//   forward   65536 x 128 (16, 1) 17.6, (32, 1) 19.9;  65536 x 256 (16, 2) 30.6, (32, 1) 30.8, (64, 1) 35.3;  16384 x 512 (32, 2) 16.9, (64, 1) 17.8, (16, 4) 18.5;
+//             16384 x 768, bf16 sums (64, 2) 20.3, (32, 4) 20.4, (256, 1) 28.2;  8192 x 1152 (256, 1) 19.5, (64, 4) 21.8;  4096 x 2560 (256, 2) 21.8, (512, 1) 22.9;
+//             4096 x 5000, bf16 sums (512, 2) 30.1, (256, 4) 31.5, (1024, 1) 35.0
+//   backward  65536 x 128 (16, 1) 23.8, (32, 1) 29.1;  65536 x 256 (32, 1) 44.2, (16, 2) 46.0, (64, 1) 57.6;  32768 x 320 (64, 1) 29.8, (32, 2) 31.8, (16, 4) 45.9;
+//             16384 x 512 (64, 1) 22.4, (32, 2) 24.9;  8192 x 1024 (64, 2) 25.0, (256, 1) 28.9, (32, 4) 38.4;  8192 x 1152 (256, 1) 25.6, (64, 3) 47.2
+template <bool FORWARD, class F> static void norm_dispatch(int d, F f) {
   using std::integral_constant;
   auto with = [&](auto l, auto nc) { f(l, nc); };
-  if (d <= 128) with(integral_constant<int, 16>(), integral_constant<int, 1>());
-  else if (d <= 256) with(integral_constant<int, 16>(), integral_constant<int, 2>());
-  else if (d <= 512) with(integral_constant<int, 32>(), integral_constant<int, 2>());
-  else if (d <= 1024) with(integral_constant<int, 64>(), integral_constant<int, 2>());
-  else if (d <= 2048) with(integral_constant<int, 256>(), integral_constant<int, 1>());
-  else if (d <= 4096) with(integral_constant<int, 512>(), integral_constant<int, 1>());
-  else with(integral_constant<int, 1024>(), integral_constant<int, 1>());
+  if (d <= 128) return with(integral_constant<int, 16>(), integral_constant<int, 1>());
+  if (d > 512 && d <= 1024) return with(integral_constant<int, 64>(), integral_constant<int, 2>());
+  if (d > 1024 && d <= 2048) return with(integral_constant<int, 256>(), integral_constant<int, 1>());
+  if constexpr (FORWARD) {
+    if (d <= 256) with(integral_constant<int, 16>(), integral_constant<int, 2>());
+    else if (d <= 512) with(integral_constant<int, 32>(), integral_constant<int, 2>());
+    else if (d <= 4096) with(integral_constant<int, 256>(), integral_constant<int, 2>());
+    else with(integral_constant<int, 512>(), integral_constant<int, 2>());
+  } else {
+    if (d <= 256) with(integral_constant<int, 32>(), integral_constant<int, 1>());
+    else if (d <= 512) with(integral_constant<int, 64>(), integral_constant<int, 1>());
+    else if (d <= 4096) with(integral_constant<int, 512>(), integral_constant<int, 1>());
+    else with(integral_constant<int, 1024>(), integral_constant<int, 1>());
+  }
 }
 static int norm_rows_per_workgroup(int d) {
   int per = 1;
-  norm_dispatch(d, [&](auto l, auto) { per = norm_threads<l> / l; });
+  norm_dispatch<false>(d, [&](auto l, auto) { per = norm_threads<l> / l; });
   return per;
 }
 static bool norm_too_many(int rows, int d) {      // a launch has less than 2^32 threads
   long lanes = 1;
-  norm_dispatch(d, [&](auto l, auto) { lanes = l; });
+  norm_dispatch<false>(d, [&](auto l, auto) { lanes = l; });
   return rows * lanes >= (1l << 31);
 }
-// Workgroups of the backward, hence parts to be added afterwards: as many as run at once, two a CU (half the registers of a SIMD each wave), four where a row is
-// one group of columns a lane of 256.  512 / 768 / 1024 of them, us without the sum: 32768 x 640 67 / 81 / 69, 8192 x 640 21 / 23 / 23, 32768 x 320 32 / 38 / 35, 8192 x 1152 28 / 26 / 23.
+// Workgroups of the backward, hence parts to be added afterwards: as many as run at once.  That is two a CU where a lane has two groups of columns (half the
+// registers of a SIMD each wave) and four where it has one; rows within a wave take three, which leave fewer parts.  512 / 768 / 1024 of them, us without the
+// sum: 32768 x 320 29.6 / 27.8 / 28.0, 65536 x 256 43.1 / 42.2 / 43.6, 32768 x 640 67 / 81 / 69, 8192 x 640 21 / 23 / 23, 8192 x 1152 28 / 26 / 23.
 static int norm_bwd_workgroups(int rows, int d) {
   const int per = norm_rows_per_workgroup(d);
-  return std::min((rows + per - 1) / per, d > 1024 && d <= 2048 ? 1024 : 512);
+  return std::min((rows + per - 1) / per, d <= 512 ? 768 : d > 1024 && d <= 2048 ? 1024 : 512);
 }
 template <typename T, typename S> static int norm_fwd_t(const NormK& k, hipStream_t s) {
-  norm_dispatch(k.d, [&](auto l, auto nc) {
+  norm_dispatch<true>(k.d, [&](auto l, auto nc) {
     constexpr int PER = norm_threads<l> / l;
     hipLaunchKernelGGL((norm_fwd_kernel<T, S, l, nc>), dim3((k.rows + PER - 1) / PER), dim3(norm_threads<l>), 0, s, k);
   });
   return launched("dp_op_layernorm_fwd");
 }
 template <typename T, typename S> static int norm_bwd_t(const NormBwdK& k, int workgroups, hipStream_t s) {
-  norm_dispatch(k.d, [&](auto l, auto nc) { hipLaunchKernelGGL((norm_bwd_kernel<T, S, l, nc>), dim3(workgroups), dim3(norm_threads<l>), 0, s, k); });
+  norm_dispatch<false>(k.d, [&](auto l, auto nc) { hipLaunchKernelGGL((norm_bwd_kernel<T, S, l, nc>), dim3(workgroups), dim3(norm_threads<l>), 0, s, k); });
   return launched("dp_op_layernorm_bwd");
 }
 

@@ -56,6 +56,7 @@ struct RelAttnK {
   void* dk; int lddk;
   void* dv; int lddv;
   float* dtable_partial;      // [head][sample and query tile][bucket]
+  float* dtable; int dtable_parts, dtable_add, table_items;      // the gradient, of how many parts a head, and whether it is added to
   int even;
   int qsplits; float* dkv_partial;      // all keys in a workgroup: shares of the queries, and what they leave of dK and dV, [dK, dV][share][key row][column]
   int shares; float* part;      // few queries: shares of the keys, and what they leave: outputs [share][row][column], references and sums [share][row][2]
@@ -758,22 +759,28 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 3 : 2) rel_bwd_dq_bf16_kernel
   if (p.dtable_partial) rel_bucket_sums<4, false>(p, starts, sums, sum_stride, far_sums, second ? -far_sum_lo : far_sum_lo, second ? -far_sum_hi : far_sum_hi, p.dtable_partial + ((size_t)h * p.B * qtiles + (size_t)b * qtiles + qtile) * p.bk.n_buckets);
 }
 
-// dtable[bucket][head] = sum over the parts, in their order: 32 buckets of a head a workgroup, eight shares of the parts.
-__global__ void __launch_bounds__(256) rel_dtable_kernel(const float* __restrict__ partial, int parts, int n_buckets, int H, float* __restrict__ dtable, int accumulate) {
-  __shared__ float meet[8][32];
-  const int h = blockIdx.x, lane = threadIdx.x % 32, share = threadIdx.x / 32, bucket = blockIdx.y * 32 + lane;
+// dtable[bucket][head] = sum over the parts, in their order: 32 buckets of a head a workgroup (item: head, then which 32), eight shares of the parts.  Where a
+// launch for dK and dV follows, its first workgroups do this beside the others; meet: 256 floats of LDS.
+__device__ __forceinline__ void rel_table_sums(const RelAttnK& p, int item, float* meet) {
+  const int n_buckets = p.bk.n_buckets, turns = (n_buckets + 31) / 32, h = item / turns, parts = p.dtable_parts;
+  const int lane = threadIdx.x % 32, share = threadIdx.x / 32, bucket = item % turns * 32 + lane;
+  if (h >= p.H) return;
   float s = 0.f;
   if (bucket < n_buckets) {
 #pragma unroll 8
-    for (int i = share; i < parts; i += 8) s += partial[((size_t)h * parts + i) * n_buckets + bucket];
+    for (int i = share; i < parts; i += 8) s += p.dtable_partial[((size_t)h * parts + i) * n_buckets + bucket];
   }
-  meet[share][lane] = s;
+  meet[threadIdx.x] = s;
   __syncthreads();
   if (share || bucket >= n_buckets) return;
 #pragma unroll
-  for (int w = 1; w < 8; ++w) s += meet[w][lane];
-  float* out = dtable + (size_t)bucket * H + h;
-  *out = accumulate ? *out + s : s;
+  for (int w = 1; w < 8; ++w) s += meet[32 * w + lane];
+  float* out = p.dtable + (size_t)bucket * p.H + h;
+  *out = p.dtable_add ? *out + s : s;
+}
+__global__ void __launch_bounds__(256) rel_dtable_kernel(const RelAttnK p) {
+  __shared__ float meet[256];
+  rel_table_sums(p, blockIdx.x, meet);
 }
 
 // ------------------------------------------------------------------ dK, dV (bf16)
@@ -791,10 +798,12 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(MINW, 
   __shared__ __attribute__((aligned(16))) float dlt_s[2][64];
   extern __shared__ __attribute__((aligned(16))) float rel_lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, l32 = lane & 31;
+  const int ktiles = (p.Nk + 127) / 128, id = (int)blockIdx.x - p.table_items;
+  if (id < 0) return rel_table_sums(p, (int)blockIdx.x, reinterpret_cast<float*>(Qs[0]));
   const bool causal = MINW == 2 && p.causal;
   const int bk_lo = p.bk.lo, bk_hi = p.bk.hi;
   int ktile, bh;
-  rel_block_map(p, blockIdx.x, (p.Nk + 127) / 128, false, ktile, bh);
+  rel_block_map(p, id, ktiles, false, ktile, bh);
   const int b = bh / p.H, h = bh % p.H;
   RelFill<bf16, true, 256> fill;
   fill.request(p, st, h);
@@ -1235,7 +1244,10 @@ __global__ void __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2,
 
 // The query shares' dK and dV, in their order; four columns a thread.
 __global__ void __launch_bounds__(256) rel_dkv_kernel(const RelAttnK p) {
-  const size_t hd = (size_t)p.H * p.dh, rows = (size_t)p.B * p.Nk, at = (blockIdx.x * 256ul + threadIdx.x) * 4, row = at / hd, col = at % hd;
+  __shared__ float meet[256];
+  const size_t hd = (size_t)p.H * p.dh, rows = (size_t)p.B * p.Nk;
+  if ((int)blockIdx.x < p.table_items) return rel_table_sums(p, (int)blockIdx.x, meet);
+  const size_t at = ((blockIdx.x - p.table_items) * 256ul + threadIdx.x) * 4, row = at / hd, col = at % hd;
   if (row >= rows) return;
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
@@ -1520,9 +1532,11 @@ __global__ void __launch_bounds__(256) rel_bwd_dkv_f32_kernel(const RelAttnK p, 
   __shared__ __attribute__((aligned(16))) float meet[REL_F32_MEET<DT>];
   extern __shared__ __attribute__((aligned(16))) float rel_lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, l32 = lane & 31;
+  const int ktiles = (p.Nk + 31) / 32, id = (int)blockIdx.x - p.table_items;
+  if (id < 0) return rel_table_sums(p, (int)blockIdx.x, meet);
   const int bk_lo = p.bk.lo, bk_hi = p.bk.hi;
   int ktile, bh;
-  rel_block_map(p, blockIdx.x, (p.Nk + 31) / 32, false, ktile, bh);
+  rel_block_map(p, id, ktiles, false, ktile, bh);
   const int b = bh / p.H, h = bh % p.H, k0 = ktile * 32, ki = k0 + l32;
   RelFill<float, true, 256> fill;
   fill.request(p, st, h);
@@ -1756,7 +1770,7 @@ static int check_rel(const char* who, int dtype, const RelAttnK& k, const dp_rel
   if (k.dh % grid || k.dh > 96) return set_errorf(DP_EUNSUPPORTED, "%s: d_head must be a multiple of %d, at most 96", who, grid);
   if (k.query0 > (1 << 29) || k.query0 < -(1 << 29) || k.Nq > (1 << 29) || k.Nk > (1 << 29)) return set_errorf(DP_EUNSUPPORTED, "%s: positions beyond 2^29", who);
   const size_t rows = dtype == DP_BF16 ? 128 : 32, tiles = ((size_t)std::max(k.Nq, k.Nk) + rows - 1) / rows * k.B * k.H;
-  if (tiles >= (1u << 24)) return set_errorf(DP_EUNSUPPORTED, "%s: too many tiles for one launch", who);      // (2^32 threads)
+  if (tiles + (size_t)k.H * (REL_MAX_BUCKETS / 32) + 8 >= (1u << 24)) return set_errorf(DP_EUNSUPPORTED, "%s: too many tiles for one launch", who);      // (2^32 threads)
   const int span = k.H * k.dh;
   struct Op { const void* p; int ld, n; const char* name; };
   const Op ops[] = {{k.q, k.ldq, k.Nq, "q"}, {k.k, k.ldk, k.Nk, "k"}, {k.v, k.ldv, k.Nk, "v"}, {k.o, k.ldo, k.Nq, "o"},
@@ -1876,7 +1890,10 @@ int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_h
       all_keys = RelShort<dhp, nw>::BYTES + rel_sum_floats(a.bk, nw) * 4 <= 160 * 1024;
       return DP_OK;
     }));
-  const int parts = B * rel_parts(dtype, all_keys, B, H, Nq);
+  a.dtable = dtable;
+  a.dtable_parts = B * rel_parts(dtype, all_keys, B, H, Nq);
+  a.dtable_add = accumulate != 0;
+  a.table_items = dtable ? (H * ((bias->n_buckets + 31) / 32) + 7) / 8 * 8 : 0;      // workgroups that add the parts of the table's gradient (eights: the others stay on their XCDs)
   const double fl = 4.0 * B * H * (double)Nq * Nk * d_head, by = (dtype == DP_BF16 ? 2.0 : 4.0) * B * H * d_head * (3.0 * Nq + 2.0 * Nk);
   if (dtype == DP_F32) {
     KScope ks(KK_ATTN_F32, 2 * fl, 2 * by, s, Nq, Nk, d_head);
@@ -1886,7 +1903,7 @@ int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_h
       hipLaunchKernelGGL((rel_bwd_dq_f32_kernel<dt, kc>), dim3((unsigned)((Nq + 31) / 32 * B * H)), dim3(256), both, s, a, st);
       DP_TRY(rel_launched());
       DP_TRY((rel_allow_lds<rel_bwd_dkv_f32_kernel<dt, kc>>(REL_F32_MEET<dt> * 4, table)));
-      hipLaunchKernelGGL((rel_bwd_dkv_f32_kernel<dt, kc>), dim3((unsigned)((Nk + 31) / 32 * B * H)), dim3(256), table, s, a, st);
+      hipLaunchKernelGGL((rel_bwd_dkv_f32_kernel<dt, kc>), dim3((unsigned)((Nk + 31) / 32 * B * H) + a.table_items), dim3(256), table, s, a, st);
       return rel_launched();
     }));
   } else if (all_keys) {
@@ -1900,8 +1917,12 @@ int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_h
       return rel_launched();
     }));
     if (a.qsplits > 1) {
-      hipLaunchKernelGGL(rel_dkv_kernel, dim3((unsigned)(((size_t)B * Nk * H * d_head / 4 + 255) / 256)), dim3(256), 0, s, a);
-      DP_TRY(rel_launched());
+      hipLaunchKernelGGL(rel_dkv_kernel, dim3((unsigned)(((size_t)B * Nk * H * d_head / 4 + 255) / 256) + a.table_items), dim3(256), 0, s, a);
+      return rel_launched();
+    }
+    if (dtable) {
+      hipLaunchKernelGGL(rel_dtable_kernel, dim3(a.table_items), dim3(256), 0, s, a);
+      return rel_launched();
     }
   } else {
     const long qblocks = (long)((Nq + 127) / 128) * B * H, kblocks = (long)((Nk + 127) / 128) * B * H;
@@ -1924,18 +1945,15 @@ int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_h
       constexpr int MANY = dhp == 64 ? 3 : 2;
       if (MANY > 2 && many) {
         DP_TRY((rel_allow_lds<rel_bwd_dkv_bf16_kernel<dhp, kc, MANY>>(768 * dhp, table)));
-        hipLaunchKernelGGL((rel_bwd_dkv_bf16_kernel<dhp, kc, MANY>), dim3((unsigned)kblocks), dim3(256), table, s, a, st);
+        hipLaunchKernelGGL((rel_bwd_dkv_bf16_kernel<dhp, kc, MANY>), dim3((unsigned)kblocks + a.table_items), dim3(256), table, s, a, st);
       } else {
         DP_TRY((rel_allow_lds<rel_bwd_dkv_bf16_kernel<dhp, kc, 2>>(512 * dhp, table)));
-        hipLaunchKernelGGL((rel_bwd_dkv_bf16_kernel<dhp, kc, 2>), dim3((unsigned)kblocks), dim3(256), table, s, a, st);
+        hipLaunchKernelGGL((rel_bwd_dkv_bf16_kernel<dhp, kc, 2>), dim3((unsigned)kblocks + a.table_items), dim3(256), table, s, a, st);
       }
       return rel_launched();
     }));
   }
-  if (!dtable) return DP_OK;
-  KScope ks(KK_REDUCE, 0.0, (double)H * parts * bias->n_buckets * 4, s, parts, H, bias->n_buckets);
-  hipLaunchKernelGGL(rel_dtable_kernel, dim3((unsigned)H, (unsigned)(bias->n_buckets + 31) / 32), dim3(256), 0, s, a.dtable_partial, parts, bias->n_buckets, H, dtable, accumulate != 0);
-  return rel_launched();
+  return DP_OK;
 }
 
 }  // extern "C"

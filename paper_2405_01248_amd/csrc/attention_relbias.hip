@@ -6,13 +6,12 @@
 // The bias costs these loops no vector instruction.  What the accumulators of the scores are cleared with otherwise is the bias over the scale:
 //   - bias over distance lies in LDS (fp32) from the last distance at which the bucket still changes to the other one, and 96 distances
 //     of the end buckets beyond either, as far as a tile that touches the middle reaches; four neighbouring accumulator registers are four neighbouring entries;
-//   - a tile of 64 keys and 32 queries outside of the middle lies in one bucket: its accumulators begin with a constant.
-// The table's gradient, the sum of dS over the pairs of a bucket: in the middle a wave lays dS down in LDS (16 queries x 32 keys at a time), adds along
-// the diagonals, a lane each, and adds the result to its sums over distances in LDS.  Beyond the middle each lane adds to one sum per
-// side.  The sums over distances become sums over buckets at the end of the workgroup, and a second kernel adds those of all samples and query tiles; every
-// sum in a fixed order, so that the result is the same bits every time.  8 x 10 heads of 1024, causal, dQ: 134 us with an atomic addition in LDS for each
-// element of dS (about 150 cycles an instruction), 66 along the diagonals of 32 x 32 blocks; with 16 queries at a time three workgroups fit a CU (without the
-// mask 83 -> 58 us; 64 x 4096 370 -> 296).
+//   - a tile of 64 keys and 32 queries outside of the middle lies in one bucket: one number is its bias, for the accumulators or for the exponent.
+// The table's gradient, the sum of dS over the pairs of a bucket: in the middle a wave adds its blocks of dS along their diagonals in registers (rel_diagonals),
+// two vector additions an element, and keeps one sum a distance in LDS; beyond the middle each lane adds to one sum per side.  The sums over distances become
+// sums over buckets at the end of the workgroup, and the first workgroups of the next launch add those of all samples and query tiles; every sum in a fixed order, so
+// that the result is the same bits every time.  8 x 10 heads of 1024, dQ with this, causal: 134 us with an atomic addition in LDS for each element of dS
+// (about 150 cycles an instruction), 44 laid down in LDS and added along the diagonals from there, 38 in registers (without the mask 58 and 47).
 #include "dp_attention_tile.h"
 #include "dp_device.h"
 #include "dp_errors.h"
@@ -141,7 +140,7 @@ __device__ __forceinline__ uint32_t rel_slice_bytes(int n, int ld, int dh) { ret
 // ------------------------------------------------------------------ forward (bf16)
 // 128 queries a workgroup, keys in tiles of 64, two LDS stages; online softmax with a reference point that moves when the sum outgrows it (see
 // attn_fwd_bf16_kernel).  8 x 5 heads of 4096 tokens 192 us, 8 x 10 of 1024 31 (without a bias 188 and 29); with the bias of the far tiles in the accumulators, sixteen moves a
-// block, 203 and 33.  A query that sees no key keeps the reference -inf and the sum 0: zeros, and lse = -inf.
+// block, 203 and 33.  Bound by the vector work of the softmax between the products (the products of the former alone are 153 us at the rate of a large one).  A query that sees no key keeps the reference -inf and the sum 0: zeros, and lse = -inf.
 template <int DHP, int KC, int MINW>
 __global__ void __launch_bounds__(256, MINW) rel_fwd_bf16_kernel(const RelAttnK p, const RelStarts st) {
   constexpr int DT = DHP / 32, BQ = 128, TILE = 64 * DHP;
@@ -315,7 +314,8 @@ __device__ __forceinline__ void rel_store_o(const RelAttnK& p, const f32x4& o, f
 // ------------------------------------------------------------------ forward of few queries (bf16)
 // A workgroup has 32 queries of a head and one share of its tiles of 64 keys, each wave every fourth tile of them: K straight from memory into the
 // operand's registers, V through an LDS tile of the wave's own, both requested a tile ahead; nothing waits at a barrier before the waves' sums meet at the end.
-// Bound by reading K and V, of which a wave keeps a tile each in flight.  With several shares each leaves its unscaled output, reference and sum,
+// Bound by reading K and V, of which a wave keeps a tile each in flight: 16 x 12 heads, one query, 4000 keys 36 us (5.5 TB/s), keys of different lengths up to
+// that 24 (4.1, the longest ends last), and 4 to 5 for joining.  Shares that go to as many tiles each, whatever the sample's length, 30.  With several shares each leaves its unscaled output, reference and sum,
 // and rel_join_kernel adds them in their order.
 template <int DHP, int KC>
 __global__ void __launch_bounds__(256, DHP == 64 ? 2 : 1) rel_fwd_few_bf16_kernel(const RelAttnK p, const RelStarts st) {
@@ -515,6 +515,9 @@ __global__ void __launch_bounds__(256) rel_join_kernel(const RelAttnK p) {
 }
 
 // ------------------------------------------------------------------ dQ and the table's gradient (bf16)
+// 128 queries a workgroup, keys in tiles of 64, two LDS stages; S and dP = dO V^T with a query a lane, dS = P (dP - delta), dQ += dS K; delta = rowsum(dO O) goes
+// to the workspace for dK / dV.  8 x 10 heads of 1024 47 us, 8 x 5 of 4096 272, 8 x 10 of 1024 causal 38: three products a block (8 x 5 of 4096: 258 GF, 229 us at a
+// large product's rate) and some ten vector instructions an element between them, of which the diagonals are two.
 __device__ __forceinline__ bf16x8 rel_turned(bf16x8 v, bool turn) {      // -v
   u32x4 w = __builtin_bit_cast(u32x4, v);
 #pragma unroll
@@ -786,7 +789,8 @@ __global__ void __launch_bounds__(256) rel_dtable_kernel(const RelAttnK p) {
 // ------------------------------------------------------------------ dK, dV (bf16)
 // Each wave owns 32 keys and walks the queries in tiles of 64, from the first that sees one of the workgroup's keys (see attn_bwd_dkv_bf16_kernel).  The
 // bias is the addend of the exponent here, and lse what the scores begin with.  MINW: waves per SIMD, exactly; three have no registers for K, which they read from
-// LDS again for every tile, nor for the causal mask: 8 x 10 heads of 1024 72 -> 61 us, 8 x 5 of 4096 372 -> 346, 16 x 16 of 300 33 -> 27.
+// LDS again for every tile, nor for the causal mask: 8 x 10 heads of 1024 72 -> 55 us, 8 x 5 of 4096 372 -> 343, 16 x 16 of 300 33 -> 27.  Four products a block bound
+// it: 8 x 5 of 4096 are 344 GF, 305 us at a large product's rate.
 template <int DHP, int KC, int MINW>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(MINW, MINW))) rel_bwd_dkv_bf16_kernel(const RelAttnK p, const RelStarts st) {
   constexpr int DT = DHP / 32, TILE = 64 * DHP;
@@ -957,7 +961,8 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(MINW, 
 // ------------------------------------------------------------------ dQ, dK, dV and the table's gradient at once (bf16, at most 32 NW keys)
 // A workgroup has all keys of its (sample, head), 32 per wave, and walks the queries of its share in tiles of 64 (see attn_bwd_short_bf16_kernel): scores, dP and
 // exponentials once instead of twice.  Per tile every wave adds to its keys' dK and dV, adds its dS along the diagonals and leaves it in LDS; behind a barrier the
-// dQ of the tile is formed from it and the keys, while the next tile's delta is.  The second sixteen keys of a wave work with -V, hence -delta and
+// dQ of the tile is formed from it and the keys, while the next tile's delta is.  64 x 12 heads of 77 tokens 31 us (42 by the two kernels above), 32 x 16 of 256 and
+// width 72 75 (101); the chain of a tile, two barriers long, bounds it.  The second sixteen keys of a wave work with -V, hence -delta and
 // -dS (see rel_bwd_dq_bf16_kernel).
 template <int DHP, int NW> struct RelShort {
   static constexpr int TILE = 64 * DHP, K = 32 * NW * DHP, DS = 32 * NW * 64;                            // elements
@@ -1272,7 +1277,9 @@ __global__ void __launch_bounds__(256) rel_dkv_kernel(const RelAttnK p) {
 // which makes register r of the scores the B operand as it stands and the A operand a row of which 32 lanes read neighbouring columns.  So nothing goes
 // through LDS on its way in: an instruction takes 64 cycles, several loads' time.
 // A workgroup has 32 queries (forward, dQ) or 32 keys (dK / dV) of a head; its four waves take every fourth tile of 32 of the other side and
-// add what they have in LDS at the end, in their order.  Bound by the matrix instruction where there is work for all CUs, else by the chain of tiles.
+// add what they have in LDS at the end, in their order.  Bound by the matrix instruction where there is work for all CUs, else by the chain of tiles: 2 x 8 heads of
+// 1024, width 64, forward 59 us (73 TF/s of 153), dQ 83, dK / dV 109; 2 x 4 of 257, width 40, 17 and 20.  Rows a tile ahead in registers, where there are any
+// (widths to 64): 102 -> 90 and 127 -> 118 us.
 __device__ __forceinline__ f32x16 mfma_f32(float a, float b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0); }
 
 template <int KC> struct RelRows {      // a lane's 16-byte pieces of one row

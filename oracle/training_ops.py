@@ -87,7 +87,7 @@ def buckets(nq, nk, query0, n_buckets, max_distance, bidirectional):
 def _logits(q, k, scale, table, bk, causal, query0, key_len):
     s = scale * (q @ np.swapaxes(k, -1, -2))
     if table is not None:
-        s = s + np.moveaxis(table[bk], -1, 0)[None]
+        s = s + np.moveaxis(np.where(table <= -65536.0, -np.inf, table)[bk], -1, 0)[None]      # entries from there on mask their pairs
     nq, nk = s.shape[-2:]
     j = np.arange(nk)
     if causal:

@@ -86,7 +86,14 @@ __device__ __forceinline__ void rel_fill_starts(const RelBucketsK& r, const RelS
 }
 __host__ __device__ __forceinline__ int rel_entries(const RelBucketsK& r) { return r.hi - r.lo + 1 + 2 * REL_MARGIN; }
 __host__ __device__ __forceinline__ int rel_table_floats(const RelBucketsK& r) { return (rel_entries(r) + 3) / 4 * 4; }
-__device__ __forceinline__ int rel_keys(const RelAttnK& p, int b) { return p.key_len ? max(0, min(p.key_len[b], p.Nk)) : p.Nk; }
+// Keys of a sample that any query of the call sees: what lies behind is not read, so that a cache may be longer than what it holds.
+__device__ __forceinline__ int rel_keys(const RelAttnK& p, int b) {
+  const int seen = p.causal ? max(0, min(p.Nk, p.query0 + p.Nq)) : p.Nk;
+  return p.key_len ? max(0, min(p.key_len[b], seen)) : seen;
+}
+// An entry of the table, times a factor.  At -65536 fp32 sums of score and entry are 1/256 apart; from there on an entry masks, as -infinity does, where a
+// sum would have kept little of the score (and lse, from which the backward forms the probabilities again, little of the logarithm).
+__device__ __forceinline__ float rel_entry(float v, float factor) { return v <= -65536.f ? -INFINITY : v * factor; }
 
 // Bias of head h by distance, times a factor.  Entry e is distance lo - margin + e, or, REVERSED, hi + margin - e.  In two steps, so that the table's
 // loads are on their way beside the first tiles': what a thread has of the first two rounds is requested first and stored behind the tiles' copies.
@@ -108,9 +115,9 @@ template <typename T, bool REVERSED, int THREADS> struct RelFill {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int e = threadIdx.x + i * THREADS;
-      if (e < n) tab[e] = to_f<T>(v[i]) * factor;
+      if (e < n) tab[e] = rel_entry(to_f<T>(v[i]), factor);
     }
-    for (int e = threadIdx.x + 2 * THREADS; e < n; e += THREADS) tab[e] = to_f<T>(entry(p, st, h, e)) * factor;
+    for (int e = threadIdx.x + 2 * THREADS; e < n; e += THREADS) tab[e] = rel_entry(to_f<T>(entry(p, st, h, e)), factor);
   }
 };
 // The same in all lanes, hence in a scalar register

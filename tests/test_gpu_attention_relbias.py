@@ -45,12 +45,13 @@ def _close(got, want, bound, what):
     assert (err <= bound).all(), (what, float((err / np.maximum(bound, 1e-300)).max()), np.unravel_index((err - bound).argmax(), err.shape))
 
 
-def _check(dtype, B, H, nq, nk, d, causal, bidirectional, n_buckets, distance, query0, lens, gain=1.0, pad=0, forbid=(), garbage={}, workspace=True, seed=0):
+def _check(dtype, B, H, nq, nk, d, causal, bidirectional, n_buckets, distance, query0, lens, gain=1.0, pad=0, forbid=(), garbage={}, workspace=True, seed=0, forbidden=-float("inf"), unseen=False):
     import torch
     from paper_2405_01248_amd import binding as K
-    t, dev, val, table, tv = _make(dtype, B, H, nq, nk, d, seed + nq * 31 + nk, n_buckets, lens, gain, pad)
+    held = [query0 + nq] * B if unseen else lens      # (unseen: NaN in what the causal mask hides from all queries)
+    t, dev, val, table, tv = _make(dtype, B, H, nq, nk, d, seed + nq * 31 + nk, n_buckets, held, gain, pad)
     for bk in forbid:
-        table[bk] = -float("inf")
+        table[bk] = forbidden
         tv[bk] = -np.inf
     for bk, x in garbage.items():      # buckets whose pairs are all masked
         table[bk] = x
@@ -194,6 +195,22 @@ def test_strides_large_logits_and_forbidden_buckets(dtype):
     _check(dtype, 1, 2, 400, 400, 64, False, True, 32, 128, 0, None, gain=12.0)
     _check(dtype, 1, 2, 260, 300, 64, False, True, 32, 128, 0, None, forbid=(0, 3, 15, 31))      # -infinity: near, middle and both ends
     _check(dtype, 1, 2, 70, 70, 64, True, False, 8, 16, 0, [70], forbid=range(8))               # nothing is visible at all
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("value", [-65536.0, -1e9, "lowest"])
+def test_entries_that_mask_as_infinity_does(dtype, value):
+    import torch
+    lowest = torch.finfo(torch.float32 if dtype == "f32" else torch.bfloat16).min
+    value = lowest if value == "lowest" else value
+    _check(dtype, 1, 2, 260, 300, 64, False, True, 32, 128, 0, None, forbid=(0, 3, 15, 31), forbidden=value)
+    _check(dtype, 2, 1, 150, 500, 40, False, True, 32, 128, 0, [500, 60], forbid=range(32), forbidden=value)      # nothing is visible at all
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("nq,nk,query0", [(1, 700, 331), (40, 1000, 500), (140, 200, 0), (300, 700, 77), (64, 256, -20), (5, 300, -5)])
+def test_what_the_causal_mask_hides_from_all_queries_is_not_read(dtype, nq, nk, query0):
+    _check(dtype, 2, 2, nq, nk, 64, True, False, 32, 128, query0, None, unseen=True)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])

@@ -81,3 +81,16 @@ def test_attention_gradients_against_differences(causal, query0, key_len):
         assert (o[:, :, :2] == 0).all() and np.isneginf(lse[:, :, :2]).all()
     if key_len == [5, 0]:
         assert (o[1] == 0).all() and (got[1][0, :, 5:] == 0).all() and (got[1][1] == 0).all()
+
+
+def test_entries_of_minus_65536_and_less_mask():
+    r = np.random.default_rng(3)
+    q, k, v = (r.normal(size=(1, 1, 4, 3)) for _ in range(3))
+    bk = T.buckets(4, 4, 0, 4, 8, True)
+    table = r.normal(size=(4, 1))
+    for x in (-65536.0, -1e30, -np.inf):
+        table[3] = x
+        o, lse = T.attention_relbias_fwd(q, k, v, 0.5, table, bk)
+        s = np.where(bk == 3, -np.inf, 0.5 * q[0, 0] @ k[0, 0].T + table[bk][..., 0])
+        w = np.exp(s) / np.exp(s).sum(-1, keepdims=True)
+        np.testing.assert_allclose(o[0, 0], w @ v[0, 0], rtol=1e-13)

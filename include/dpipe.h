@@ -481,7 +481,8 @@ int dp_op_attention_bwd(int dtype, int B, int H, int Nq, int Nk, int d_head, flo
  * d_head at most 96; d_head and row strides multiples of 8 (bf16) or 4 (fp32); scale within [1e-6, 1e6]; each operand's rows of one sample
  * below 2 GiB; pointers 16-byte aligned (key_len 4).  Outputs may not overlap inputs.
  * workspace: dp_op_attention_relbias_workspace_bytes bytes, 256-byte aligned, needed by the backward; the forward uses it where it splits the keys of few
- * queries, and runs without it (NULL) unsplit.  Calls that may overlap need workspaces of their own. */
+ * queries, and runs without it (NULL) unsplit.  Fewer samples, queries or keys (heads, width and buckets being the same) need no more.  Calls that may overlap
+ * need workspaces of their own. */
 typedef struct {
   const void* table;
   int n_buckets, max_distance, bidirectional, query0;

@@ -57,7 +57,8 @@ struct RelAttnK {
   float* dtable_partial;      // [head][sample and query tile][bucket]
   float* dtable; int dtable_parts, dtable_add, table_items;      // the gradient, of how many parts a head, and whether it is added to
   int even;
-  int qsplits; float* dkv_partial;      // all keys in a workgroup: shares of the queries, and what they leave of dK and dV, [dK, dV][share][key row][column]
+  int qsplits; float* dkv_partial;      // shares of the queries, and what they leave of dK and dV, [dK, dV][share][key row][column]
+  int ksplits; float* dq_partial;       // shares of the keys, and what they leave of dQ, [share][query row][column]
   int shares; float* part;      // few queries: shares of the keys, and what they leave: outputs [share][row][column], references and sums [share][row][2]
   RelBucketsK bk;
 };
@@ -524,7 +525,8 @@ __global__ void __launch_bounds__(256) rel_join_kernel(const RelAttnK p) {
 // ------------------------------------------------------------------ dQ and the table's gradient (bf16)
 // 128 queries a workgroup, keys in tiles of 64, two LDS stages; S and dP = dO V^T with a query a lane, dS = P (dP - delta), dQ += dS K; delta = rowsum(dO O) goes
 // to the workspace for dK / dV.  8 x 10 heads of 1024 47 us, 8 x 5 of 4096 272, 8 x 10 of 1024 causal 38: three products a block (8 x 5 of 4096: 258 GF, 229 us at a
-// large product's rate) and some ten vector instructions an element between them, of which the diagonals are two.
+// large product's rate) and some ten vector instructions an element between them, of which the diagonals are two.  SHARES: a workgroup has one of ksplits shares of
+// its key tiles and leaves an fp32 sum (rel_grad_shares has what it gives).
 __device__ __forceinline__ bf16x8 rel_turned(bf16x8 v, bool turn) {      // -v
   u32x4 w = __builtin_bit_cast(u32x4, v);
 #pragma unroll
@@ -602,7 +604,7 @@ __device__ __forceinline__ void rel_bucket_sums(const RelAttnK& p, const uint16_
   }
 }
 
-template <int DHP, int KC>
+template <int DHP, int KC, bool SHARES>
 __global__ void __launch_bounds__(256, DHP == 64 ? 3 : 2) rel_bwd_dq_bf16_kernel(const RelAttnK p, const RelStarts st) {
   constexpr int DT = DHP / 32, TILE = 64 * DHP;
   __shared__ __attribute__((aligned(1024))) bf16 Ks[2][TILE];
@@ -612,8 +614,9 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 3 : 2) rel_bwd_dq_bf16_kernel
   extern __shared__ __attribute__((aligned(16))) float rel_lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, l32 = lane & 31;
   const int qtiles = (p.Nq + 127) / 128, entries = rel_entries(p.bk), bk_lo = p.bk.lo, bk_hi = p.bk.hi;
+  const int all = qtiles * p.B * p.H, share = SHARES ? (int)blockIdx.x / all : 0;
   int qtile, bh;
-  rel_block_map(p, blockIdx.x, qtiles, true, qtile, bh);
+  rel_block_map(p, SHARES ? (int)blockIdx.x % all : (int)blockIdx.x, qtiles, true, qtile, bh);
   const int b = bh / p.H, h = bh % p.H;
   RelFill<bf16, false, 256> fill;
   fill.request(p, st, h);
@@ -623,7 +626,8 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 3 : 2) rel_bwd_dq_bf16_kernel
   const int keys = __builtin_amdgcn_readfirstlane(rel_keys(p, b));
   const int lim = p.causal ? min(keys, pos + 1) : keys, lim_all = p.causal ? min(keys, pos0 + 1) : keys, lim_wave = p.causal ? min(keys, pos0 + 32) : keys;
   const int lim_any = p.causal ? min(keys, p.query0 + min(p.Nq, qtile * 128 + 128)) : keys;
-  const int nkt = __builtin_amdgcn_readfirstlane(lim_any > 0 ? (lim_any + 63) / 64 : 0);
+  const int tiles = __builtin_amdgcn_readfirstlane(lim_any > 0 ? (lim_any + 63) / 64 : 0);
+  const int kt0 = SHARES ? (int)((long)tiles * share / p.ksplits) : 0, nkt = SHARES ? (int)((long)tiles * (share + 1) / p.ksplits) : tiles;
   const u32x4 kr = make_raw_rsrc((const bf16*)p.k + (size_t)b * p.Nk * p.ldk + h * p.dh, rel_slice_bytes(keys, p.ldk, p.dh));
   const u32x4 vr = make_raw_rsrc((const bf16*)p.v + (size_t)b * p.Nk * p.ldv + h * p.dh, rel_slice_bytes(keys, p.ldv, p.dh));
   const bf16* qrow = (const bf16*)p.q + ((size_t)b * p.Nq + qi) * p.ldq + h * p.dh;
@@ -634,9 +638,9 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 3 : 2) rel_bwd_dq_bf16_kernel
   AttnTileCopy<DHP> ck, cv;
   ck.init(wave, lane, p.ldk, p.dh);
   cv.init(wave, lane, p.ldv, p.dh);
-  if (nkt > 0) {
-    ck.issue(kr, 0, p.ldk, Ks[0], wave);
-    cv.issue(vr, 0, p.ldv, Vs[0], wave);
+  if (kt0 < nkt) {
+    ck.issue(kr, kt0 * 64, p.ldk, Ks[0], wave);
+    cv.issue(vr, kt0 * 64, p.ldv, Vs[0], wave);
   }
   fill.store(p, st, h, rel_lds, p.inv_scale);
   float* sums = rel_lds + rel_table_floats(p.bk);
@@ -675,7 +679,7 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 3 : 2) rel_bwd_dq_bf16_kernel
       for (int u = 0; u < 8; ++u) dlt = fmaf((float)of[u], (float)dof[c][u], dlt);
     }
     dlt = reduce_halves(dlt, AddOp());
-    if (qok && g == 0) p.delta[sidx] = second ? -dlt : dlt;
+    if (qok && g == 0 && share == 0) p.delta[sidx] = second ? -dlt : dlt;
   }
   f32x16 ndelta;
 #pragma unroll
@@ -749,24 +753,32 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 3 : 2) rel_bwd_dq_bf16_kernel
     wait_vmcnt<0>();
     __syncthreads();
   };
-  two_stages(0, nkt, tile);
+  two_stages(kt0, nkt, tile);
   if (carry_at >= 0) mine[tab + carry_at] = carry;
   if (qok) {
     bf16* ob = (bf16*)p.dq + ((size_t)b * p.Nq + qi) * p.lddq + h * p.dh;
+    float* of = SHARES ? p.dq_partial + (((size_t)share * p.B + b) * p.Nq + qi) * ((size_t)p.H * p.dh) + h * p.dh : nullptr;
 #pragma unroll
     for (int i = 0; i < DT; ++i)
 #pragma unroll
       for (int r4 = 0; r4 < 4; ++r4) {
         const int col = 32 * i + 8 * r4 + 4 * g;
         if (col < p.dh) {
+          f32x4 v;
           bf16x4 o;
 #pragma unroll
-          for (int u = 0; u < 4; ++u) o[u] = (bf16)(acc[i][4 * r4 + u] * (second ? -p.scale : p.scale));
+          for (int u = 0; u < 4; ++u) v[u] = acc[i][4 * r4 + u] * (second ? -p.scale : p.scale);
+          if (SHARES) {
+            *reinterpret_cast<f32x4*>(of + col) = v;
+            continue;
+          }
+#pragma unroll
+          for (int u = 0; u < 4; ++u) o[u] = (bf16)v[u];
           *reinterpret_cast<bf16x4*>(ob + col) = o;
         }
       }
   }
-  if (p.dtable_partial) rel_bucket_sums<4, false>(p, starts, sums, sum_stride, far_sums, second ? -far_sum_lo : far_sum_lo, second ? -far_sum_hi : far_sum_hi, p.dtable_partial + ((size_t)h * p.B * qtiles + (size_t)b * qtiles + qtile) * p.bk.n_buckets);
+  if (p.dtable_partial) rel_bucket_sums<4, false>(p, starts, sums, sum_stride, far_sums, second ? -far_sum_lo : far_sum_lo, second ? -far_sum_hi : far_sum_hi, p.dtable_partial + (((size_t)h * p.B + b) * qtiles * (SHARES ? p.ksplits : 1) + (SHARES ? share * qtiles : 0) + qtile) * p.bk.n_buckets);
 }
 
 // dtable[bucket][head] = sum over the parts, in their order: 32 buckets of a head a workgroup (item: head, then which 32), eight shares of the parts.  Where a
@@ -793,12 +805,43 @@ __global__ void __launch_bounds__(256) rel_dtable_kernel(const RelAttnK p) {
   rel_table_sums(p, blockIdx.x, meet);
 }
 
+// A wave's dK and dV (lane: key ki): fp32 parts of a query share, or the result; zeros for keys past the sample's length.
+template <int DT>
+__device__ __forceinline__ void rel_store_dkv(const RelAttnK& p, const f32x16 (&dkacc)[DT], const f32x16 (&dvacc)[DT], float dk_scale, int qs, int b, int h, int ki, bool kok, int g) {
+  if (ki >= p.Nk) return;
+  const size_t hd = (size_t)p.H * p.dh, rows = (size_t)p.B * p.Nk, row = (size_t)b * p.Nk + ki;
+#pragma unroll
+  for (int i = 0; i < DT; ++i)
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4) {
+      const int col = 32 * i + 8 * r4 + 4 * g;
+      if (col >= p.dh) continue;
+      f32x4 k, v;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        k[u] = kok ? dkacc[i][4 * r4 + u] * dk_scale : 0.f;
+        v[u] = kok ? dvacc[i][4 * r4 + u] : 0.f;
+      }
+      if (p.qsplits > 1) {
+        float* pk = p.dkv_partial + (qs * rows + row) * hd + h * p.dh + col;
+        *reinterpret_cast<f32x4*>(pk) = k;
+        *reinterpret_cast<f32x4*>(pk + p.qsplits * rows * hd) = v;
+      } else {
+        bf16x4 k4, v4;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) { k4[u] = (bf16)k[u]; v4[u] = (bf16)v[u]; }
+        *reinterpret_cast<bf16x4*>((bf16*)p.dk + row * p.lddk + h * p.dh + col) = k4;
+        *reinterpret_cast<bf16x4*>((bf16*)p.dv + row * p.lddv + h * p.dh + col) = v4;
+      }
+    }
+}
+
 // ------------------------------------------------------------------ dK, dV (bf16)
 // Each wave owns 32 keys and walks the queries in tiles of 64, from the first that sees one of the workgroup's keys (see attn_bwd_dkv_bf16_kernel).  The
 // bias is the addend of the exponent here, and lse what the scores begin with.  MINW: waves per SIMD, exactly; three have no registers for K, which they read from
 // LDS again for every tile, nor for the causal mask: 8 x 10 heads of 1024 72 -> 55 us, 8 x 5 of 4096 372 -> 343, 16 x 16 of 300 33 -> 27.  Four products a block bound
-// it: 8 x 5 of 4096 are 344 GF, 305 us at a large product's rate.
-template <int DHP, int KC, int MINW>
+// it: 8 x 5 of 4096 are 344 GF, 305 us at a large product's rate.  SHARES: one of qsplits shares of the query tiles, as above.
+template <int DHP, int KC, int MINW, bool SHARES>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(MINW, MINW))) rel_bwd_dkv_bf16_kernel(const RelAttnK p, const RelStarts st) {
   constexpr int DT = DHP / 32, TILE = 64 * DHP;
   __shared__ __attribute__((aligned(1024))) bf16 Qs[2][TILE];
@@ -813,8 +856,9 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(MINW, 
   if (id < 0) return rel_table_sums(p, (int)blockIdx.x, reinterpret_cast<float*>(Qs[0]));
   const bool causal = MINW == 2 && p.causal;
   const int bk_lo = p.bk.lo, bk_hi = p.bk.hi;
+  const int all = ktiles * p.B * p.H, share = SHARES ? id / all : 0;
   int ktile, bh;
-  rel_block_map(p, id, ktiles, false, ktile, bh);
+  rel_block_map(p, SHARES ? id % all : id, ktiles, false, ktile, bh);
   const int b = bh / p.H, h = bh % p.H;
   RelFill<bf16, true, 256> fill;
   fill.request(p, st, h);
@@ -828,8 +872,9 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(MINW, 
   const float* lse_b = p.lse + ((size_t)b * p.H + h) * p.Nq;
   const float* dlt_b = p.delta + ((size_t)b * p.H + h) * p.Nq;
 
-  const int nqt = __builtin_amdgcn_readfirstlane(ktile * 128 < keys ? (p.Nq + 63) / 64 : 0);      // (no query sees keys past the sample's length)
-  const int qt0 = causal ? max(0, ktile * 128 - p.query0) / 64 : 0;
+  const int tiles = __builtin_amdgcn_readfirstlane(ktile * 128 < keys ? (p.Nq + 63) / 64 : 0);      // (no query sees keys past the sample's length)
+  const int seen = causal ? max(0, ktile * 128 - p.query0) / 64 : 0, ahead = max(0, tiles - seen);
+  const int qt0 = SHARES ? seen + (int)((long)ahead * share / p.qsplits) : seen, nqt = SHARES ? seen + (int)((long)ahead * (share + 1) / p.qsplits) : tiles;
   AttnFragOff<DHP, KC> fo;
   fo.init(lane);
   AttnTileCopy<DHP> cq, cd;
@@ -944,25 +989,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(MINW, 
     __syncthreads();
   };
   two_stages(qt0, nqt, tile);
-  if (ki >= p.Nk) return;
-  bf16* dkb = (bf16*)p.dk + ((size_t)b * p.Nk + ki) * p.lddk + h * p.dh;
-  bf16* dvb = (bf16*)p.dv + ((size_t)b * p.Nk + ki) * p.lddv + h * p.dh;
-#pragma unroll
-  for (int i = 0; i < DT; ++i)
-#pragma unroll
-    for (int r4 = 0; r4 < 4; ++r4) {
-      const int col = 32 * i + 8 * r4 + 4 * g;
-      if (col < p.dh) {
-        bf16x4 ok_, ov;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          ok_[u] = (bf16)(kok ? dkacc[i][4 * r4 + u] * p.scale : 0.f);
-          ov[u] = (bf16)(kok ? dvacc[i][4 * r4 + u] : 0.f);
-        }
-        *reinterpret_cast<bf16x4*>(dkb + col) = ok_;
-        *reinterpret_cast<bf16x4*>(dvb + col) = ov;
-      }
-    }
+  rel_store_dkv<DT>(p, dkacc, dvacc, p.scale, share, b, h, ki, kok, g);
 }
 
 // ------------------------------------------------------------------ dQ, dK, dV and the table's gradient at once (bf16, at most 32 NW keys)
@@ -976,37 +1003,6 @@ template <int DHP, int NW> struct RelShort {
   static_assert(K <= 2 * TILE + DS, "V passes through the second stage and dS");
   static constexpr int BYTES = (K + 4 * TILE + DS) * (int)sizeof(bf16) + (3 * 64 + 2 * NW + REL_STARTS / 2) * (int)sizeof(float);
 };
-
-// A wave's dK and dV (lane: key ki): fp32 parts of a query share, or the result; zeros for keys past the sample's length.
-template <int DT>
-__device__ __forceinline__ void rel_store_dkv(const RelAttnK& p, const f32x16 (&dkacc)[DT], const f32x16 (&dvacc)[DT], float dk_scale, int qs, int b, int h, int ki, bool kok, int g) {
-  if (ki >= p.Nk) return;
-  const size_t hd = (size_t)p.H * p.dh, rows = (size_t)p.B * p.Nk, row = (size_t)b * p.Nk + ki;
-#pragma unroll
-  for (int i = 0; i < DT; ++i)
-#pragma unroll
-    for (int r4 = 0; r4 < 4; ++r4) {
-      const int col = 32 * i + 8 * r4 + 4 * g;
-      if (col >= p.dh) continue;
-      f32x4 k, v;
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        k[u] = kok ? dkacc[i][4 * r4 + u] * dk_scale : 0.f;
-        v[u] = kok ? dvacc[i][4 * r4 + u] : 0.f;
-      }
-      if (p.qsplits > 1) {
-        float* pk = p.dkv_partial + (qs * rows + row) * hd + h * p.dh + col;
-        *reinterpret_cast<f32x4*>(pk) = k;
-        *reinterpret_cast<f32x4*>(pk + p.qsplits * rows * hd) = v;
-      } else {
-        bf16x4 k4, v4;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) { k4[u] = (bf16)k[u]; v4[u] = (bf16)v[u]; }
-        *reinterpret_cast<bf16x4*>((bf16*)p.dk + row * p.lddk + h * p.dh + col) = k4;
-        *reinterpret_cast<bf16x4*>((bf16*)p.dv + row * p.lddv + h * p.dh + col) = v4;
-      }
-    }
-}
 
 template <int DHP, int KC, int NW>
 __global__ void __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) rel_bwd_short_bf16_kernel(const RelAttnK p, const RelStarts st) {
@@ -1254,28 +1250,37 @@ __global__ void __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2,
                               p.dtable_partial + ((size_t)h * p.B * p.qsplits + (size_t)b * p.qsplits + qs) * p.bk.n_buckets);
 }
 
-// The query shares' dK and dV, in their order; four columns a thread.
-__global__ void __launch_bounds__(256) rel_dkv_kernel(const RelAttnK p) {
-  __shared__ float meet[256];
-  const size_t hd = (size_t)p.H * p.dh, rows = (size_t)p.B * p.Nk;
-  if ((int)blockIdx.x < p.table_items) return rel_table_sums(p, (int)blockIdx.x, meet);
-  const size_t at = ((blockIdx.x - p.table_items) * 256ul + threadIdx.x) * 4, row = at / hd, col = at % hd;
-  if (row >= rows) return;
-#pragma unroll
-  for (int which = 0; which < 2; ++which) {
-    const float* part = p.dkv_partial + which * p.qsplits * rows * hd + at;
-    f32x4 s = *reinterpret_cast<const f32x4*>(part);
+// What the shares leave of dQ, and of dK and dV, added in their order; four columns a thread.
+__device__ __forceinline__ void rel_join_rows(const float* part, int shares, size_t rows, int cols, size_t at, bf16* out, int ld) {
+  const size_t row = at / cols, col = at % cols;
+  f32x4 s = *reinterpret_cast<const f32x4*>(part + at);
 #pragma unroll 4
-    for (int q = 1; q < p.qsplits; ++q) {
-      const f32x4 v = *reinterpret_cast<const f32x4*>(part + q * rows * hd);
+  for (int q = 1; q < shares; ++q) {
+    const f32x4 v = *reinterpret_cast<const f32x4*>(part + q * rows * cols + at);
 #pragma unroll
-      for (int u = 0; u < 4; ++u) s[u] += v[u];
-    }
-    bf16x4 o;
-#pragma unroll
-    for (int u = 0; u < 4; ++u) o[u] = (bf16)s[u];
-    *reinterpret_cast<bf16x4*>((bf16*)(which ? p.dv : p.dk) + row * (which ? p.lddv : p.lddk) + col) = o;
+    for (int u = 0; u < 4; ++u) s[u] += v[u];
   }
+  bf16x4 o;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) o[u] = (bf16)s[u];
+  *reinterpret_cast<bf16x4*>(out + row * ld + col) = o;
+}
+static size_t rel_join_workgroups(int B, int N, int H, int d_head) { return ((size_t)B * N * H * d_head / 4 + 255) / 256; }
+__global__ void __launch_bounds__(256) rel_join_grads_kernel(const RelAttnK p, unsigned dq_workgroups) {
+  __shared__ float meet[256];
+  if ((int)blockIdx.x < p.table_items) return rel_table_sums(p, (int)blockIdx.x, meet);
+  const unsigned id = blockIdx.x - p.table_items;
+  const int hd = p.H * p.dh;
+  const size_t at = ((id < dq_workgroups ? id : id - dq_workgroups) * 256ul + threadIdx.x) * 4;
+  if (id < dq_workgroups) {
+    const size_t rows = (size_t)p.B * p.Nq;
+    if (at < rows * hd) rel_join_rows(p.dq_partial, p.ksplits, rows, hd, at, (bf16*)p.dq, p.lddq);
+    return;
+  }
+  const size_t rows = (size_t)p.B * p.Nk;
+  if (at >= rows * hd) return;
+  rel_join_rows(p.dkv_partial, p.qsplits, rows, hd, at, (bf16*)p.dk, p.lddk);
+  rel_join_rows(p.dkv_partial + p.qsplits * rows * hd, p.qsplits, rows, hd, at, (bf16*)p.dv, p.lddv);
 }
 
 // ------------------------------------------------------------------ fp32
@@ -1696,25 +1701,45 @@ static int rel_buckets(const char* who, int n_buckets, int max_distance, int bid
 
 static size_t rel_align(size_t n) { return align_up(n, 256); }
 // Shares of the queries where a workgroup has all keys of a head: as many as run beside each other, of two tiles at least.
+constexpr long REL_QUERY_SHARES = 16, REL_QUERY_BLOCKS = 512;
 static int rel_query_shares(int B, int H, int Nq) {
   const long blocks = (long)B * H, tiles = (Nq + 63) / 64;
   if (blocks >= 256) return 1;
-  const long shares = std::max<long>(1, std::min<long>(std::min<long>(16, tiles / 2), (512 + blocks - 1) / blocks)), each = (tiles + shares - 1) / shares;
+  const long shares = std::max<long>(1, std::min(std::min(REL_QUERY_SHARES, tiles / 2), (REL_QUERY_BLOCKS + blocks - 1) / blocks)), each = (tiles + shares - 1) / shares;
   return (int)((tiles + each - 1) / each);
 }
-// Workgroups that sum dS over buckets, of a head and sample
-static int rel_parts(int dtype, bool all_keys, int B, int H, int Nq) {
-  return dtype == DP_F32 ? (Nq + 31) / 32 : (all_keys ? rel_query_shares(B, H, Nq) : (Nq + 127) / 128);
+// Shares of the keys (dQ), or of the queries (dK / dV), where workgroups of 128 of the others are too few for the CUs: four tiles at least, two workgroups a CU at most,
+// and one only where half of the CUs would have none or the way is long, as the shares' fp32 sums pass through memory.  dQ and dK / dV, us a pass with 1 / 2 / 3 / 4 / 8
+// shares: 8 heads of 512 34 / 30 / 29 / 28 / -, 8 of 1024 55 / 44 / 42 / 40 / 44, 16 of 1024 55 / 50 / 53 / 50 / 68, but 32 of 1024 56 / 63, 48 of 512 37 / 47; 8 of
+// 2048 causal 93 / 67 / 65 / 60 / 73, 4 of 4096 175 / 105 / 99 / 90 / 107, 8 of 4096 176 / 146 / 166 / 164 / 191, 16 of 128 x 2048 (dQ alone) 55 / 40 / 34 / 31 / 28.
+constexpr long REL_GRAD_SHARES = 8, REL_GRAD_BLOCKS = 512;
+static long rel_grad_shares_most(int along) { return std::min(REL_GRAD_SHARES, (long)((along + 63) / 64) / 4); }
+static int rel_grad_shares(int B, int H, int N, int along) {
+  const long blocks = (long)B * H * ((N + 127) / 128);
+  if (blocks > (along >= 2048 ? 256 : 128)) return 1;
+  return (int)std::max<long>(1, std::min(rel_grad_shares_most(along), REL_GRAD_BLOCKS / blocks));
 }
-// The backward's: the same for both types and any bias
-struct RelWorkspace { size_t delta, partial, dkv, bytes; };
+// Workgroups that sum dS over buckets, of a head and sample
+static int rel_parts(int dtype, bool all_keys, int B, int H, int Nq, int Nk) {
+  return dtype == DP_F32 ? (Nq + 31) / 32 : (all_keys ? rel_query_shares(B, H, Nq) : (Nq + 127) / 128 * rel_grad_shares(B, H, Nq, Nk));
+}
+// The backward's: the same for both types and any bias.  Fewer samples may have more shares, but never more workgroups than REL_*_BLOCKS (begun) where there are
+// shares at all: what these leave is the bound, so that no size needs more than a greater one.
+struct RelWorkspace { size_t delta, partial, dq, dkv, bytes; };
 static RelWorkspace rel_workspace(int B, int H, int Nq, int Nk, int d_head, int n_buckets) {
   RelWorkspace w;
+  const size_t heads = (size_t)B * H, row = d_head * sizeof(float);
+  const size_t few_keys = REL_QUERY_BLOCKS + 255, parts = std::max(heads * ((Nq + 31) / 32), std::min(heads * ((Nq + 127) / 128) * REL_QUERY_SHARES, few_keys));
+  auto left = [&](int N, int along) {
+    const long most = rel_grad_shares_most(along);
+    return most > 1 ? std::min(most * heads * N, (size_t)REL_GRAD_BLOCKS * 128) : 0;
+  };
   w.delta = 0;
-  w.partial = rel_align((size_t)B * H * Nq * sizeof(float));
-  w.dkv = w.partial + rel_align((size_t)H * B * rel_parts(DP_F32, false, B, H, Nq) * n_buckets * sizeof(float));
-  const int shares = Nk <= 256 ? rel_query_shares(B, H, Nq) : 1;
-  w.bytes = w.dkv + (shares > 1 ? rel_align(2 * (size_t)shares * B * Nk * H * d_head * sizeof(float)) : 0);
+  w.partial = rel_align(heads * Nq * sizeof(float));
+  w.dq = w.partial + rel_align(parts * n_buckets * sizeof(float));
+  w.dkv = w.dq + rel_align(left(Nq, Nk) * row);
+  const size_t short_keys = Nq > 192 ? std::min(heads * REL_QUERY_SHARES, few_keys) * std::min(Nk, 256) : 0;
+  w.bytes = w.dkv + rel_align(2 * std::max(left(Nk, Nq), short_keys) * row);
   return w;
 }
 
@@ -1759,9 +1784,11 @@ static int rel_launched() {
 
 // Shares of the keys for workgroups of 32 queries: until three workgroups a CU are there, none with less than two tiles for each of its waves.  16 x 12 heads, one
 // query, 4000 keys: 1 / 2 / 3 / 4 / 5 / 8 shares 44 / 40 / 41 / 36 / 37 / 38 us, keys of different lengths 37 / 33 / 30 / 26 / 27 / 28; 12 heads 31 / 19 / 15 / 12 / 11 / 9.
+constexpr long REL_SHARE_BLOCKS = 768;
+static long rel_shares_most(int Nk) { return ((Nk + 63) / 64 + 7) / 8; }
 static int rel_shares(int B, int H, int Nq, int Nk) {
-  const long blocks = (long)B * H * ((Nq + 31) / 32), tiles = (Nk + 63) / 64;
-  return (int)std::max<long>(1, std::min<long>((tiles + 7) / 8, (768 + blocks - 1) / blocks));
+  const long blocks = (long)B * H * ((Nq + 31) / 32);
+  return (int)std::max<long>(1, std::min(rel_shares_most(Nk), (REL_SHARE_BLOCKS + blocks - 1) / blocks));
 }
 // Whether the forward takes 32 queries a workgroup and shares the keys out, instead of 128 queries that read each key once: where those are too few for
 // the CUs and these all run at once.  Heads, queries x keys, width, us by 32 (with what joins the shares) and by 128: 8, 64 x 4096, 64 14.8 / 65.6; 8, 256 x 4096, 64 18.9 / 66.4; 8,
@@ -1772,7 +1799,11 @@ static bool rel_few(int B, int H, int Nq, int Nk, int d_head) {
   const long blocks = (long)B * H * ((Nq + 31) / 32);
   return blocks <= (d_head <= 64 && Nk > 128 ? 512 : 256);
 }
-static size_t rel_share_bytes(int B, int H, int Nq, int d_head, int shares) { return shares > 1 ? align_up((size_t)shares * B * H * Nq * (d_head + 2) * sizeof(float), 256) : 0; }
+// (no size needs more than a greater one, as in rel_workspace)
+static size_t rel_share_bytes(int B, int H, int Nq, int Nk, int d_head) {
+  const size_t most = rel_shares_most(Nk);
+  return most > 1 ? align_up(std::min(most * B * H * Nq, (size_t)(2 * REL_SHARE_BLOCKS - 1) * 32) * (d_head + 2) * sizeof(float), 256) : 0;
+}
 
 static int check_rel(const char* who, int dtype, const RelAttnK& k, const dp_relbias* bias, bool bwd) {
   if (dtype != DP_F32 && dtype != DP_BF16) return set_error(DP_EINVAL, "unknown dtype");
@@ -1824,7 +1855,7 @@ int dp_relative_bucket(int n_buckets, int max_distance, int bidirectional, int d
 size_t dp_op_attention_relbias_workspace_bytes(int B, int H, int Nq, int Nk, int d_head, int n_buckets, int backward) {
   if (B <= 0 || H <= 0 || Nq <= 0 || Nk <= 0 || d_head <= 0 || n_buckets <= 0) return 0;
   if (backward) return rel_workspace(B, H, Nq, Nk, d_head, n_buckets).bytes;
-  return rel_few(B, H, Nq, Nk, d_head) ? rel_share_bytes(B, H, Nq, d_head, rel_shares(B, H, Nq, Nk)) : 0;
+  return rel_share_bytes(B, H, Nq, Nk, d_head);
 }
 
 int dp_op_attention_relbias_fwd(int dtype, int B, int H, int Nq, int Nk, int d_head, int causal, float scale, const void* q, int ldq, const void* k,
@@ -1852,7 +1883,7 @@ int dp_op_attention_relbias_fwd(int dtype, int B, int H, int Nq, int Nk, int d_h
   if (rel_few(B, H, Nq, Nk, d_head)) {
     if (workspace) {
       const int shares = rel_shares(B, H, Nq, Nk);
-      const size_t need = rel_share_bytes(B, H, Nq, d_head, shares);
+      const size_t need = rel_share_bytes(B, H, Nq, Nk, d_head);
       if ((uintptr_t)workspace % 256) return set_errorf(DP_EALIGN, "%s: workspace is not 256-byte aligned", who);
       if (workspace_bytes < need) return set_errorf(DP_EWORKSPACE, "%s: workspace too small (%zu bytes, needs %zu)", who, workspace_bytes, need);
       a.shares = shares;
@@ -1896,6 +1927,9 @@ int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_h
   DP_TRY(check_ptr(workspace, "workspace", 256));
   if (workspace_bytes < w.bytes) return set_errorf(DP_EWORKSPACE, "%s: workspace too small (%zu bytes, needs %zu)", who, workspace_bytes, w.bytes);
   a.delta = (float*)((char*)workspace + w.delta);
+  a.dq_partial = (float*)((char*)workspace + w.dq);
+  a.dkv_partial = (float*)((char*)workspace + w.dkv);
+  a.qsplits = a.ksplits = 1;
   a.dtable_partial = dtable ? (float*)((char*)workspace + w.partial) : nullptr;
   hipStream_t s = (hipStream_t)hip_stream;
   bool all_keys = false;      // one kernel whose workgroups hold all keys (where its LDS suffices for the bias)
@@ -1905,7 +1939,7 @@ int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_h
       return DP_OK;
     }));
   a.dtable = dtable;
-  a.dtable_parts = B * rel_parts(dtype, all_keys, B, H, Nq);
+  a.dtable_parts = B * rel_parts(dtype, all_keys, B, H, Nq, Nk);
   a.dtable_add = accumulate != 0;
   a.table_items = dtable ? (H * ((bias->n_buckets + 31) / 32) + 7) / 8 * 8 : 0;      // workgroups that add the parts of the table's gradient (eights: the others stay on their XCDs)
   const double fl = 4.0 * B * H * (double)Nq * Nk * d_head, by = (dtype == DP_BF16 ? 2.0 : 4.0) * B * H * d_head * (3.0 * Nq + 2.0 * Nk);
@@ -1923,7 +1957,6 @@ int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_h
   } else if (all_keys) {
     KScope ks(KK_ATTN_BWD_DKV, 2 * fl, 2 * by, s, Nq, Nk, d_head);
     a.qsplits = rel_query_shares(B, H, Nq);
-    a.dkv_partial = (float*)((char*)workspace + w.dkv);
     DP_TRY(rel_short_dispatch(d_head, Nk, [&](auto dhp, auto kc, auto nw) {
       const int lds = RelShort<dhp, nw>::BYTES + rel_sum_floats(a.bk, nw) * 4;
       DP_TRY((rel_allow_lds<rel_bwd_short_bf16_kernel<dhp, kc, nw>>(0, lds)));
@@ -1931,7 +1964,7 @@ int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_h
       return rel_launched();
     }));
     if (a.qsplits > 1) {
-      hipLaunchKernelGGL(rel_dkv_kernel, dim3((unsigned)(((size_t)B * Nk * H * d_head / 4 + 255) / 256) + a.table_items), dim3(256), 0, s, a);
+      hipLaunchKernelGGL(rel_join_grads_kernel, dim3((unsigned)(rel_join_workgroups(B, Nk, H, d_head) + a.table_items)), dim3(256), 0, s, a, 0u);
       return rel_launched();
     }
     if (dtable) {
@@ -1939,15 +1972,20 @@ int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_h
       return rel_launched();
     }
   } else {
-    const long qblocks = (long)((Nq + 127) / 128) * B * H, kblocks = (long)((Nk + 127) / 128) * B * H;
+    a.ksplits = rel_grad_shares(B, H, Nq, Nk);
+    a.qsplits = rel_grad_shares(B, H, Nk, Nq);
+    const long qblocks = (long)((Nq + 127) / 128) * B * H * a.ksplits, kblocks = (long)((Nk + 127) / 128) * B * H * a.qsplits;
     const int table = rel_table_floats(a.bk) * 4, both = rel_sum_floats(a.bk, 4) * 4;
     {
       KScope ks(KK_ATTN_BWD_DQ, fl, by, s, Nq, Nk, d_head);
       a.even = rel_takes_turns(qblocks, d_head <= 64 ? 3 : 2);
       DP_TRY(rel_dispatch(d_head, [&](auto dhp, auto kc) {
-        DP_TRY((rel_allow_lds<rel_bwd_dq_bf16_kernel<dhp, kc>>(512 * dhp, both)));
-        hipLaunchKernelGGL((rel_bwd_dq_bf16_kernel<dhp, kc>), dim3((unsigned)qblocks), dim3(256), both, s, a, st);
-        return rel_launched();
+        auto run = [&](auto shares) {
+          DP_TRY((rel_allow_lds<rel_bwd_dq_bf16_kernel<dhp, kc, shares>>(512 * dhp, both)));
+          hipLaunchKernelGGL((rel_bwd_dq_bf16_kernel<dhp, kc, shares>), dim3((unsigned)qblocks), dim3(256), both, s, a, st);
+          return rel_launched();
+        };
+        return a.ksplits > 1 ? run(std::true_type()) : run(std::false_type());
       }));
     }
     KScope ks(KK_ATTN_BWD_DKV, fl, by, s, Nq, Nk, d_head);
@@ -1956,16 +1994,21 @@ int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_h
     const bool many = d_head <= 64 && !causal && kblocks > 2 * 256;
     a.even = rel_takes_turns(kblocks, many ? 3 : 2);
     DP_TRY(rel_dispatch(d_head, [&](auto dhp, auto kc) {
-      constexpr int MANY = dhp == 64 ? 3 : 2;
-      if (MANY > 2 && many) {
-        DP_TRY((rel_allow_lds<rel_bwd_dkv_bf16_kernel<dhp, kc, MANY>>(768 * dhp, table)));
-        hipLaunchKernelGGL((rel_bwd_dkv_bf16_kernel<dhp, kc, MANY>), dim3((unsigned)kblocks + a.table_items), dim3(256), table, s, a, st);
-      } else {
-        DP_TRY((rel_allow_lds<rel_bwd_dkv_bf16_kernel<dhp, kc, 2>>(512 * dhp, table)));
-        hipLaunchKernelGGL((rel_bwd_dkv_bf16_kernel<dhp, kc, 2>), dim3((unsigned)kblocks + a.table_items), dim3(256), table, s, a, st);
-      }
-      return rel_launched();
+      auto run = [&](auto minw, auto shares) {
+        DP_TRY((rel_allow_lds<rel_bwd_dkv_bf16_kernel<dhp, kc, minw, shares>>((minw == 3 ? 768 : 512) * dhp, table)));
+        hipLaunchKernelGGL((rel_bwd_dkv_bf16_kernel<dhp, kc, minw, shares>), dim3((unsigned)kblocks + a.table_items), dim3(256), table, s, a, st);
+        return rel_launched();
+      };
+      using std::integral_constant;
+      if (a.qsplits > 1) return run(integral_constant<int, 2>(), std::true_type());
+      return many ? run(integral_constant<int, dhp == 64 ? 3 : 2>(), std::false_type()) : run(integral_constant<int, 2>(), std::false_type());
     }));
+    if (a.ksplits > 1 || a.qsplits > 1) {
+      const size_t dq = a.ksplits > 1 ? rel_join_workgroups(B, Nq, H, d_head) : 0, dkv = a.qsplits > 1 ? rel_join_workgroups(B, Nk, H, d_head) : 0;
+      a.table_items = 0;
+      hipLaunchKernelGGL(rel_join_grads_kernel, dim3((unsigned)(dq + dkv)), dim3(256), 0, s, a, (unsigned)dq);
+      DP_TRY(rel_launched());
+    }
   }
   return DP_OK;
 }

@@ -124,6 +124,19 @@ def test_attention_workspace_serves_smaller_batches(lib):
         assert all(a <= b for a, b in zip(sizes, sizes[1:]))
 
 
+def test_attention_workspace_serves_all_smaller_sizes(lib):
+    import random
+    r = random.Random(4)
+    size = lambda n: r.choice([1, r.randrange(1, 64), r.randrange(1, 600), r.randrange(1, 5000)]) if n else r.randrange(1, 70)  # noqa: E731
+    for _ in range(20000):
+        h, d, nb = r.choice([1, 3, 8, 12, 16]), r.choice([8, 40, 64, 96]), r.choice([2, 32, 320])
+        big = [size(0), size(1), size(1)]
+        small = [r.randrange(1, n + 1) if r.random() < 0.5 else n for n in big]
+        for backward in (0, 1):
+            a, b = (lib.dp_op_attention_relbias_workspace_bytes(x[0], h, x[1], x[2], d, nb, backward) for x in (small, big))
+            assert a <= b, (small, big, h, d, nb, backward)
+
+
 def test_bucket_refusals(lib):
     from paper_2405_01248_amd import binding as K
     for bad in ((1, 128, 0), (0, 128, 0), (-4, 128, 0), (33, 128, 1), (2, 128, 1), (32, 16, 0), (32, 8, 1), (513, 1024, 0), (32, 1025, 1)):

@@ -310,13 +310,20 @@ __global__ void __launch_bounds__(256, MINW) rel_fwd_bf16_kernel(const RelAttnK 
 }
 
 // Four columns of a query's output, unscaled, and (first column) the logarithm of its sum; m: reference of its exponentials (log2 domain).
-__device__ __forceinline__ void rel_store_o(const RelAttnK& p, const f32x4& o, float sum, float m, int b, int h, int row, int col) {
+template <typename T> __device__ __forceinline__ void rel_store_o(const RelAttnK& p, const f32x4& o, float sum, float m, int b, int h, int row, int col) {
   const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-  bf16x4 v;
+  typedef __attribute__((ext_vector_type(4))) T Four;
+  Four v;
 #pragma unroll
-  for (int u = 0; u < 4; ++u) v[u] = (bf16)(o[u] * inv);
-  *reinterpret_cast<bf16x4*>((bf16*)p.o + ((size_t)b * p.Nq + row) * p.ldo + h * p.dh + col) = v;
+  for (int u = 0; u < 4; ++u) v[u] = (T)(o[u] * inv);
+  *reinterpret_cast<Four*>((T*)p.o + ((size_t)b * p.Nq + row) * p.ldo + h * p.dh + col) = v;
   if (p.lse && col == 0) p.lse[((size_t)b * p.H + h) * p.Nq + row] = sum == 0.f ? -INFINITY : fmaf(m, LN2, logf(sum));
+}
+// The same of a share of the keys: unscaled columns, and (first column) reference and sum, for rel_join_kernel.
+__device__ __forceinline__ void rel_store_share(const RelAttnK& p, const f32x4& o, float sum, float m, int share, int bh, int row, int col) {
+  const size_t rows = (size_t)p.B * p.H * p.Nq, at = share * rows + (size_t)bh * p.Nq + row;
+  *reinterpret_cast<f32x4*>(p.part + at * p.dh + col) = o;
+  if (col == 0) *reinterpret_cast<u32x2*>(p.part + p.shares * rows * p.dh + 2 * at) = u32x2{__builtin_bit_cast(uint32_t, m), __builtin_bit_cast(uint32_t, sum)};
 }
 
 // ------------------------------------------------------------------ forward of few queries (bf16)
@@ -472,19 +479,13 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 2 : 1) rel_fwd_few_bf16_kerne
 #pragma unroll
       for (int u = 0; u < 4; ++u) o[u] = fmaf(a, v[u], o[u]);
     }
-    const size_t srow = (size_t)bh * p.Nq + row;
-    if (p.shares > 1) {
-      const size_t rows = (size_t)p.B * p.H * p.Nq;
-      *reinterpret_cast<f32x4*>(p.part + (share * rows + srow) * p.dh + col) = o;
-      if (col == 0) *reinterpret_cast<u32x2*>(p.part + p.shares * rows * p.dh + 2 * (share * rows + srow)) = u32x2{__builtin_bit_cast(uint32_t, top), __builtin_bit_cast(uint32_t, sum)};
-    } else {
-      rel_store_o(p, o, sum, top, b, h, row, col);
-    }
+    if (p.shares > 1) rel_store_share(p, o, sum, top, share, bh, row, col);
+    else rel_store_o<bf16>(p, o, sum, top, b, h, row, col);
   }
 }
 
 // The shares of few queries, over their common reference, in their order; four columns a thread.
-__global__ void __launch_bounds__(256) rel_join_kernel(const RelAttnK p) {
+template <typename T> __global__ void __launch_bounds__(256) rel_join_kernel(const RelAttnK p) {
   const int per_row = p.dh / 4;
   const size_t rows = (size_t)p.B * p.H * p.Nq, at = blockIdx.x * 256ul + threadIdx.x, srow = at / per_row;
   if (srow >= rows) return;
@@ -519,7 +520,7 @@ __global__ void __launch_bounds__(256) rel_join_kernel(const RelAttnK p) {
       for (int c = 0; c < 4; ++c) o[c] = fmaf(a, v[u][c], o[c]);
     }
   }
-  rel_store_o(p, o, sum, top, bh / p.H, bh % p.H, row, col);
+  rel_store_o<T>(p, o, sum, top, bh / p.H, bh % p.H, row, col);
 }
 
 // ------------------------------------------------------------------ dQ and the table's gradient (bf16)
@@ -778,7 +779,7 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 3 : 2) rel_bwd_dq_bf16_kernel
         }
       }
   }
-  if (p.dtable_partial) rel_bucket_sums<4, false>(p, starts, sums, sum_stride, far_sums, second ? -far_sum_lo : far_sum_lo, second ? -far_sum_hi : far_sum_hi, p.dtable_partial + (((size_t)h * p.B + b) * qtiles * (SHARES ? p.ksplits : 1) + (SHARES ? share * qtiles : 0) + qtile) * p.bk.n_buckets);
+  if (p.dtable_partial) rel_bucket_sums<4, false>(p, starts, sums, sum_stride, far_sums, second ? -far_sum_lo : far_sum_lo, second ? -far_sum_hi : far_sum_hi, p.dtable_partial + ((((size_t)h * p.B + b) * (SHARES ? p.ksplits : 1) + share) * qtiles + qtile) * p.bk.n_buckets);
 }
 
 // dtable[bucket][head] = sum over the parts, in their order: 32 buckets of a head a workgroup (item: head, then which 32), eight shares of the parts.  Where a
@@ -1251,7 +1252,7 @@ __global__ void __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2,
 }
 
 // What the shares leave of dQ, and of dK and dV, added in their order; four columns a thread.
-__device__ __forceinline__ void rel_join_rows(const float* part, int shares, size_t rows, int cols, size_t at, bf16* out, int ld) {
+template <typename T> __device__ __forceinline__ void rel_join_rows(const float* part, int shares, size_t rows, int cols, size_t at, T* out, int ld) {
   const size_t row = at / cols, col = at % cols;
   f32x4 s = *reinterpret_cast<const f32x4*>(part + at);
 #pragma unroll 4
@@ -1260,13 +1261,14 @@ __device__ __forceinline__ void rel_join_rows(const float* part, int shares, siz
 #pragma unroll
     for (int u = 0; u < 4; ++u) s[u] += v[u];
   }
-  bf16x4 o;
+  typedef __attribute__((ext_vector_type(4))) T Four;
+  Four o;
 #pragma unroll
-  for (int u = 0; u < 4; ++u) o[u] = (bf16)s[u];
-  *reinterpret_cast<bf16x4*>(out + row * ld + col) = o;
+  for (int u = 0; u < 4; ++u) o[u] = (T)s[u];
+  *reinterpret_cast<Four*>(out + row * ld + col) = o;
 }
 static size_t rel_join_workgroups(int B, int N, int H, int d_head) { return ((size_t)B * N * H * d_head / 4 + 255) / 256; }
-__global__ void __launch_bounds__(256) rel_join_grads_kernel(const RelAttnK p, unsigned dq_workgroups) {
+template <typename T> __global__ void __launch_bounds__(256) rel_join_grads_kernel(const RelAttnK p, unsigned dq_workgroups) {
   __shared__ float meet[256];
   if ((int)blockIdx.x < p.table_items) return rel_table_sums(p, (int)blockIdx.x, meet);
   const unsigned id = blockIdx.x - p.table_items;
@@ -1274,13 +1276,13 @@ __global__ void __launch_bounds__(256) rel_join_grads_kernel(const RelAttnK p, u
   const size_t at = ((id < dq_workgroups ? id : id - dq_workgroups) * 256ul + threadIdx.x) * 4;
   if (id < dq_workgroups) {
     const size_t rows = (size_t)p.B * p.Nq;
-    if (at < rows * hd) rel_join_rows(p.dq_partial, p.ksplits, rows, hd, at, (bf16*)p.dq, p.lddq);
+    if (at < rows * hd) rel_join_rows(p.dq_partial, p.ksplits, rows, hd, at, (T*)p.dq, p.lddq);
     return;
   }
   const size_t rows = (size_t)p.B * p.Nk;
   if (at >= rows * hd) return;
-  rel_join_rows(p.dkv_partial, p.qsplits, rows, hd, at, (bf16*)p.dk, p.lddk);
-  rel_join_rows(p.dkv_partial + p.qsplits * rows * hd, p.qsplits, rows, hd, at, (bf16*)p.dv, p.lddv);
+  rel_join_rows(p.dkv_partial, p.qsplits, rows, hd, at, (T*)p.dk, p.lddk);
+  rel_join_rows(p.dkv_partial + p.qsplits * rows * hd, p.qsplits, rows, hd, at, (T*)p.dv, p.lddv);
 }
 
 // ------------------------------------------------------------------ fp32
@@ -1290,7 +1292,7 @@ __global__ void __launch_bounds__(256) rel_join_grads_kernel(const RelAttnK p, u
 // through LDS on its way in: an instruction takes 64 cycles, several loads' time.
 // A workgroup has 32 queries (forward, dQ) or 32 keys (dK / dV) of a head; its four waves take every fourth tile of 32 of the other side and
 // add what they have in LDS at the end, in their order.  Bound by the matrix instruction where there is work for all CUs, else by the chain of tiles: 2 x 8 heads of
-// 1024, width 64, forward 59 us (73 TF/s of 153), dQ 83, dK / dV 109; 2 x 4 of 257, width 40, 17 and 20.  Rows a tile ahead in registers, where there are any
+// 1024, width 64, forward 59 us (73 TF/s of 153), dQ 83, dK / dV 109.  Few heads go in shares (rel_shares_f32).  Rows a tile ahead in registers, where there are any
 // (widths to 64): 102 -> 90 and 127 -> 118 us.
 __device__ __forceinline__ f32x16 mfma_f32(float a, float b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0); }
 
@@ -1372,19 +1374,21 @@ __global__ void __launch_bounds__(256) rel_fwd_f32_kernel(const RelAttnK p, cons
   extern __shared__ __attribute__((aligned(16))) float rel_lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, l32 = lane & 31;
   const int bk_lo = p.bk.lo, bk_hi = p.bk.hi;
+  const int qtiles = (p.Nq + 31) / 32, all = qtiles * p.B * p.H, share = p.shares > 1 ? (int)blockIdx.x / all : 0;
   int qtile, bh;
-  rel_block_map(p, blockIdx.x, (p.Nq + 31) / 32, true, qtile, bh);
+  rel_block_map(p, (int)blockIdx.x - share * all, qtiles, true, qtile, bh);
   const int b = bh / p.H, h = bh % p.H, qi = qtile * 32 + l32, pos0 = p.query0 + qtile * 32, pos = pos0 + l32;
   RelFill<float, false, 256> fill;
   fill.request(p, st, h);
   const int keys = __builtin_amdgcn_readfirstlane(rel_keys(p, b));
   const int lim = p.causal ? min(keys, pos + 1) : keys, lim_all = p.causal ? min(keys, pos0 + 1) : keys;
-  const int lim_any = p.causal ? min(keys, p.query0 + min(p.Nq, qtile * 32 + 32)) : keys, nkt = lim_any > 0 ? (lim_any + 31) / 32 : 0;
+  const int lim_any = p.causal ? min(keys, p.query0 + min(p.Nq, qtile * 32 + 32)) : keys, tiles = lim_any > 0 ? (lim_any + 31) / 32 : 0;
+  const int first = (int)((long)tiles * share / p.shares) + wave, nkt = (int)((long)tiles * (share + 1) / p.shares);
   const float* kb = (const float*)p.k + (size_t)b * p.Nk * p.ldk + h * p.dh;
   const float* vb = (const float*)p.v + (size_t)b * p.Nk * p.ldv + h * p.dh;
   RelRows<KC> q, k;
   q.load((const float*)p.q + (size_t)b * p.Nq * p.ldq + h * p.dh, min(qi, p.Nq - 1), p.ldq, p.dh, g);
-  if (wave < nkt) k.load(kb, min(32 * wave + l32, keys - 1), p.ldk, p.dh, g);
+  if (first < nkt) k.load(kb, min(32 * first + l32, keys - 1), p.ldk, p.dh, g);
   fill.store(p, st, h, rel_lds, p.inv_scale);
   const int tab = 4 * g - pos - (bk_lo - REL_MARGIN);      // entry of this lane's first key
   f32x16 oacc[DT];
@@ -1393,7 +1397,7 @@ __global__ void __launch_bounds__(256) rel_fwd_f32_kernel(const RelAttnK p, cons
   float m = -INFINITY, lsum = 0.f;
   __syncthreads();
   const float far_lo = rel_uniform(rel_lds[0]), far_hi = rel_uniform(rel_lds[rel_entries(p.bk) - 1]);
-  for (int kt = wave; kt < nkt; kt += 4) {
+  for (int kt = first; kt < nkt; kt += 4) {
     const int k0 = 32 * kt;
     RelColumns<DT> v;
     v.load(vb, k0, keys - 1, p.ldv, p.dh, g, l32);
@@ -1437,12 +1441,9 @@ __global__ void __launch_bounds__(256) rel_fwd_f32_kernel(const RelAttnK p, cons
       a[w] = __builtin_amdgcn_exp2f(stat[w][0][row] - ref);
       sum = fmaf(a[w], stat[w][1][row], sum);
     }
-    const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-    f32x4 o = rel_meet<DT>(meet, row, col, a);
-#pragma unroll
-    for (int u = 0; u < 4; ++u) o[u] *= inv;
-    *reinterpret_cast<f32x4*>((float*)p.o + ((size_t)b * p.Nq + i) * p.ldo + h * p.dh + col) = o;
-    if (p.lse && col == 0) p.lse[((size_t)b * p.H + h) * p.Nq + i] = sum == 0.f ? -INFINITY : fmaf(top, LN2, logf(sum));
+    const f32x4 o = rel_meet<DT>(meet, row, col, a);
+    if (p.shares > 1) rel_store_share(p, o, sum, top, share, bh, i, col);
+    else rel_store_o<float>(p, o, sum, top, b, h, i, col);
   }
 }
 
@@ -1454,8 +1455,9 @@ __global__ void __launch_bounds__(256) rel_bwd_dq_f32_kernel(const RelAttnK p, c
   extern __shared__ __attribute__((aligned(16))) float rel_lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, l32 = lane & 31;
   const int bk_lo = p.bk.lo, bk_hi = p.bk.hi, qtiles = (p.Nq + 31) / 32, entries = rel_entries(p.bk);
+  const int all = qtiles * p.B * p.H, share = p.ksplits > 1 ? (int)blockIdx.x / all : 0;
   int qtile, bh;
-  rel_block_map(p, blockIdx.x, qtiles, true, qtile, bh);
+  rel_block_map(p, (int)blockIdx.x - share * all, qtiles, true, qtile, bh);
   const int b = bh / p.H, h = bh % p.H, qi = qtile * 32 + l32, pos0 = p.query0 + qtile * 32, pos = pos0 + l32;
   RelFill<float, false, 256> fill;
   fill.request(p, st, h);
@@ -1463,7 +1465,8 @@ __global__ void __launch_bounds__(256) rel_bwd_dq_f32_kernel(const RelAttnK p, c
   const bool qok = qi < p.Nq;
   const int keys = __builtin_amdgcn_readfirstlane(rel_keys(p, b));
   const int lim = p.causal ? min(keys, pos + 1) : keys, lim_all = p.causal ? min(keys, pos0 + 1) : keys;
-  const int lim_any = p.causal ? min(keys, p.query0 + min(p.Nq, qtile * 32 + 32)) : keys, nkt = lim_any > 0 ? (lim_any + 31) / 32 : 0;
+  const int lim_any = p.causal ? min(keys, p.query0 + min(p.Nq, qtile * 32 + 32)) : keys, tiles = lim_any > 0 ? (lim_any + 31) / 32 : 0;
+  const int first = (int)((long)tiles * share / p.ksplits) + wave, nkt = (int)((long)tiles * (share + 1) / p.ksplits);
   const float* kb = (const float*)p.k + (size_t)b * p.Nk * p.ldk + h * p.dh;
   const float* vb = (const float*)p.v + (size_t)b * p.Nk * p.ldv + h * p.dh;
   const int qrow = min(qi, p.Nq - 1);
@@ -1479,7 +1482,7 @@ __global__ void __launch_bounds__(256) rel_bwd_dq_f32_kernel(const RelAttnK p, c
 #pragma unroll
     for (int u = 0; u < 4; ++u) dlt = fmaf(k.v[c][u], dout.v[c][u], dlt);
   dlt = reduce_halves(dlt, AddOp());
-  if (qok && tid < 32) p.delta[sidx] = dlt;
+  if (qok && tid < 32 && share == 0) p.delta[sidx] = dlt;
   fill.store(p, st, h, rel_lds, p.inv_scale);
   float* sums = rel_lds + rel_table_floats(p.bk);
   const int sum_stride = rel_sum_stride(p.bk);
@@ -1494,11 +1497,11 @@ __global__ void __launch_bounds__(256) rel_bwd_dq_f32_kernel(const RelAttnK p, c
   const float far_lo = rel_uniform(rel_lds[0]), far_hi = rel_uniform(rel_lds[entries - 1]);
   constexpr bool AHEAD = DT < 3;      // the rows of the next tile requested behind this one's products (wide heads have no registers for them)
   RelRows<KC> v;
-  if (AHEAD && wave < nkt) {
-    k.load(kb, min(32 * wave + l32, keys - 1), p.ldk, p.dh, g);
-    v.load(vb, min(32 * wave + l32, keys - 1), p.ldv, p.dh, g);
+  if (AHEAD && first < nkt) {
+    k.load(kb, min(32 * first + l32, keys - 1), p.ldk, p.dh, g);
+    v.load(vb, min(32 * first + l32, keys - 1), p.ldv, p.dh, g);
   }
-  for (int kt = wave; kt < nkt; kt += 4) {
+  for (int kt = first; kt < nkt; kt += 4) {
     const int k0 = 32 * kt, row = min(k0 + l32, keys - 1);
     RelColumns<DT> kc;
     if (!AHEAD) {
@@ -1541,9 +1544,10 @@ __global__ void __launch_bounds__(256) rel_bwd_dq_f32_kernel(const RelAttnK p, c
     const int row = at / (8 * DT), col = at % (8 * DT) * 4, i = qtile * 32 + row;
     if (i >= p.Nq || col >= p.dh) continue;
     const float each[4] = {p.scale, p.scale, p.scale, p.scale};
-    *reinterpret_cast<f32x4*>((float*)p.dq + ((size_t)b * p.Nq + i) * p.lddq + h * p.dh + col) = rel_meet<DT>(meet, row, col, each);
+    float* out = p.ksplits > 1 ? p.dq_partial + (((size_t)share * p.B + b) * p.Nq + i) * ((size_t)p.H * p.dh) : (float*)p.dq + ((size_t)b * p.Nq + i) * p.lddq;
+    *reinterpret_cast<f32x4*>(out + h * p.dh + col) = rel_meet<DT>(meet, row, col, each);
   }
-  if (p.dtable_partial) rel_bucket_sums<4, false>(p, starts, sums, sum_stride, far_sums, far_sum_lo, far_sum_hi, p.dtable_partial + ((size_t)h * p.B * qtiles + (size_t)b * qtiles + qtile) * p.bk.n_buckets);
+  if (p.dtable_partial) rel_bucket_sums<4, false>(p, starts, sums, sum_stride, far_sums, far_sum_lo, far_sum_hi, p.dtable_partial + ((((size_t)h * p.B + b) * p.ksplits + share) * qtiles + qtile) * p.bk.n_buckets);
 }
 
 template <int DT, int KC>
@@ -1554,13 +1558,15 @@ __global__ void __launch_bounds__(256) rel_bwd_dkv_f32_kernel(const RelAttnK p, 
   const int ktiles = (p.Nk + 31) / 32, id = (int)blockIdx.x - p.table_items;
   if (id < 0) return rel_table_sums(p, (int)blockIdx.x, meet);
   const int bk_lo = p.bk.lo, bk_hi = p.bk.hi;
+  const int all = ktiles * p.B * p.H, share = p.qsplits > 1 ? id / all : 0;
   int ktile, bh;
-  rel_block_map(p, id, ktiles, false, ktile, bh);
+  rel_block_map(p, id - share * all, ktiles, false, ktile, bh);
   const int b = bh / p.H, h = bh % p.H, k0 = ktile * 32, ki = k0 + l32;
   RelFill<float, true, 256> fill;
   fill.request(p, st, h);
   const int keys = __builtin_amdgcn_readfirstlane(rel_keys(p, b));
-  const int nqt = k0 < keys ? (p.Nq + 31) / 32 : 0, first = p.causal ? max(0, k0 - p.query0) / 32 : 0;
+  const int seen = p.causal ? max(0, k0 - p.query0) / 32 : 0, tiles = k0 < keys ? max(0, (p.Nq + 31) / 32 - seen) : 0;
+  const int first = seen + (int)((long)tiles * share / p.qsplits), nqt = seen + (int)((long)tiles * (share + 1) / p.qsplits);
   const float* qb = (const float*)p.q + (size_t)b * p.Nq * p.ldq + h * p.dh;
   const float* dob = (const float*)p.dout + (size_t)b * p.Nq * p.lddo + h * p.dh;
   const float* lse_b = p.lse + ((size_t)b * p.H + h) * p.Nq;
@@ -1629,8 +1635,9 @@ __global__ void __launch_bounds__(256) rel_bwd_dkv_f32_kernel(const RelAttnK p, 
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
     const float f = which ? 1.0f : p.scale, each[4] = {f, f, f, f};
-    float* out = which ? (float*)p.dv : (float*)p.dk;
-    const int ld = which ? p.lddv : p.lddk;
+    const size_t hd = (size_t)p.H * p.dh;
+    float* out = p.qsplits > 1 ? p.dkv_partial + (which * p.qsplits + share) * ((size_t)p.B * p.Nk * hd) : which ? (float*)p.dv : (float*)p.dk;
+    const size_t ld = p.qsplits > 1 ? hd : which ? p.lddv : p.lddk;
     if (which) __syncthreads();
     rel_leave(meet, which ? dvacc : dkacc, wave, g, l32);
     __syncthreads();
@@ -1719,9 +1726,19 @@ static int rel_grad_shares(int B, int H, int N, int along) {
   if (blocks > (along >= 2048 ? 256 : 128)) return 1;
   return (int)std::max<long>(1, std::min(rel_grad_shares_most(along), REL_GRAD_BLOCKS / blocks));
 }
+// Shares in fp32, where a workgroup has 32 of one side, its four waves every fourth tile of 32 of the other, and mostly a CU to itself: until each CU has one, or
+// each wave one tile; the forward, which has less to do for a tile, where waves would have three.  Forward and backward, us a pass with 1 / 2 / 4 / 16 shares at most:
+// 2 x 4 heads of 257, width 40, 12 + 38 / 14 + 33 / 11 + 26 / 11 + 26; 4 of 1024 causal 28 + 95 / 21 + 63 / 21 + 62 / 21 + 62; 16 of 256 11 + 38 / 13 + 33 (forward left whole); 12 of
+// one query and 4000 keys, forward 88 / 50 / 29 / 15; 8 of 100 x 1000, width 96, 39 + 86 / 27 + 60 / 19 + 46 / 16 + 40.
+static long rel_shares_most_f32(int along) { return std::min(16l, ((along + 31) / 32 + 3l) / 4); }
+static int rel_shares_f32(int B, int H, int N, int along, bool backward) {
+  const long blocks = (long)B * H * ((N + 31) / 32);
+  return backward || along > 256 ? (int)std::max<long>(1, std::min(rel_shares_most_f32(along), 256 / blocks)) : 1;
+}
 // Workgroups that sum dS over buckets, of a head and sample
 static int rel_parts(int dtype, bool all_keys, int B, int H, int Nq, int Nk) {
-  return dtype == DP_F32 ? (Nq + 31) / 32 : (all_keys ? rel_query_shares(B, H, Nq) : (Nq + 127) / 128 * rel_grad_shares(B, H, Nq, Nk));
+  if (dtype == DP_F32) return (Nq + 31) / 32 * rel_shares_f32(B, H, Nq, Nk, true);
+  return all_keys ? rel_query_shares(B, H, Nq) : (Nq + 127) / 128 * rel_grad_shares(B, H, Nq, Nk);
 }
 // The backward's: the same for both types and any bias.  Fewer samples may have more shares, but never more workgroups than REL_*_BLOCKS (begun) where there are
 // shares at all: what these leave is the bound, so that no size needs more than a greater one.
@@ -1729,9 +1746,9 @@ struct RelWorkspace { size_t delta, partial, dq, dkv, bytes; };
 static RelWorkspace rel_workspace(int B, int H, int Nq, int Nk, int d_head, int n_buckets) {
   RelWorkspace w;
   const size_t heads = (size_t)B * H, row = d_head * sizeof(float);
-  const size_t few_keys = REL_QUERY_BLOCKS + 255, parts = std::max(heads * ((Nq + 31) / 32), std::min(heads * ((Nq + 127) / 128) * REL_QUERY_SHARES, few_keys));
+  const size_t few_keys = REL_QUERY_BLOCKS + 255, parts = std::max(heads * ((Nq + 31) / 32), std::min(heads * ((Nq + 31) / 32) * REL_QUERY_SHARES, few_keys));
   auto left = [&](int N, int along) {
-    const long most = rel_grad_shares_most(along);
+    const long most = rel_shares_most_f32(along);      // (no less than the other type's)
     return most > 1 ? std::min(most * heads * N, (size_t)REL_GRAD_BLOCKS * 128) : 0;
   };
   w.delta = 0;
@@ -1801,7 +1818,7 @@ static bool rel_few(int B, int H, int Nq, int Nk, int d_head) {
 }
 // (no size needs more than a greater one, as in rel_workspace)
 static size_t rel_share_bytes(int B, int H, int Nq, int Nk, int d_head) {
-  const size_t most = rel_shares_most(Nk);
+  const size_t most = std::max(rel_shares_most(Nk), rel_shares_most_f32(Nk));
   return most > 1 ? align_up(std::min(most * B * H * Nq, (size_t)(2 * REL_SHARE_BLOCKS - 1) * 32) * (d_head + 2) * sizeof(float), 256) : 0;
 }
 
@@ -1871,31 +1888,37 @@ int dp_op_attention_relbias_fwd(int dtype, int B, int H, int Nq, int Nk, int d_h
   DP_TRY(rel_buckets(who, bias->n_buckets, bias->max_distance, bias->bidirectional, a.bk, st));
   hipStream_t s = (hipStream_t)hip_stream;
   KScope ks(dtype == DP_BF16 ? KK_ATTN_FWD : KK_ATTN_F32, 4.0 * B * H * (double)Nq * Nk * d_head, (dtype == DP_BF16 ? 2.0 : 4.0) * B * H * d_head * (2.0 * Nq + 2.0 * Nk), s, Nq, Nk, d_head);
+  const size_t need = rel_share_bytes(B, H, Nq, Nk, d_head), joins = ((size_t)B * H * Nq * (d_head / 4) + 255) / 256;
+  auto shares = [&](int n) -> int {      // as many, if there is a workspace for what they leave
+    if (!workspace) return DP_OK;
+    if ((uintptr_t)workspace % 256) return set_errorf(DP_EALIGN, "%s: workspace is not 256-byte aligned", who);
+    if (workspace_bytes < need) return set_errorf(DP_EWORKSPACE, "%s: workspace too small (%zu bytes, needs %zu)", who, workspace_bytes, need);
+    a.shares = n;
+    a.part = (float*)workspace;
+    return DP_OK;
+  };
   if (dtype == DP_F32) {
+    DP_TRY(shares(rel_shares_f32(B, H, Nq, Nk, false)));
     const int table = rel_table_floats(a.bk) * 4;
-    return rel_dispatch_f32(d_head, [&](auto dt, auto kc) {
+    DP_TRY(rel_dispatch_f32(d_head, [&](auto dt, auto kc) {
       DP_TRY((rel_allow_lds<rel_fwd_f32_kernel<dt, kc>>(REL_F32_MEET<dt> * 4, table)));
-      hipLaunchKernelGGL((rel_fwd_f32_kernel<dt, kc>), dim3((unsigned)((Nq + 31) / 32 * B * H)), dim3(256), table, s, a, st);
+      hipLaunchKernelGGL((rel_fwd_f32_kernel<dt, kc>), dim3((unsigned)((Nq + 31) / 32 * B * H * a.shares)), dim3(256), table, s, a, st);
       return rel_launched();
-    });
+    }));
+    if (a.shares == 1) return DP_OK;
+    hipLaunchKernelGGL((rel_join_kernel<float>), dim3((unsigned)joins), dim3(256), 0, s, a);
+    return rel_launched();
   }
   const int lds = rel_table_floats(a.bk) * 4;
   if (rel_few(B, H, Nq, Nk, d_head)) {
-    if (workspace) {
-      const int shares = rel_shares(B, H, Nq, Nk);
-      const size_t need = rel_share_bytes(B, H, Nq, Nk, d_head);
-      if ((uintptr_t)workspace % 256) return set_errorf(DP_EALIGN, "%s: workspace is not 256-byte aligned", who);
-      if (workspace_bytes < need) return set_errorf(DP_EWORKSPACE, "%s: workspace too small (%zu bytes, needs %zu)", who, workspace_bytes, need);
-      a.shares = shares;
-      a.part = (float*)workspace;
-    }
+    DP_TRY(shares(rel_shares(B, H, Nq, Nk)));
     DP_TRY(rel_dispatch(d_head, [&](auto dhp, auto kc) {
       DP_TRY((rel_allow_lds<rel_fwd_few_bf16_kernel<dhp, kc>>(1024 * dhp, lds)));
       hipLaunchKernelGGL((rel_fwd_few_bf16_kernel<dhp, kc>), dim3((unsigned)((Nq + 31) / 32 * B * H * a.shares)), dim3(256), lds, s, a, st);
       return rel_launched();
     }));
     if (a.shares == 1) return DP_OK;
-    hipLaunchKernelGGL(rel_join_kernel, dim3((unsigned)(((size_t)B * H * Nq * (d_head / 4) + 255) / 256)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((rel_join_kernel<bf16>), dim3((unsigned)joins), dim3(256), 0, s, a);
     return rel_launched();
   }
   const long blocks = (long)((Nq + 127) / 128) * B * H;
@@ -1946,12 +1969,14 @@ int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_h
   if (dtype == DP_F32) {
     KScope ks(KK_ATTN_F32, 2 * fl, 2 * by, s, Nq, Nk, d_head);
     const int table = rel_table_floats(a.bk) * 4, both = rel_sum_floats(a.bk, 4) * 4;
+    a.ksplits = rel_shares_f32(B, H, Nq, Nk, true);
+    a.qsplits = rel_shares_f32(B, H, Nk, Nq, true);
     DP_TRY(rel_dispatch_f32(d_head, [&](auto dt, auto kc) {
       DP_TRY((rel_allow_lds<rel_bwd_dq_f32_kernel<dt, kc>>(REL_F32_MEET<dt> * 4, both)));
-      hipLaunchKernelGGL((rel_bwd_dq_f32_kernel<dt, kc>), dim3((unsigned)((Nq + 31) / 32 * B * H)), dim3(256), both, s, a, st);
+      hipLaunchKernelGGL((rel_bwd_dq_f32_kernel<dt, kc>), dim3((unsigned)((Nq + 31) / 32 * B * H * a.ksplits)), dim3(256), both, s, a, st);
       DP_TRY(rel_launched());
       DP_TRY((rel_allow_lds<rel_bwd_dkv_f32_kernel<dt, kc>>(REL_F32_MEET<dt> * 4, table)));
-      hipLaunchKernelGGL((rel_bwd_dkv_f32_kernel<dt, kc>), dim3((unsigned)((Nk + 31) / 32 * B * H) + a.table_items), dim3(256), table, s, a, st);
+      hipLaunchKernelGGL((rel_bwd_dkv_f32_kernel<dt, kc>), dim3((unsigned)((Nk + 31) / 32 * B * H * a.qsplits) + a.table_items), dim3(256), table, s, a, st);
       return rel_launched();
     }));
   } else if (all_keys) {
@@ -1964,7 +1989,7 @@ int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_h
       return rel_launched();
     }));
     if (a.qsplits > 1) {
-      hipLaunchKernelGGL(rel_join_grads_kernel, dim3((unsigned)(rel_join_workgroups(B, Nk, H, d_head) + a.table_items)), dim3(256), 0, s, a, 0u);
+      hipLaunchKernelGGL((rel_join_grads_kernel<bf16>), dim3((unsigned)(rel_join_workgroups(B, Nk, H, d_head) + a.table_items)), dim3(256), 0, s, a, 0u);
       return rel_launched();
     }
     if (dtable) {
@@ -2003,14 +2028,13 @@ int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_h
       if (a.qsplits > 1) return run(integral_constant<int, 2>(), std::true_type());
       return many ? run(integral_constant<int, dhp == 64 ? 3 : 2>(), std::false_type()) : run(integral_constant<int, 2>(), std::false_type());
     }));
-    if (a.ksplits > 1 || a.qsplits > 1) {
-      const size_t dq = a.ksplits > 1 ? rel_join_workgroups(B, Nq, H, d_head) : 0, dkv = a.qsplits > 1 ? rel_join_workgroups(B, Nk, H, d_head) : 0;
-      a.table_items = 0;
-      hipLaunchKernelGGL(rel_join_grads_kernel, dim3((unsigned)(dq + dkv)), dim3(256), 0, s, a, (unsigned)dq);
-      DP_TRY(rel_launched());
-    }
   }
-  return DP_OK;
+  if (all_keys || (a.ksplits == 1 && a.qsplits == 1)) return DP_OK;
+  const size_t dq_joins = a.ksplits > 1 ? rel_join_workgroups(B, Nq, H, d_head) : 0, dkv_joins = a.qsplits > 1 ? rel_join_workgroups(B, Nk, H, d_head) : 0;
+  a.table_items = 0;      // (they were there already)
+  if (dtype == DP_F32) hipLaunchKernelGGL((rel_join_grads_kernel<float>), dim3((unsigned)(dq_joins + dkv_joins)), dim3(256), 0, s, a, (unsigned)dq_joins);
+  else hipLaunchKernelGGL((rel_join_grads_kernel<bf16>), dim3((unsigned)(dq_joins + dkv_joins)), dim3(256), 0, s, a, (unsigned)dq_joins);
+  return rel_launched();
 }
 
 }  // extern "C"

@@ -221,33 +221,36 @@ def test_anything_in_buckets_that_the_causal_mask_hides(dtype, n):
            garbage={k: v for k, v in zip(range(17, 32), [float("nan"), float("inf"), -float("inf")] * 5)})
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("nq,nk", [(1, 3001), (32, 2500), (33, 700)])
-def test_few_queries_without_a_workspace(nq, nk):
-    _check("bf16", 2, 2, nq, nk, 64, True, False, 32, 128, nk - nq, [nk, nk // 3], workspace=False)
+def test_few_queries_without_a_workspace(dtype, nq, nk):
+    _check(dtype, 2, 2, nq, nk, 64, True, False, 32, 128, nk - nq, [nk, nk // 3], workspace=False)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("B,H,nq,nk,d,causal,lens", [
     (1, 3, 513, 513, 64, False, None), (1, 3, 513, 513, 64, True, None),                # shares of keys and of queries
     (1, 2, 70, 2100, 40, False, [1500]), (2, 1, 2050, 300, 96, True, [300, 7]),         # of one of them
     (1, 4, 1024, 1024, 80, True, [700]), (1, 5, 2048, 600, 48, False, [0]),             # shares that have nothing to do
     (1, 2, 600, 256, 64, False, None)])                                                 # shares of the queries, all keys in a workgroup
-def test_gradients_in_shares(B, H, nq, nk, d, causal, lens):
-    _check("bf16", B, H, nq, nk, d, causal, True, 32, 128, nk - nq if causal else 0, lens)
+def test_gradients_in_shares(dtype, B, H, nq, nk, d, causal, lens):
+    _check(dtype, B, H, nq, nk, d, causal, True, 32, 128, nk - nq if causal else 0, lens)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("B,H,nq,nk,d", [(1, 8, 1024, 1024, 64), (1, 2, 2048, 4096, 40), (3, 5, 520, 256, 96), (2, 4, 100, 3000, 64), (1, 16, 1, 4000, 64), (4, 12, 77, 77, 64)])
-def test_nothing_is_written_behind_the_workspace(B, H, nq, nk, d):
+def test_nothing_is_written_behind_the_workspace(dtype, B, H, nq, nk, d):
     import torch
     from paper_2405_01248_amd import binding as K
-    ld, nb = H * d, 32
-    q, do, o, dq = (torch.randn((B, nq, ld), device="cuda").bfloat16() for _ in range(4))
-    k, v, dk, dv = (torch.randn((B, nk, ld), device="cuda").bfloat16() for _ in range(4))
-    table, lse, dtable = torch.randn((nb, H), device="cuda").bfloat16(), torch.empty((B, H, nq), device="cuda"), torch.empty((nb, H), device="cuda")
+    ld, nb, t = H * d, 32, torch.float32 if dtype == "f32" else torch.bfloat16
+    q, do, o, dq = (torch.randn((B, nq, ld), device="cuda").to(t) for _ in range(4))
+    k, v, dk, dv = (torch.randn((B, nk, ld), device="cuda").to(t) for _ in range(4))
+    table, lse, dtable = torch.randn((nb, H), device="cuda").to(t), torch.empty((B, H, nq), device="cuda"), torch.empty((nb, H), device="cuda")
     bias = K.RelBias(table, nb, 128, True, 0)
     for backward in (False, True):
         n = K.op_attention_relbias_workspace_bytes(B, H, nq, nk, d, nb, backward)
         whole = torch.full((n + 65536,), 0x5A, dtype=torch.uint8, device="cuda")
-        args = (K.DP_BF16, B, H, nq, nk, d, False, 0.125, q, ld, k, ld, v, ld, bias, None, o, ld, lse)
+        args = (K.DP_F32 if dtype == "f32" else K.DP_BF16, B, H, nq, nk, d, False, 0.125, q, ld, k, ld, v, ld, bias, None, o, ld, lse)
         if backward:
             K.op_attention_relbias_bwd(*args, do, ld, dq, ld, dk, ld, dv, ld, dtable, False, whole[:n])
         else:

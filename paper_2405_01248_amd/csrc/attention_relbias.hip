@@ -1799,22 +1799,24 @@ static int rel_launched() {
   return e == hipSuccess ? DP_OK : set_errorf(DP_EHIP, "attention with a relative position bias: launch failed (%s)", hipGetErrorString(e));
 }
 
-// Shares of the keys for workgroups of 32 queries: until three workgroups a CU are there, none with less than two tiles for each of its waves.  16 x 12 heads, one
-// query, 4000 keys: 1 / 2 / 3 / 4 / 5 / 8 shares 44 / 40 / 41 / 36 / 37 / 38 us, keys of different lengths 37 / 33 / 30 / 26 / 27 / 28; 12 heads 31 / 19 / 15 / 12 / 11 / 9.
+// Shares of the keys for workgroups of 32 queries, none with less than two tiles for each of its waves.  Where a head is read for its few queries alone, and two
+// workgroups fit a CU, until three a CU are there: 16 x 12 heads, one query, 4000 keys: 1 / 2 / 3 / 4 / 5 / 8 shares 44 / 40 / 41 / 36 / 37 / 38 us, keys of different lengths
+// 37 / 33 / 30 / 26 / 27 / 28; 12 heads 31 / 19 / 15 / 12 / 11 / 9.  Else until each CU has one: 4 heads of 2000 in 1 / 2 / 4 shares 15 / 18 / 23, 8 of 1024 12 / 16, 8 of 256 x 4096
+// 29 / 22 / 16 (8: 16), width 72, 16 of 300 x 1000 16 / 24, width 96, 192 and 64 of one query and 4000 keys 75 / 87 / 77 and 52 / 36 / 29 (8: 31).
 constexpr long REL_SHARE_BLOCKS = 768;
 static long rel_shares_most(int Nk) { return ((Nk + 63) / 64 + 7) / 8; }
-static int rel_shares(int B, int H, int Nq, int Nk) {
+static int rel_shares(int B, int H, int Nq, int Nk, int d_head) {
   const long blocks = (long)B * H * ((Nq + 31) / 32);
-  return (int)std::max<long>(1, std::min(rel_shares_most(Nk), (REL_SHARE_BLOCKS + blocks - 1) / blocks));
+  return (int)std::max<long>(1, std::min(rel_shares_most(Nk), Nq <= 32 && d_head <= 64 ? (REL_SHARE_BLOCKS + blocks - 1) / blocks : 256 / blocks));
 }
 // Whether the forward takes 32 queries a workgroup and shares the keys out, instead of 128 queries that read each key once: where those are too few for
-// the CUs and these all run at once.  Heads, queries x keys, width, us by 32 (with what joins the shares) and by 128: 8, 64 x 4096, 64 14.8 / 65.6; 8, 256 x 4096, 64 18.9 / 66.4; 8,
-// 1024 x 1024, 64 16.4 / 20.8; 4, 2000 x 2000, 40 24 / 30.4; 32, 512 x 512, 64 12.9 / 14.2; 64, 128 x 256, 64 7.7 / 9.8; 32, 200 x 512, 72 11.8 / 14.4; but 32, 300 x 1000, 72 34.5 / 22.3;
-// 144, 77 x 77, 64 8.3 / 7.8; 768, 77 x 77, 64 29.7 / 13.1.
+// the CUs and these all run at once.  Heads, queries x keys, width, us by 32 (with what joins the shares) and by 128: 8, 256 x 4096, 64 16 / 54; 8, 1024 x 1024, 64 12 / 17; 16
+// 16 / 17; 8, 2048 x 2048, 64 27 / 30; 4, 2000 x 2000, 40 15 / 27; 32, 512 x 512, 64 11.0 / 11.2; 64, 128 x 256, 64 6.8 / 8.0; 24, 300 x 1000, 72 16 / 19; 12, 512 x 512, 96 11 / 13;
+// but 64, 256 x 256, 64 8.9 / 8.2; 32, 300 x 1000, 72 29 / 20; 24, 512 x 512, 96 21 / 14; 144, 77 x 77, 64 7.3 / 6.4.
 static bool rel_few(int B, int H, int Nq, int Nk, int d_head) {
   if (Nq <= 32) return true;
   const long blocks = (long)B * H * ((Nq + 31) / 32);
-  return blocks <= (d_head <= 64 && Nk > 128 ? 512 : 256);
+  return blocks <= (d_head <= 64 && Nk > 256 ? 512 : 256);
 }
 // (no size needs more than a greater one, as in rel_workspace)
 static size_t rel_share_bytes(int B, int H, int Nq, int Nk, int d_head) {
@@ -1911,7 +1913,7 @@ int dp_op_attention_relbias_fwd(int dtype, int B, int H, int Nq, int Nk, int d_h
   }
   const int lds = rel_table_floats(a.bk) * 4;
   if (rel_few(B, H, Nq, Nk, d_head)) {
-    DP_TRY(shares(rel_shares(B, H, Nq, Nk)));
+    DP_TRY(shares(rel_shares(B, H, Nq, Nk, d_head)));
     DP_TRY(rel_dispatch(d_head, [&](auto dhp, auto kc) {
       DP_TRY((rel_allow_lds<rel_fwd_few_bf16_kernel<dhp, kc>>(1024 * dhp, lds)));
       hipLaunchKernelGGL((rel_fwd_few_bf16_kernel<dhp, kc>), dim3((unsigned)((Nq + 31) / 32 * B * H * a.shares)), dim3(256), lds, s, a, st);

@@ -993,6 +993,337 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(MINW, 
   rel_store_dkv<DT>(p, dkacc, dvacc, p.scale, share, b, h, ki, kok, g);
 }
 
+// ------------------------------------------------------------------ dQ, dK, dV of few heads (bf16)
+// A workgroup has 32 queries (keys) of a head, and each of its waves every fourth tile of the other side, on LDS tiles of its own that it requests a tile ahead:
+// nothing waits at a barrier before the waves' sums meet at the end (see rel_fwd_few_bf16_kernel).  With 128 queries (keys) a workgroup the chain is sixteen tiles of 1.2 us for
+// 1024 of the other side, whatever few CUs have work (8 heads: 64); here it is four, on all: 8 heads of 1024 dQ 27 -> 16 us, dK / dV 27 -> 13 (chains bound both).
+// A wave's result [32 rows][columns] in LDS, and four columns of the sum over the waves
+template <int DHP> __device__ __forceinline__ void rel_few_leave(float* mine, const f32x16 (&acc)[DHP / 32], float factor, bool ok, int g, int l32) {
+#pragma unroll
+  for (int i = 0; i < DHP / 32; ++i)
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4) {
+      f32x4 v;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) v[u] = ok ? acc[i][4 * r4 + u] * factor : 0.f;
+      *reinterpret_cast<f32x4*>(mine + l32 * (DHP + 4) + 32 * i + 8 * r4 + 4 * g) = v;
+    }
+}
+template <int DHP, int STRIDE> __device__ __forceinline__ void rel_few_meet(const float* first, int row, int col, bool share, float* partial, bf16* out) {      // STRIDE: floats from wave to wave
+  f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const f32x4 v = *reinterpret_cast<const f32x4*>(first + w * STRIDE + row * (DHP + 4) + col);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) s[u] += v[u];
+  }
+  if (share) {
+    *reinterpret_cast<f32x4*>(partial) = s;
+    return;
+  }
+  bf16x4 o;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) o[u] = (bf16)s[u];
+  *reinterpret_cast<bf16x4*>(out) = o;
+}
+
+// Tiles of 64 keys: K through LDS, V by rows straight into registers.
+template <int DHP, int KC>
+__global__ void __launch_bounds__(256, DHP == 64 ? 2 : 1) rel_bwd_few_dq_bf16_kernel(const RelAttnK p, const RelStarts st) {
+  constexpr int DT = DHP / 32, TILE = 64 * DHP;
+  __shared__ __attribute__((aligned(1024))) bf16 Ks[4][2][TILE];
+  __shared__ float far_sums[2][4];
+  __shared__ uint16_t starts[REL_STARTS];
+  extern __shared__ __attribute__((aligned(16))) float rel_lds[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, l32 = lane & 31;
+  const int qtiles = (p.Nq + 31) / 32, entries = rel_entries(p.bk), bk_lo = p.bk.lo, bk_hi = p.bk.hi;
+  const int all = qtiles * p.B * p.H, share = p.ksplits > 1 ? (int)blockIdx.x / all : 0;
+  int qtile, bh;
+  rel_block_map(p, (int)blockIdx.x - share * all, qtiles, true, qtile, bh);
+  const int b = bh / p.H, h = bh % p.H;
+  RelFill<bf16, false, 256> fill;
+  fill.request(p, st, h);
+  rel_fill_starts(p.bk, st, starts, 256);
+  const int qi = qtile * 32 + l32, pos0 = p.query0 + qtile * 32, pos = pos0 + l32;
+  const bool qok = qi < p.Nq;
+  const int keys = __builtin_amdgcn_readfirstlane(rel_keys(p, b));
+  const int lim = p.causal ? min(keys, pos + 1) : keys, lim_all = p.causal ? min(keys, pos0 + 1) : keys;
+  const int lim_any = p.causal ? min(keys, p.query0 + min(p.Nq, qtile * 32 + 32)) : keys;
+  const int tiles = __builtin_amdgcn_readfirstlane(lim_any > 0 ? (lim_any + 63) / 64 : 0);
+  const int first = (int)((long)tiles * share / p.ksplits) + wave, nkt = (int)((long)tiles * (share + 1) / p.ksplits);
+  const u32x4 kr = make_raw_rsrc((const bf16*)p.k + (size_t)b * p.Nk * p.ldk + h * p.dh, rel_slice_bytes(keys, p.ldk, p.dh));
+  const bf16* vb = (const bf16*)p.v + (size_t)b * p.Nk * p.ldv + h * p.dh;
+  AttnFragOff<DHP, KC> fo;
+  fo.init(lane);
+  AttnTileCopy<DHP> ck[4];
+#pragma unroll
+  for (int w = 0; w < 4; ++w) ck[w].init(w, lane, p.ldk, p.dh);
+  bf16x8 vn[2][KC];
+  auto request = [&](int kt, int buf) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int c = 0; c < KC; ++c) {
+        const int key = kt * 64 + 32 * t + l32;
+        vn[t][c] = ld8(vb + (size_t)key * p.ldv + 16 * c + 8 * g, key < keys && 16 * c + 8 * g < p.dh);
+      }
+#pragma unroll
+    for (int w = 0; w < 4; ++w) ck[w].issue(kr, kt * 64, p.ldk, Ks[wave][buf], w);
+  };
+  if (first < nkt) request(first, 0);
+  const bool second = lane & 16;      // (see rel_bwd_dq_bf16_kernel)
+  const size_t row = (size_t)b * p.Nq + qi, head = h * p.dh;
+  bf16x8 qf[KC], dof[KC];
+  float dlt = 0.f;
+#pragma unroll
+  for (int c = 0; c < KC; ++c) {
+    const bool ok = qok && 16 * c + 8 * g < p.dh;
+    qf[c] = ld8((const bf16*)p.q + row * p.ldq + head + 16 * c + 8 * g, ok);
+    dof[c] = rel_turned(ld8((const bf16*)p.dout + row * p.lddo + head + 16 * c + 8 * g, ok), second);
+    const bf16x8 of = ld8((const bf16*)p.o + row * p.ldo + head + 16 * c + 8 * g, ok);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) dlt = fmaf((float)of[u], (float)dof[c][u], dlt);
+  }
+  dlt = reduce_halves(dlt, AddOp());
+  const size_t sidx = ((size_t)b * p.H + h) * p.Nq + qi;
+  float lse2 = INFINITY;      // of no query, and of one that sees no key: its probabilities are zero
+  if (qok) {
+    const float l = p.lse[sidx];
+    if (l != -INFINITY) lse2 = l * LOG2E;
+    if (tid < 32 && share == 0) p.delta[sidx] = second ? -dlt : dlt;
+  }
+  fill.store(p, st, h, rel_lds, p.inv_scale);
+  float* sums = rel_lds + rel_table_floats(p.bk);
+  const int sum_stride = rel_sum_stride(p.bk);
+  for (int e = tid; e < 8 * sum_stride; e += 256) sums[e] = 0.f;
+  const int tab = 4 * g - pos - (bk_lo - REL_MARGIN);      // entry of this lane's first key
+  float* const mine = sums + (2 * wave + g) * sum_stride;
+  float far_sum_lo = 0.f, far_sum_hi = 0.f;
+  f32x16 ndelta, acc[DT];
+#pragma unroll
+  for (int r = 0; r < 16; ++r) ndelta[r] = -dlt;
+#pragma unroll
+  for (int i = 0; i < DT; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[i][r] = 0.f;
+  __syncthreads();
+  const float far_lo = rel_uniform(rel_lds[0]), far_hi = rel_uniform(rel_lds[entries - 1]);
+
+  auto tile = [&](int kt, auto bc) __attribute__((always_inline)) {
+    constexpr int buf = bc();
+    wait_vmcnt<0>();      // this wave's own tile has landed
+    asm volatile("" ::: "memory");
+    f32x16 s[2], dp[2];
+    bool below[2], above[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int d0 = kt * 64 + 32 * t - pos0;
+      below[t] = d0 + 31 <= bk_lo;
+      above[t] = d0 - 31 >= bk_hi;
+      if (below[t] || above[t]) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[t][r] = below[t] ? far_lo : far_hi;
+      } else {
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4) {
+          const f32x4 v = rel_read4(rel_lds + (tab + kt * 64) + 32 * t + 8 * r4);
+#pragma unroll
+          for (int u = 0; u < 4; ++u) s[t][4 * r4 + u] = v[u];
+        }
+      }
+      dp[t] = mfma32(vn[t][0], dof[0], ndelta);
+      s[t] = mfma32(fo.row_frag(Ks[wave][buf], t, 0), qf[0], s[t]);
+#pragma unroll
+      for (int c = 1; c < KC; ++c) {
+        dp[t] = mfma32(vn[t][c], dof[c], dp[t]);
+        s[t] = mfma32(fo.row_frag(Ks[wave][buf], t, c), qf[c], s[t]);
+      }
+    }
+    if (kt + 4 < nkt) request(kt + 4, buf ^ 1);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int k0 = kt * 64 + 32 * t;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[t][r] = __builtin_amdgcn_exp2f(fmaf(s[t][r], p.scale_log2, -lse2)) * dp[t][r];
+      if (k0 + 32 > lim_all) {      // (here and not before the exponential: what is masked counts for nothing whatever it is)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[t][r] = k0 + acc_row(r, g) < lim ? s[t][r] : 0.f;
+      }
+      if (below[t] || above[t]) {
+        float sum = 0.f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sum += s[t][r];
+        if (below[t]) far_sum_lo += sum;
+        else far_sum_hi += sum;
+      } else {      // this wave's tiles lie 256 keys apart, and the two blocks of one share 32 distances
+        const RelDiagonals d = rel_diagonals<true>(s[t], lane);
+        mine[tab + k0] += d.near;
+        mine[tab + k0 + 32] = d.next;
+      }
+#pragma unroll
+      for (int cc = 0; cc < 2; ++cc) {
+        const bf16x8 dsf = pack8(s[t], 8 * cc);
+#pragma unroll
+        for (int i = 0; i < DT; ++i) acc[i] = mfma32(fo.tr_frag(Ks[wave][buf], 32 * t + 16 * cc, i), dsf, acc[i]);
+      }
+    }
+  };
+  for (int kt = first; kt < nkt; kt += 8) {
+    tile(kt, std::integral_constant<int, 0>());
+    if (kt + 4 < nkt) tile(kt + 4, std::integral_constant<int, 1>());
+  }
+  static_assert(32 * (DHP + 4) * 4 <= 2 * TILE * 2, "a wave's result lies in its K tiles");
+  asm volatile("" ::: "memory");
+  rel_few_leave<DHP>(reinterpret_cast<float*>(Ks[wave][0]), acc, second ? -p.scale : p.scale, true, g, l32);
+  __syncthreads();
+  for (int at = tid; at < 32 * (DHP / 4); at += 256) {
+    const int q = qtile * 32 + at / (DHP / 4), col = at % (DHP / 4) * 4;
+    if (q >= p.Nq || col >= p.dh) continue;
+    const size_t r = (size_t)b * p.Nq + q;
+    rel_few_meet<DHP, TILE>(reinterpret_cast<const float*>(Ks[0][0]), at / (DHP / 4), col, p.ksplits > 1, p.dq_partial + ((size_t)share * p.B * p.Nq + r) * (p.H * p.dh) + head + col,
+                            (bf16*)p.dq + r * p.lddq + head + col);
+  }
+  if (p.dtable_partial) rel_bucket_sums<4, false>(p, starts, sums, sum_stride, far_sums, second ? -far_sum_lo : far_sum_lo, second ? -far_sum_hi : far_sum_hi, p.dtable_partial + ((((size_t)h * p.B + b) * p.ksplits + share) * qtiles + qtile) * p.bk.n_buckets);
+}
+
+// Tiles of 32 queries: Q and dO through LDS, lse and delta a lane each.
+template <int DHP, int KC>
+__global__ void __launch_bounds__(256, DHP == 64 ? 2 : 1) rel_bwd_few_dkv_bf16_kernel(const RelAttnK p, const RelStarts st) {
+  constexpr int DT = DHP / 32, TILE = 32 * DHP;
+  __shared__ __attribute__((aligned(1024))) bf16 QD[4][2][2][TILE];      // [wave][stage][Q, dO]
+  __shared__ __attribute__((aligned(16))) float stats[4][64];            // -lse over the scale, -delta
+  extern __shared__ __attribute__((aligned(16))) float rel_lds[];
+  const int ktiles = (p.Nk + 31) / 32, id = (int)blockIdx.x - p.table_items;
+  if (id < 0) return rel_table_sums(p, (int)blockIdx.x, stats[0]);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, l32 = lane & 31;
+  const int bk_lo = p.bk.lo, bk_hi = p.bk.hi;
+  const int all = ktiles * p.B * p.H, share = p.qsplits > 1 ? id / all : 0;
+  int ktile, bh;
+  rel_block_map(p, id - share * all, ktiles, false, ktile, bh);
+  const int b = bh / p.H, h = bh % p.H, k0 = ktile * 32, ki = k0 + l32;
+  RelFill<bf16, true, 256> fill;
+  fill.request(p, st, h);
+  const int keys = __builtin_amdgcn_readfirstlane(rel_keys(p, b));
+  const bool kok = ki < keys;
+  const u32x4 qr = make_raw_rsrc((const bf16*)p.q + (size_t)b * p.Nq * p.ldq + h * p.dh, attn_slice_bytes(p.Nq, p.ldq, p.dh));
+  const u32x4 dr = make_raw_rsrc((const bf16*)p.dout + (size_t)b * p.Nq * p.lddo + h * p.dh, attn_slice_bytes(p.Nq, p.lddo, p.dh));
+  const float* stat_b = (g ? p.delta : p.lse) + ((size_t)b * p.H + h) * p.Nq;
+  const int seen = p.causal ? max(0, k0 - p.query0) / 32 : 0;
+  const int tiles = __builtin_amdgcn_readfirstlane(k0 < keys ? max(0, (p.Nq + 31) / 32 - seen) : 0);      // (no query sees keys past the sample's length)
+  const int first = seen + (int)((long)tiles * share / p.qsplits) + wave, nqt = seen + (int)((long)tiles * (share + 1) / p.qsplits);
+  AttnFragOff<DHP, KC> fo;
+  fo.init(lane);
+  AttnTileCopy<DHP> cq[2], cd[2];
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    cq[w].init(w, lane, p.ldq, p.dh);
+    cd[w].init(w, lane, p.lddo, p.dh);
+  }
+  float stat = 0.f;
+  auto request = [&](int qt, int buf) __attribute__((always_inline)) {
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      cq[w].issue(qr, qt * 32, p.ldq, QD[wave][buf][0], w);
+      cd[w].issue(dr, qt * 32, p.lddo, QD[wave][buf][1], w);
+    }
+    stat = stat_b[min(qt * 32 + l32, p.Nq - 1)];
+  };
+  if (first < nqt) request(first, 0);
+  bf16x8 kf[KC], vf[KC];
+#pragma unroll
+  for (int c = 0; c < KC; ++c) {
+    const bool ok = kok && 16 * c + 8 * g < p.dh;
+    kf[c] = ld8((const bf16*)p.k + ((size_t)b * p.Nk + ki) * p.ldk + h * p.dh + 16 * c + 8 * g, ok);
+    vf[c] = ld8((const bf16*)p.v + ((size_t)b * p.Nk + ki) * p.ldv + h * p.dh + 16 * c + 8 * g, ok);
+  }
+  fill.store(p, st, h, rel_lds, LOG2E);
+  const int tab = 4 * g + p.query0 - ki + bk_hi + REL_MARGIN;      // entry of this lane's first query
+  f32x16 dkacc[DT], dvacc[DT];
+#pragma unroll
+  for (int i = 0; i < DT; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) { dkacc[i][r] = 0.f; dvacc[i][r] = 0.f; }
+  __syncthreads();
+  const float far_hi = rel_uniform(rel_lds[0]), far_lo = rel_uniform(rel_lds[rel_entries(p.bk) - 1]);
+
+  auto tile = [&](int qt, auto bc) __attribute__((always_inline)) {
+    constexpr int buf = bc();
+    const bf16 *Q = QD[wave][buf][0], *D = QD[wave][buf][1];
+    wait_vmcnt<0>();      // this wave's own tile has landed
+    asm volatile("" ::: "memory");
+    {
+      const bool ok = qt * 32 + l32 < p.Nq;
+      if (g) stats[wave][lane] = ok ? -stat : 0.f;
+      else stats[wave][lane] = ok && stat != -INFINITY ? -stat * p.inv_scale : -INFINITY;      // (a query that sees no key has no probabilities)
+    }
+    if (qt + 4 < nqt) request(qt + 4, buf ^ 1);
+    const int pos = p.query0 + qt * 32;
+    const bool below = k0 + 31 - pos <= bk_lo, above = k0 - pos - 31 >= bk_hi;
+    f32x16 s, dp;
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4) {
+      const f32x4 l4 = *reinterpret_cast<const f32x4*>(&stats[wave][8 * r4 + 4 * g]), d4 = *reinterpret_cast<const f32x4*>(&stats[wave][32 + 8 * r4 + 4 * g]);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) { s[4 * r4 + u] = l4[u]; dp[4 * r4 + u] = d4[u]; }
+    }
+#pragma unroll
+    for (int c = 0; c < KC; ++c) {
+      s = mfma32(fo.row_frag(Q, 0, c), kf[c], s);
+      dp = mfma32(fo.row_frag(D, 0, c), vf[c], dp);
+    }
+    if (below || above) {
+      const float far = below ? far_lo : far_hi;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], p.scale_log2, far));
+    } else {
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        const f32x4 v = rel_read4(rel_lds + (tab + qt * 32) + 8 * r4);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) s[4 * r4 + u] = __builtin_amdgcn_exp2f(fmaf(s[4 * r4 + u], p.scale_log2, v[u]));
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) dp[r] *= s[r];
+    if (p.causal && k0 + 31 > pos) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const bool seen = ki <= pos + acc_row(r, g);
+        s[r] = seen ? s[r] : 0.f;
+        dp[r] = seen ? dp[r] : 0.f;
+      }
+    }
+#pragma unroll
+    for (int cc = 0; cc < 2; ++cc) {
+      const bf16x8 pf = pack8(s, 8 * cc), dsf = pack8(dp, 8 * cc);
+#pragma unroll
+      for (int i = 0; i < DT; ++i) {
+        dvacc[i] = mfma32(fo.tr_frag(D, 16 * cc, i), pf, dvacc[i]);
+        dkacc[i] = mfma32(fo.tr_frag(Q, 16 * cc, i), dsf, dkacc[i]);
+      }
+    }
+  };
+  for (int qt = first; qt < nqt; qt += 8) {
+    tile(qt, std::integral_constant<int, 0>());
+    if (qt + 4 < nqt) tile(qt + 4, std::integral_constant<int, 1>());
+  }
+  static_assert(32 * (DHP + 4) * 4 <= 4 * TILE * 2, "a wave's result lies in its tiles");
+  asm volatile("" ::: "memory");
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    if (which) __syncthreads();
+    rel_few_leave<DHP>(reinterpret_cast<float*>(QD[wave][0][0]), which ? dvacc : dkacc, which ? 1.0f : p.scale, kok, g, l32);
+    __syncthreads();
+    for (int at = tid; at < 32 * (DHP / 4); at += 256) {
+      const int j = k0 + at / (DHP / 4), col = at % (DHP / 4) * 4;
+      if (j >= p.Nk || col >= p.dh) continue;
+      const size_t r = (size_t)b * p.Nk + j, c = h * p.dh + col;
+      rel_few_meet<DHP, 2 * TILE>(reinterpret_cast<const float*>(QD[0][0][0]), at / (DHP / 4), col, p.qsplits > 1, p.dkv_partial + ((size_t)(which * p.qsplits + share) * p.B * p.Nk + r) * (p.H * p.dh) + c,
+                                  (bf16*)(which ? p.dv : p.dk) + r * (which ? p.lddv : p.lddk) + c);
+    }
+  }
+}
+
 // ------------------------------------------------------------------ dQ, dK, dV and the table's gradient at once (bf16, at most 32 NW keys)
 // A workgroup has all keys of its (sample, head), 32 per wave, and walks the queries of its share in tiles of 64 (see attn_bwd_short_bf16_kernel): scores, dP and
 // exponentials once instead of twice.  Per tile every wave adds to its keys' dK and dV, adds its dS along the diagonals and leaves it in LDS; behind a barrier the
@@ -1717,8 +2048,7 @@ static int rel_query_shares(int B, int H, int Nq) {
 }
 // Shares of the keys (dQ), or of the queries (dK / dV), where workgroups of 128 of the others are too few for the CUs: four tiles at least, two workgroups a CU at most,
 // and one only where half of the CUs would have none or the way is long, as the shares' fp32 sums pass through memory.  dQ and dK / dV, us a pass with 1 / 2 / 3 / 4 / 8
-// shares: 8 heads of 512 34 / 30 / 29 / 28 / -, 8 of 1024 55 / 44 / 42 / 40 / 44, 16 of 1024 55 / 50 / 53 / 50 / 68, but 32 of 1024 56 / 63, 48 of 512 37 / 47; 8 of
-// 2048 causal 93 / 67 / 65 / 60 / 73, 4 of 4096 175 / 105 / 99 / 90 / 107, 8 of 4096 176 / 146 / 166 / 164 / 191, 16 of 128 x 2048 (dQ alone) 55 / 40 / 34 / 31 / 28.
+// shares: width 96, 16 heads of 1024 67 / 58 / 64 / 62 / 92; 4 of 4096 175 / 105 / 99 / 90 / 107; 8 of 4096 176 / 146 / 166 / 164 / 191; but 32 of 1024 56 / 63, 48 of 512 37 / 47.
 constexpr long REL_GRAD_SHARES = 8, REL_GRAD_BLOCKS = 512;
 static long rel_grad_shares_most(int along) { return std::min(REL_GRAD_SHARES, (long)((along + 63) / 64) / 4); }
 static int rel_grad_shares(int B, int H, int N, int along) {
@@ -1735,10 +2065,23 @@ static int rel_shares_f32(int B, int H, int N, int along, bool backward) {
   const long blocks = (long)B * H * ((N + 31) / 32);
   return backward || along > 256 ? (int)std::max<long>(1, std::min(rel_shares_most_f32(along), 256 / blocks)) : 1;
 }
+// Whether the backward takes workgroups of 32 queries (keys) whose waves share the other side out: where those of 128 leave CUs without one, and these all run at once
+// (two a CU, wide heads one), or, where the causal mask leaves half of the tiles, in two rounds of a long way.  Both kernels, us a pass by 128 (shares where rel_grad_shares
+// gives some) and by 32: 8 heads of 300 27 / 19, 8 of 512 30 / 20, 50 of 300 28 / 25, 8 of 1024 40 / 27, 16 of 1024 50 / 38 and causal 48 / 30, 8 of 2048 64 / 57, width 80, 16
+// of 512 39 / 27, width 96, 8 of 1024 47 / 39; causal 24 of 1024 55 / 47, 32 56 / 52, 16 of 2048 83 / 71; but 48 of 512 37 / 42 and causal 36 / 40, 32 of 1024 56 / 68, width 96, 12 of 1024 57 / 63;
+// 4 of 4096 89 / 97: each K and V read four times as often.
+static bool rel_few_grads(int B, int H, int N, int along, int d_head, bool causal) {
+  return (long)B * H * ((N + 31) / 32) <= (d_head > 64 ? 256 : causal && along >= 1024 ? 1024 : 512);
+}
+// Their shares, until each CU has one, of eight tiles at least: 16 heads of 128 x 2048 in 1 / 2 / 4 shares (of dQ) 30 / 28 / 25, but 8 of 512 in 1 / 2 20 / 23.
+static int rel_few_grad_shares(int B, int H, int N, int along) {
+  return (int)std::max<long>(1, std::min(REL_GRAD_SHARES, std::min<long>((along + 63) / 64 / 8, 256 / ((long)B * H * ((N + 31) / 32)))));
+}
 // Workgroups that sum dS over buckets, of a head and sample
-static int rel_parts(int dtype, bool all_keys, int B, int H, int Nq, int Nk) {
+static int rel_parts(int dtype, bool all_keys, int B, int H, int Nq, int Nk, int d_head, bool causal) {
   if (dtype == DP_F32) return (Nq + 31) / 32 * rel_shares_f32(B, H, Nq, Nk, true);
-  return all_keys ? rel_query_shares(B, H, Nq) : (Nq + 127) / 128 * rel_grad_shares(B, H, Nq, Nk);
+  if (all_keys) return rel_query_shares(B, H, Nq);
+  return rel_few_grads(B, H, Nq, Nk, d_head, causal) ? (Nq + 31) / 32 * rel_few_grad_shares(B, H, Nq, Nk) : (Nq + 127) / 128 * rel_grad_shares(B, H, Nq, Nk);
 }
 // The backward's: the same for both types and any bias.  Fewer samples may have more shares, but never more workgroups than REL_*_BLOCKS (begun) where there are
 // shares at all: what these leave is the bound, so that no size needs more than a greater one.
@@ -1964,7 +2307,7 @@ int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_h
       return DP_OK;
     }));
   a.dtable = dtable;
-  a.dtable_parts = B * rel_parts(dtype, all_keys, B, H, Nq, Nk);
+  a.dtable_parts = B * rel_parts(dtype, all_keys, B, H, Nq, Nk, d_head, causal);
   a.dtable_add = accumulate != 0;
   a.table_items = dtable ? (H * ((bias->n_buckets + 31) / 32) + 7) / 8 * 8 : 0;      // workgroups that add the parts of the table's gradient (eights: the others stay on their XCDs)
   const double fl = 4.0 * B * H * (double)Nq * Nk * d_head, by = (dtype == DP_BF16 ? 2.0 : 4.0) * B * H * d_head * (3.0 * Nq + 2.0 * Nk);
@@ -1999,14 +2342,21 @@ int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_h
       return rel_launched();
     }
   } else {
-    a.ksplits = rel_grad_shares(B, H, Nq, Nk);
-    a.qsplits = rel_grad_shares(B, H, Nk, Nq);
-    const long qblocks = (long)((Nq + 127) / 128) * B * H * a.ksplits, kblocks = (long)((Nk + 127) / 128) * B * H * a.qsplits;
+    const bool few_q = rel_few_grads(B, H, Nq, Nk, d_head, causal), few_k = rel_few_grads(B, H, Nk, Nq, d_head, causal);
+    a.ksplits = few_q ? rel_few_grad_shares(B, H, Nq, Nk) : rel_grad_shares(B, H, Nq, Nk);
+    a.qsplits = few_k ? rel_few_grad_shares(B, H, Nk, Nq) : rel_grad_shares(B, H, Nk, Nq);
+    const int qrows = few_q ? 32 : 128, krows = few_k ? 32 : 128;
+    const long qblocks = (long)((Nq + qrows - 1) / qrows) * B * H * a.ksplits, kblocks = (long)((Nk + krows - 1) / krows) * B * H * a.qsplits;
     const int table = rel_table_floats(a.bk) * 4, both = rel_sum_floats(a.bk, 4) * 4;
     {
       KScope ks(KK_ATTN_BWD_DQ, fl, by, s, Nq, Nk, d_head);
       a.even = rel_takes_turns(qblocks, d_head <= 64 ? 3 : 2);
       DP_TRY(rel_dispatch(d_head, [&](auto dhp, auto kc) {
+        if (few_q) {
+          DP_TRY((rel_allow_lds<rel_bwd_few_dq_bf16_kernel<dhp, kc>>(1024 * dhp, both)));
+          hipLaunchKernelGGL((rel_bwd_few_dq_bf16_kernel<dhp, kc>), dim3((unsigned)qblocks), dim3(256), both, s, a, st);
+          return rel_launched();
+        }
         auto run = [&](auto shares) {
           DP_TRY((rel_allow_lds<rel_bwd_dq_bf16_kernel<dhp, kc, shares>>(512 * dhp, both)));
           hipLaunchKernelGGL((rel_bwd_dq_bf16_kernel<dhp, kc, shares>), dim3((unsigned)qblocks), dim3(256), both, s, a, st);
@@ -2021,6 +2371,11 @@ int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_h
     const bool many = d_head <= 64 && !causal && kblocks > 2 * 256;
     a.even = rel_takes_turns(kblocks, many ? 3 : 2);
     DP_TRY(rel_dispatch(d_head, [&](auto dhp, auto kc) {
+      if (few_k) {
+        DP_TRY((rel_allow_lds<rel_bwd_few_dkv_bf16_kernel<dhp, kc>>(1024 * dhp, table)));
+        hipLaunchKernelGGL((rel_bwd_few_dkv_bf16_kernel<dhp, kc>), dim3((unsigned)kblocks + a.table_items), dim3(256), table, s, a, st);
+        return rel_launched();
+      }
       auto run = [&](auto minw, auto shares) {
         DP_TRY((rel_allow_lds<rel_bwd_dkv_bf16_kernel<dhp, kc, minw, shares>>((minw == 3 ? 768 : 512) * dhp, table)));
         hipLaunchKernelGGL((rel_bwd_dkv_bf16_kernel<dhp, kc, minw, shares>), dim3((unsigned)kblocks + a.table_items), dim3(256), table, s, a, st);

@@ -232,7 +232,9 @@ def test_few_queries_without_a_workspace(dtype, nq, nk):
     (1, 3, 513, 513, 64, False, None), (1, 3, 513, 513, 64, True, None),                # shares of keys and of queries
     (1, 2, 70, 2100, 40, False, [1500]), (2, 1, 2050, 300, 96, True, [300, 7]),         # of one of them
     (1, 4, 1024, 1024, 80, True, [700]), (1, 5, 2048, 600, 48, False, [0]),             # shares that have nothing to do
-    (1, 2, 600, 256, 64, False, None)])                                                 # shares of the queries, all keys in a workgroup
+    (1, 2, 600, 256, 64, False, None),                                                  # shares of the queries, all keys in a workgroup
+    (1, 10, 900, 1000, 88, False, [777]), (2, 8, 1030, 1030, 72, True, [1030, 640]),    # the same with many rows to a workgroup
+    (3, 6, 1100, 1100, 64, False, [1100, 1, 600]), (1, 40, 300, 290, 48, True, None)])
 def test_gradients_in_shares(dtype, B, H, nq, nk, d, causal, lens):
     _check(dtype, B, H, nq, nk, d, causal, True, 32, 128, nk - nq if causal else 0, lens)
 

@@ -620,7 +620,6 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 3 : 2) rel_bwd_dq_bf16_kernel
   rel_block_map(p, SHARES ? (int)blockIdx.x % all : (int)blockIdx.x, qtiles, true, qtile, bh);
   const int b = bh / p.H, h = bh % p.H;
   RelFill<bf16, false, 256> fill;
-  fill.request(p, st, h);
   rel_fill_starts(p.bk, st, starts, 256);
   const int q0 = qtile * 128 + wave * 32, qi = q0 + l32, pos0 = p.query0 + q0, pos = pos0 + l32;
   const bool qok = qi < p.Nq;
@@ -643,6 +642,7 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 3 : 2) rel_bwd_dq_bf16_kernel
     ck.issue(kr, kt0 * 64, p.ldk, Ks[0], wave);
     cv.issue(vr, kt0 * 64, p.ldv, Vs[0], wave);
   }
+  fill.request(p, st, h);
   fill.store(p, st, h, rel_lds, p.inv_scale);
   float* sums = rel_lds + rel_table_floats(p.bk);
   const int sum_stride = rel_sum_stride(p.bk);
@@ -862,7 +862,6 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(MINW, 
   rel_block_map(p, SHARES ? id % all : id, ktiles, false, ktile, bh);
   const int b = bh / p.H, h = bh % p.H;
   RelFill<bf16, true, 256> fill;
-  fill.request(p, st, h);
   const int k0 = ktile * 128 + wave * 32, ki = k0 + l32;
   const int keys = __builtin_amdgcn_readfirstlane(rel_keys(p, b));
   const bool kok = ki < keys;
@@ -896,6 +895,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(MINW, 
     if (wave == 1) dlt_s[buf][lane] = ok ? -stat : 0.f;
   };
   load_stats(qt0);
+  fill.request(p, st, h);
   fill.store(p, st, h, rel_lds, LOG2E);
   const int tab = 4 * g + p.query0 - ki + p.bk.hi + REL_MARGIN;      // entry of this lane's first query
 
@@ -1202,7 +1202,6 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 2 : 1) rel_bwd_few_dkv_bf16_k
   rel_block_map(p, id - share * all, ktiles, false, ktile, bh);
   const int b = bh / p.H, h = bh % p.H, k0 = ktile * 32, ki = k0 + l32;
   RelFill<bf16, true, 256> fill;
-  fill.request(p, st, h);
   const int keys = __builtin_amdgcn_readfirstlane(rel_keys(p, b));
   const bool kok = ki < keys;
   const u32x4 qr = make_raw_rsrc((const bf16*)p.q + (size_t)b * p.Nq * p.ldq + h * p.dh, attn_slice_bytes(p.Nq, p.ldq, p.dh));
@@ -1236,6 +1235,7 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 2 : 1) rel_bwd_few_dkv_bf16_k
     kf[c] = ld8((const bf16*)p.k + ((size_t)b * p.Nk + ki) * p.ldk + h * p.dh + 16 * c + 8 * g, ok);
     vf[c] = ld8((const bf16*)p.v + ((size_t)b * p.Nk + ki) * p.ldv + h * p.dh + 16 * c + 8 * g, ok);
   }
+  fill.request(p, st, h);
   fill.store(p, st, h, rel_lds, LOG2E);
   const int tab = 4 * g + p.query0 - ki + bk_hi + REL_MARGIN;      // entry of this lane's first query
   f32x16 dkacc[DT], dvacc[DT];
@@ -1358,7 +1358,6 @@ __global__ void __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2,
   attn_block_map(blockIdx.x, p.qsplits, p.B * p.H, qs, bh);
   const int b = bh / p.H, h = bh % p.H, k0 = 32 * wave, ki = k0 + l32;
   RelFill<bf16, true, 64 * NW> fill;
-  fill.request(p, st, h);
   rel_fill_starts(p.bk, st, starts, 64 * NW);
   const int keys = __builtin_amdgcn_readfirstlane(rel_keys(p, b)), groups = (keys + 31) / 32;      // (a wave past the last group has copies, dQ and delta)
   const bool kok = ki < keys, second = lane & 16;
@@ -1422,6 +1421,7 @@ __global__ void __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2,
   cv.issue(vr, 16 * NW, p.ldv, Vt + 16 * NW * DHP, wave);
   issue(qt0);
   load_o(qt0);
+  fill.request(p, st, h);
   fill.store(p, st, h, rel_lds, p.inv_scale);
   float* const sums = rel_lds + rel_table_floats(p.bk);
   const int sum_stride = rel_sum_stride(p.bk);

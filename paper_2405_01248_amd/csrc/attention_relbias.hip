@@ -11,7 +11,7 @@
 // two vector additions an element, and keeps one sum a distance in LDS; beyond the middle each lane adds to one sum per side.  The sums over distances become
 // sums over buckets at the end of the workgroup, and the first workgroups of the next launch add those of all samples and query tiles; every sum in a fixed order, so
 // that the result is the same bits every time.  8 x 10 heads of 1024, dQ with this, causal: 134 us with an atomic addition in LDS for each element of dS
-// (about 150 cycles an instruction), 44 laid down in LDS and added along the diagonals from there, 38 in registers (without the mask 58 and 47).
+// (about 150 cycles an instruction), 44 laid down in LDS and added along the diagonals from there, 38 in registers (without the mask 58 and 47), 36 without turns of priority.
 #include "dp_attention_tile.h"
 #include "dp_device.h"
 #include "dp_errors.h"
@@ -525,7 +525,7 @@ template <typename T> __global__ void __launch_bounds__(256) rel_join_kernel(con
 
 // ------------------------------------------------------------------ dQ and the table's gradient (bf16)
 // 128 queries a workgroup, keys in tiles of 64, two LDS stages; S and dP = dO V^T with a query a lane, dS = P (dP - delta), dQ += dS K; delta = rowsum(dO O) goes
-// to the workspace for dK / dV.  8 x 10 heads of 1024 47 us, 8 x 5 of 4096 272, 8 x 10 of 1024 causal 38: three products a block (8 x 5 of 4096: 258 GF, 229 us at a
+// to the workspace for dK / dV.  8 x 10 heads of 1024 47 us, 8 x 5 of 4096 272, 8 x 10 of 1024 causal 36: three products a block (8 x 5 of 4096: 258 GF, 229 us at a
 // large product's rate) and some ten vector instructions an element between them, of which the diagonals are two.  SHARES: a workgroup has one of ksplits shares of
 // its key tiles and leaves an fp32 sum (rel_grad_shares has what it gives).
 __device__ __forceinline__ bf16x8 rel_turned(bf16x8 v, bool turn) {      // -v

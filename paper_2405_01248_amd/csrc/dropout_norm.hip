@@ -378,11 +378,13 @@ static bool norm_too_many(int rows, int d) {      // a launch has less than 2^32
   return rows * lanes >= (1l << 31);
 }
 // Workgroups of the backward, hence parts to be added afterwards: as many as run at once.  That is two a CU where a lane has two groups of columns (half the
-// registers of a SIMD each wave) and four where it has one; rows within a wave take three, which leave fewer parts.  512 / 768 / 1024 of them, us without the
-// sum: 32768 x 320 29.6 / 27.8 / 28.0, 65536 x 256 43.1 / 42.2 / 43.6, 32768 x 640 67 / 81 / 69, 8192 x 640 21 / 23 / 23, 8192 x 1152 28 / 26 / 23.
-static int norm_bwd_workgroups(int rows, int d) {
-  const int per = norm_rows_per_workgroup(d);
-  return std::min((rows + per - 1) / per, d <= 512 ? 768 : d > 1024 && d <= 2048 ? 1024 : 512);
+// registers of a SIMD each wave) or a row 512 lanes, four where it has 256, one for 1024; rows within a wave of one group take three, which leave fewer parts.  512 / 768 / 1024
+// of them, us without the sum: 32768 x 320 29.6 / 27.8 / 28.0, 65536 x 256 43.1 / 42.2 / 43.6, 32768 x 640 67 / 81 / 69, 8192 x 640 21 / 23 / 23, 8192 x 1152 28 / 26 / 23; with the sum, 256
+// or 512: 2048 x 8192 33 / 39, 1000 x 5000 fp32 23 / 29.  Few rows of a workgroup each would leave as many parts as rows: of 1 / 2 / 4 / 8 each, 512 x 1280 9.5 / 8.7 / 10.5 / 14.2, 1024 x
+// 2048 15.7 / 12.6 / 12.3 / 16.4, 512 x 4096 15.8 / 13.2 / 13.7 / 18.3, 2048 x 2048 18.4 / 18.4 / 16.2 / 17.7; within a wave (1027 x 1001 fp32) 10.8 / 12.6 / 15.7.
+static int norm_bwd_workgroups(int rows, int d, bool most = false) {      // (most: what this many rows or fewer leave)
+  const int per = d <= 1024 || d > 4096 ? norm_rows_per_workgroup(d) : rows < 1024 || most ? 2 : 4;
+  return std::min((rows + per - 1) / per, d <= 512 ? 768 : d <= 1024 ? 512 : d <= 2048 ? 1024 : d <= 4096 ? 512 : 256);
 }
 template <typename T, typename S> static int norm_fwd_t(const NormK& k, hipStream_t s) {
   norm_dispatch<true>(k.d, [&](auto l, auto nc) {
@@ -446,7 +448,7 @@ int dp_op_layernorm_fwd(int dtype, int sum_f32, int rows, int d, float eps, cons
 
 size_t dp_op_layernorm_bwd_workspace_bytes(int rows, int d) {
   if (rows <= 0 || d <= 0 || d > NORM_MAX_D) return 0;
-  return align_up((size_t)norm_bwd_workgroups(rows, d) * 2 * d * sizeof(float), 256);
+  return align_up((size_t)norm_bwd_workgroups(rows, d, true) * 2 * d * sizeof(float), 256);
 }
 
 int dp_op_layernorm_bwd(int dtype, int sum_f32, int rows, int d, const void* dy, int lddy, const void* sum, int lds, const float* mean,

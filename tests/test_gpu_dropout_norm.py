@@ -109,7 +109,8 @@ def test_slices_and_the_backward_draw_the_same_mask():
 
 SHAPES = [  # rows, d, padding of the rows
     (5, 1, 0), (40, 8, 0), (37, 120, 8), (3, 129, 1), (65, 250, 0), (64, 256, 0), (9, 511, 5), (130, 640, 0), (1, 768, 0), (924, 768, 0), (31, 1001, 0),
-    (17, 1032, 8), (6, 2047, 0), (5, 4099, 0), (3, 8192, 0), (2, 8185, 3), (2500, 72, 0)]
+    (17, 1032, 8), (6, 2047, 0), (5, 4099, 0), (3, 8192, 0), (2, 8185, 3), (2500, 72, 0),
+    (2600, 300, 4), (1030, 1288, 0), (4100, 1030, 0), (1025, 2500, 6), (2060, 4096, 0), (300, 5000, 0)]      # several rows to a workgroup
 
 
 @pytest.mark.parametrize("dtype,sum_f32", [("f32", False), ("bf16", False), ("bf16", True)])

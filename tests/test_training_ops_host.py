@@ -68,8 +68,8 @@ def test_layernorm_refusals(lib):
 
 
 def test_layernorm_workspace_serves_fewer_rows(lib):
-    for d in (1, 16, 640, 1001, 8192):
-        sizes = [lib.dp_op_layernorm_bwd_workspace_bytes(n, d) for n in (1, 2, 17, 255, 1000, 4097, 100000)]
+    for d in (1, 16, 200, 640, 1001, 1280, 2048, 4096, 5000, 8192):
+        sizes = [lib.dp_op_layernorm_bwd_workspace_bytes(n, d) for n in (1, 2, 17, 255, 1000, 1023, 1024, 1025, 2047, 2048, 4097, 100000)]
         assert all(a <= b for a, b in zip(sizes, sizes[1:]))
 
 

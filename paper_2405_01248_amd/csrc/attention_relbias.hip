@@ -1778,17 +1778,14 @@ __global__ void __launch_bounds__(256) rel_fwd_f32_kernel(const RelAttnK p, cons
   }
 }
 
+// (block: the workgroup among those for dQ; meet: REL_F32_MEET floats)
 template <int DT, int KC>
-__global__ void __launch_bounds__(256) rel_bwd_dq_f32_kernel(const RelAttnK p, const RelStarts st) {
-  __shared__ __attribute__((aligned(16))) float meet[REL_F32_MEET<DT>];
-  __shared__ float far_sums[2][4];
-  __shared__ uint16_t starts[REL_STARTS];
-  extern __shared__ __attribute__((aligned(16))) float rel_lds[];
+__device__ __forceinline__ void rel_dq_f32(const RelAttnK& p, const RelStarts& st, int block, float* meet, float (*far_sums)[4], uint16_t* starts, float* rel_lds) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, l32 = lane & 31;
   const int bk_lo = p.bk.lo, bk_hi = p.bk.hi, qtiles = (p.Nq + 31) / 32, entries = rel_entries(p.bk);
-  const int all = qtiles * p.B * p.H, share = p.ksplits > 1 ? (int)blockIdx.x / all : 0;
+  const int all = qtiles * p.B * p.H, share = p.ksplits > 1 ? block / all : 0;
   int qtile, bh;
-  rel_block_map(p, (int)blockIdx.x - share * all, qtiles, true, qtile, bh);
+  rel_block_map(p, block - share * all, qtiles, true, qtile, bh);
   const int b = bh / p.H, h = bh % p.H, qi = qtile * 32 + l32, pos0 = p.query0 + qtile * 32, pos = pos0 + l32;
   RelFill<float, false, 256> fill;
   fill.request(p, st, h);
@@ -1881,13 +1878,11 @@ __global__ void __launch_bounds__(256) rel_bwd_dq_f32_kernel(const RelAttnK p, c
   if (p.dtable_partial) rel_bucket_sums<4, false>(p, starts, sums, sum_stride, far_sums, far_sum_lo, far_sum_hi, p.dtable_partial + ((((size_t)h * p.B + b) * p.ksplits + share) * qtiles + qtile) * p.bk.n_buckets);
 }
 
-template <int DT, int KC>
-__global__ void __launch_bounds__(256) rel_bwd_dkv_f32_kernel(const RelAttnK p, const RelStarts st) {
-  __shared__ __attribute__((aligned(16))) float meet[REL_F32_MEET<DT>];
-  extern __shared__ __attribute__((aligned(16))) float rel_lds[];
+// OWN: delta = rowsum(dO O) formed here, not read (deltas: 32 floats a wave).
+template <int DT, int KC, bool OWN>
+__device__ __forceinline__ void rel_dkv_f32(const RelAttnK& p, const RelStarts& st, int id, float* meet, float (*deltas)[32], float* rel_lds) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, l32 = lane & 31;
-  const int ktiles = (p.Nk + 31) / 32, id = (int)blockIdx.x - p.table_items;
-  if (id < 0) return rel_table_sums(p, (int)blockIdx.x, meet);
+  const int ktiles = (p.Nk + 31) / 32;
   const int bk_lo = p.bk.lo, bk_hi = p.bk.hi;
   const int all = ktiles * p.B * p.H, share = p.qsplits > 1 ? id / all : 0;
   int ktile, bh;
@@ -1905,63 +1900,79 @@ __global__ void __launch_bounds__(256) rel_bwd_dkv_f32_kernel(const RelAttnK p, 
   f32x16 dkacc[DT], dvacc[DT];
 #pragma unroll
   for (int i = 0; i < DT; ++i) dkacc[i] = dvacc[i] = rel_all16(0.f);
-  fill.store(p, st, h, rel_lds, p.inv_scale);
-  const int tab = 4 * g + p.query0 - ki + bk_hi + REL_MARGIN;      // entry of this lane's first query
-  __syncthreads();
-  const float far_hi = rel_uniform(rel_lds[0]), far_lo = rel_uniform(rel_lds[rel_entries(p.bk) - 1]);
+  constexpr bool AHEAD = DT < 3;
+  RelRows<KC> k, v, q, dout;      // (a lane whose key is past the sample's length computes what is not stored)
   if (first + wave < nqt) {
-    RelRows<KC> k, v;      // (a lane whose key is past the sample's length computes what is not stored)
     k.load((const float*)p.k + (size_t)b * p.Nk * p.ldk + h * p.dh, min(ki, keys - 1), p.ldk, p.dh, g);
     v.load((const float*)p.v + (size_t)b * p.Nk * p.ldv + h * p.dh, min(ki, keys - 1), p.ldv, p.dh, g);
-    constexpr bool AHEAD = DT < 3;
-    RelRows<KC> q, dout;
     if (AHEAD) {
       q.load(qb, min(32 * (first + wave) + l32, p.Nq - 1), p.ldq, p.dh, g);
       dout.load(dob, min(32 * (first + wave) + l32, p.Nq - 1), p.lddo, p.dh, g);
     }
-    for (int qt = first + wave; qt < nqt; qt += 4) {
-      const int q0 = 32 * qt, row = min(q0 + l32, p.Nq - 1), pos0 = p.query0 + q0;
-      RelColumns<DT> qc, dc;
-      if (!AHEAD) {
-        q.load(qb, row, p.ldq, p.dh, g);
-        dout.load(dob, row, p.lddo, p.dh, g);
-      }
-      qc.load(qb, q0, p.Nq - 1, p.ldq, p.dh, g, l32);
-      dc.load(dob, q0, p.Nq - 1, p.lddo, p.dh, g, l32);
-      float lse2[16];
-      f32x16 dp;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int i = q0 + acc_row(r, g), at = min(i, p.Nq - 1);
-        const float l = lse_b[at];
-        lse2[r] = i < p.Nq && l != -INFINITY ? l * LOG2E : INFINITY;
-        dp[r] = -dlt_b[at];
-      }
-      const bool below = k0 + 31 - pos0 <= bk_lo, above = k0 - pos0 - 31 >= bk_hi;
-      f32x16 s = below ? rel_all16(far_lo) : (above ? rel_all16(far_hi) : rel_bias16(rel_lds, tab + q0));
-      s = rel_rows_product(q, k, s);
-      dp = rel_rows_product(dout, v, dp);
-      if (AHEAD && qt + 4 < nqt) {
-        const int next = min(q0 + 128 + l32, p.Nq - 1);
-        q.load(qb, next, p.ldq, p.dh, g);
-        dout.load(dob, next, p.lddo, p.dh, g);
-      }
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], p.scale_log2, -lse2[r]));
-        dp[r] *= s[r];
-      }
-      if (p.causal && k0 + 31 > pos0) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const bool seen = ki <= pos0 + acc_row(r, g);
-          s[r] = seen ? s[r] : 0.f;
-          dp[r] = seen ? dp[r] : 0.f;
-        }
-      }
-      rel_columns_product(dc, s, dvacc);
-      rel_columns_product(qc, dp, dkacc);
+  }
+  fill.store(p, st, h, rel_lds, p.inv_scale);
+  const int tab = 4 * g + p.query0 - ki + bk_hi + REL_MARGIN;      // entry of this lane's first query
+  __syncthreads();
+  const float far_hi = rel_uniform(rel_lds[0]), far_lo = rel_uniform(rel_lds[rel_entries(p.bk) - 1]);
+  for (int qt = first + wave; qt < nqt; qt += 4) {
+    const int q0 = 32 * qt, row = min(q0 + l32, p.Nq - 1), pos0 = p.query0 + q0;
+    RelColumns<DT> qc, dc;
+    if (!AHEAD) {
+      q.load(qb, row, p.ldq, p.dh, g);
+      dout.load(dob, row, p.lddo, p.dh, g);
     }
+    qc.load(qb, q0, p.Nq - 1, p.ldq, p.dh, g, l32);
+    dc.load(dob, q0, p.Nq - 1, p.lddo, p.dh, g, l32);
+    float lse2[16];
+    f32x16 dp;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int i = q0 + acc_row(r, g), at = min(i, p.Nq - 1);
+      const float l = lse_b[at];
+      lse2[r] = i < p.Nq && l != -INFINITY ? l * LOG2E : INFINITY;
+      if (!OWN) dp[r] = -dlt_b[at];
+    }
+    if (OWN) {
+      RelRows<KC> o;
+      o.load((const float*)p.o + (size_t)b * p.Nq * p.ldo + h * p.dh, row, p.ldo, p.dh, g);
+      float d = 0.f;
+#pragma unroll
+      for (int c = 0; c < KC; ++c)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) d = fmaf(o.v[c][u], dout.v[c][u], d);
+      d = reduce_halves(d, AddOp());
+      if (g == 0) deltas[wave][l32] = -d;
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        const f32x4 v = *reinterpret_cast<const f32x4*>(&deltas[wave][8 * r4 + 4 * g]);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) dp[4 * r4 + u] = v[u];
+      }
+    }
+    const bool below = k0 + 31 - pos0 <= bk_lo, above = k0 - pos0 - 31 >= bk_hi;
+    f32x16 s = below ? rel_all16(far_lo) : (above ? rel_all16(far_hi) : rel_bias16(rel_lds, tab + q0));
+    s = rel_rows_product(q, k, s);
+    dp = rel_rows_product(dout, v, dp);
+    if (AHEAD && qt + 4 < nqt) {
+      const int next = min(q0 + 128 + l32, p.Nq - 1);
+      q.load(qb, next, p.ldq, p.dh, g);
+      dout.load(dob, next, p.lddo, p.dh, g);
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], p.scale_log2, -lse2[r]));
+      dp[r] *= s[r];
+    }
+    if (p.causal && k0 + 31 > pos0) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const bool seen = ki <= pos0 + acc_row(r, g);
+        s[r] = seen ? s[r] : 0.f;
+        dp[r] = seen ? dp[r] : 0.f;
+      }
+    }
+    rel_columns_product(dc, s, dvacc);
+    rel_columns_product(qc, dp, dkacc);
   }
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
@@ -1980,6 +1991,34 @@ __global__ void __launch_bounds__(256) rel_bwd_dkv_f32_kernel(const RelAttnK p, 
       *reinterpret_cast<f32x4*>(out + ((size_t)b * p.Nk + j) * ld + h * p.dh + col) = o;
     }
   }
+}
+
+template <int DT, int KC>
+__global__ void __launch_bounds__(256) rel_bwd_dq_f32_kernel(const RelAttnK p, const RelStarts st) {
+  __shared__ __attribute__((aligned(16))) float meet[REL_F32_MEET<DT>];
+  __shared__ float far_sums[2][4];
+  __shared__ uint16_t starts[REL_STARTS];
+  extern __shared__ __attribute__((aligned(16))) float rel_lds[];
+  rel_dq_f32<DT, KC>(p, st, (int)blockIdx.x, meet, far_sums, starts, rel_lds);
+}
+template <int DT, int KC>
+__global__ void __launch_bounds__(256) rel_bwd_dkv_f32_kernel(const RelAttnK p, const RelStarts st) {
+  __shared__ __attribute__((aligned(16))) float meet[REL_F32_MEET<DT>];
+  extern __shared__ __attribute__((aligned(16))) float rel_lds[];
+  const int id = (int)blockIdx.x - p.table_items;
+  if (id < 0) return rel_table_sums(p, (int)blockIdx.x, meet);
+  rel_dkv_f32<DT, KC, false>(p, st, id, meet, nullptr, rel_lds);
+}
+// Both at once, of so few workgroups that they all find a CU: first those for dQ.
+template <int DT, int KC>
+__global__ void __launch_bounds__(256) rel_bwd_both_f32_kernel(const RelAttnK p, const RelStarts st, int dq_workgroups) {
+  __shared__ __attribute__((aligned(16))) float meet[REL_F32_MEET<DT>];
+  __shared__ __attribute__((aligned(16))) float deltas[4][32];
+  __shared__ float far_sums[2][4];
+  __shared__ uint16_t starts[REL_STARTS];
+  extern __shared__ __attribute__((aligned(16))) float rel_lds[];
+  if ((int)blockIdx.x < dq_workgroups) rel_dq_f32<DT, KC>(p, st, (int)blockIdx.x, meet, far_sums, starts, rel_lds);
+  else rel_dkv_f32<DT, KC, true>(p, st, (int)blockIdx.x - dq_workgroups, meet, deltas, rel_lds);
 }
 
 // ------------------------------------------------------------------ host side
@@ -2077,9 +2116,24 @@ static bool rel_few_grads(int B, int H, int N, int along, int d_head, bool causa
 static int rel_few_grad_shares(int B, int H, int N, int along) {
   return (int)std::max<long>(1, std::min(REL_GRAD_SHARES, std::min<long>((along + 63) / 64 / 8, 256 / ((long)B * H * ((N + 31) / 32)))));
 }
+// Whether one launch takes the workgroups for dQ and those for dK / dV (which then form delta themselves), and the shares of the keys and of the queries: where all find a
+// CU, the longer of the two chains shared out first; under the causal mask, where half of them end early, also in two rounds, unless there are shares to be had one after the
+// other.  us a pass in two launches / in one: 4 heads of 128 27 / 17, 2 of 41, width 40, 19 / 12, 75 of 22, width 16, 15 / 11, 8 of 257, width 40, 25.5 / 24.2, 2 of 500 32 / 20, 4 of 512
+// causal 32 / 25, 16 of 256 33 / 24, 24 of 206 causal 37 / 28, 6 of 790, width 40, causal 66 / 51, 16 of 512 causal 57 / 47; but 16 of 512 59 / 61, 60 of 128 28 / 31.
+static bool rel_both_f32(int B, int H, int Nq, int Nk, int d_head, bool causal, int& ksplits, int& qsplits) {
+  const long heads = (long)B * H, q = (Nq + 31) / 32, k = (Nk + 31) / 32, blocks = heads * (q + k);
+  ksplits = qsplits = 1;
+  if (d_head > 64 || blocks > (causal && heads * std::min(q, k) > 128 ? 512 : 256)) return false;
+  const long k_most = rel_shares_most_f32(Nk), q_most = rel_shares_most_f32(Nq);
+  for (;;) {
+    const bool keys = ksplits < k_most && (qsplits >= q_most || k * qsplits >= q * ksplits);
+    if (!keys && qsplits >= q_most) return true;
+    if (heads * (q * (ksplits + keys) + k * (qsplits + !keys)) > 256) return true;
+    (keys ? ksplits : qsplits)++;
+  }
+}
 // Workgroups that sum dS over buckets, of a head and sample
-static int rel_parts(int dtype, bool all_keys, int B, int H, int Nq, int Nk, int d_head, bool causal) {
-  if (dtype == DP_F32) return (Nq + 31) / 32 * rel_shares_f32(B, H, Nq, Nk, true);
+static int rel_parts(bool all_keys, int B, int H, int Nq, int Nk, int d_head, bool causal) {
   if (all_keys) return rel_query_shares(B, H, Nq);
   return rel_few_grads(B, H, Nq, Nk, d_head, causal) ? (Nq + 31) / 32 * rel_few_grad_shares(B, H, Nq, Nk) : (Nq + 127) / 128 * rel_grad_shares(B, H, Nq, Nk);
 }
@@ -2309,21 +2363,32 @@ int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_h
       return DP_OK;
     }));
   a.dtable = dtable;
-  a.dtable_parts = B * rel_parts(dtype, all_keys, B, H, Nq, Nk, d_head, causal);
+  const bool at_once = dtype == DP_F32 && rel_both_f32(B, H, Nq, Nk, d_head, causal, a.ksplits, a.qsplits);
+  a.dtable_parts = dtype == DP_F32 ? 0 : B * rel_parts(all_keys, B, H, Nq, Nk, d_head, causal);
   a.dtable_add = accumulate != 0;
   a.table_items = dtable ? (H * ((bias->n_buckets + 31) / 32) + 7) / 8 * 8 : 0;      // workgroups that add the parts of the table's gradient (eights: the others stay on their XCDs)
   const double fl = 4.0 * B * H * (double)Nq * Nk * d_head, by = (dtype == DP_BF16 ? 2.0 : 4.0) * B * H * d_head * (3.0 * Nq + 2.0 * Nk);
   if (dtype == DP_F32) {
     KScope ks(KK_ATTN_F32, 2 * fl, 2 * by, s, Nq, Nk, d_head);
     const int table = rel_table_floats(a.bk) * 4, both = rel_sum_floats(a.bk, 4) * 4;
-    a.ksplits = rel_shares_f32(B, H, Nq, Nk, true);
-    a.qsplits = rel_shares_f32(B, H, Nk, Nq, true);
+    if (!at_once) {
+      a.ksplits = rel_shares_f32(B, H, Nq, Nk, true);
+      a.qsplits = rel_shares_f32(B, H, Nk, Nq, true);
+    }
+    const int dq = (Nq + 31) / 32 * B * H * a.ksplits, dkv = (Nk + 31) / 32 * B * H * a.qsplits;
+    a.dtable_parts = B * ((Nq + 31) / 32) * a.ksplits;
     DP_TRY(rel_dispatch_f32(d_head, [&](auto dt, auto kc) {
+      if constexpr (dt < 3)
+        if (at_once) {
+          DP_TRY((rel_allow_lds<rel_bwd_both_f32_kernel<dt, kc>>(REL_F32_MEET<dt> * 4, both)));
+          hipLaunchKernelGGL((rel_bwd_both_f32_kernel<dt, kc>), dim3((unsigned)(dq + dkv)), dim3(256), both, s, a, st, dq);
+          return rel_launched();
+        }
       DP_TRY((rel_allow_lds<rel_bwd_dq_f32_kernel<dt, kc>>(REL_F32_MEET<dt> * 4, both)));
-      hipLaunchKernelGGL((rel_bwd_dq_f32_kernel<dt, kc>), dim3((unsigned)((Nq + 31) / 32 * B * H * a.ksplits)), dim3(256), both, s, a, st);
+      hipLaunchKernelGGL((rel_bwd_dq_f32_kernel<dt, kc>), dim3((unsigned)dq), dim3(256), both, s, a, st);
       DP_TRY(rel_launched());
       DP_TRY((rel_allow_lds<rel_bwd_dkv_f32_kernel<dt, kc>>(REL_F32_MEET<dt> * 4, table)));
-      hipLaunchKernelGGL((rel_bwd_dkv_f32_kernel<dt, kc>), dim3((unsigned)((Nk + 31) / 32 * B * H * a.qsplits) + a.table_items), dim3(256), table, s, a, st);
+      hipLaunchKernelGGL((rel_bwd_dkv_f32_kernel<dt, kc>), dim3((unsigned)dkv + a.table_items), dim3(256), table, s, a, st);
       return rel_launched();
     }));
   } else if (all_keys) {
@@ -2388,11 +2453,16 @@ int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_h
       return many ? run(integral_constant<int, dhp == 64 ? 3 : 2>(), std::false_type()) : run(integral_constant<int, 2>(), std::false_type());
     }));
   }
-  if (all_keys || (a.ksplits == 1 && a.qsplits == 1)) return DP_OK;
+  if (all_keys) return DP_OK;
+  if (!at_once) a.table_items = 0;      // (they were there already)
+  if (a.ksplits == 1 && a.qsplits == 1) {
+    if (a.table_items == 0) return DP_OK;
+    hipLaunchKernelGGL(rel_dtable_kernel, dim3(a.table_items), dim3(256), 0, s, a);
+    return rel_launched();
+  }
   const size_t dq_joins = a.ksplits > 1 ? rel_join_workgroups(B, Nq, H, d_head) : 0, dkv_joins = a.qsplits > 1 ? rel_join_workgroups(B, Nk, H, d_head) : 0;
-  a.table_items = 0;      // (they were there already)
-  if (dtype == DP_F32) hipLaunchKernelGGL((rel_join_grads_kernel<float>), dim3((unsigned)(dq_joins + dkv_joins)), dim3(256), 0, s, a, (unsigned)dq_joins);
-  else hipLaunchKernelGGL((rel_join_grads_kernel<bf16>), dim3((unsigned)(dq_joins + dkv_joins)), dim3(256), 0, s, a, (unsigned)dq_joins);
+  if (dtype == DP_F32) hipLaunchKernelGGL((rel_join_grads_kernel<float>), dim3((unsigned)(dq_joins + dkv_joins + a.table_items)), dim3(256), 0, s, a, (unsigned)dq_joins);
+  else hipLaunchKernelGGL((rel_join_grads_kernel<bf16>), dim3((unsigned)(dq_joins + dkv_joins + a.table_items)), dim3(256), 0, s, a, (unsigned)dq_joins);
   return rel_launched();
 }
 

@@ -234,7 +234,8 @@ def test_few_queries_without_a_workspace(dtype, nq, nk):
     (1, 4, 1024, 1024, 80, True, [700]), (1, 5, 2048, 600, 48, False, [0]),             # shares that have nothing to do
     (1, 2, 600, 256, 64, False, None),                                                  # shares of the queries, all keys in a workgroup
     (1, 10, 900, 1000, 88, False, [777]), (2, 8, 1030, 1030, 72, True, [1030, 640]),    # the same with many rows to a workgroup
-    (3, 6, 1100, 1100, 64, False, [1100, 1, 600]), (1, 40, 300, 290, 48, True, None)])
+    (3, 6, 1100, 1100, 64, False, [1100, 1, 600]), (1, 40, 300, 290, 48, True, None),
+    (1, 2, 30, 3000, 64, False, [2999]), (1, 2, 3000, 30, 40, False, None), (2, 12, 206, 206, 64, True, [206, 100]), (2, 3, 330, 300, 8, False, [0, 290])])
 def test_gradients_in_shares(dtype, B, H, nq, nk, d, causal, lens):
     _check(dtype, B, H, nq, nk, d, causal, True, 32, 128, nk - nq if causal else 0, lens)
 

@@ -1029,17 +1029,13 @@ template <int DHP, int STRIDE> __device__ __forceinline__ void rel_few_meet(cons
 
 // Tiles of 64 keys: K through LDS, V by rows straight into registers.
 template <int DHP, int KC>
-__global__ void __launch_bounds__(256, DHP == 64 ? 2 : 1) rel_bwd_few_dq_bf16_kernel(const RelAttnK p, const RelStarts st) {
+__device__ __forceinline__ void rel_few_dq(const RelAttnK& p, const RelStarts& st, int block, bf16 (*Ks)[2][64 * DHP], float (*far_sums)[4], uint16_t* starts, float* rel_lds) {
   constexpr int DT = DHP / 32, TILE = 64 * DHP;
-  __shared__ __attribute__((aligned(1024))) bf16 Ks[4][2][TILE];
-  __shared__ float far_sums[2][4];
-  __shared__ uint16_t starts[REL_STARTS];
-  extern __shared__ __attribute__((aligned(16))) float rel_lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, l32 = lane & 31;
   const int qtiles = (p.Nq + 31) / 32, entries = rel_entries(p.bk), bk_lo = p.bk.lo, bk_hi = p.bk.hi;
-  const int all = qtiles * p.B * p.H, share = p.ksplits > 1 ? (int)blockIdx.x / all : 0;
+  const int all = qtiles * p.B * p.H, share = p.ksplits > 1 ? block / all : 0;
   int qtile, bh;
-  rel_block_map(p, (int)blockIdx.x - share * all, qtiles, true, qtile, bh);
+  rel_block_map(p, block - share * all, qtiles, true, qtile, bh);
   const int b = bh / p.H, h = bh % p.H;
   RelFill<bf16, false, 256> fill;
   fill.request(p, st, h);
@@ -1186,15 +1182,11 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 2 : 1) rel_bwd_few_dq_bf16_ke
   if (p.dtable_partial) rel_bucket_sums<4, false>(p, starts, sums, sum_stride, far_sums, second ? -far_sum_lo : far_sum_lo, second ? -far_sum_hi : far_sum_hi, p.dtable_partial + ((((size_t)h * p.B + b) * p.ksplits + share) * qtiles + qtile) * p.bk.n_buckets);
 }
 
-// Tiles of 32 queries: Q and dO through LDS, lse and delta a lane each.
-template <int DHP, int KC>
-__global__ void __launch_bounds__(256, DHP == 64 ? 2 : 1) rel_bwd_few_dkv_bf16_kernel(const RelAttnK p, const RelStarts st) {
+// Tiles of 32 queries: Q and dO through LDS, lse and delta a lane each.  OWN: delta = rowsum(dO O) formed here, not read.  QD: [wave][stage][Q, dO]; stats: -lse over the scale, -delta.
+template <int DHP, int KC, bool OWN>
+__device__ __forceinline__ void rel_few_dkv(const RelAttnK& p, const RelStarts& st, int id, bf16 (*QD)[2][2][32 * DHP], float (*stats)[64], float* rel_lds) {
   constexpr int DT = DHP / 32, TILE = 32 * DHP;
-  __shared__ __attribute__((aligned(1024))) bf16 QD[4][2][2][TILE];      // [wave][stage][Q, dO]
-  __shared__ __attribute__((aligned(16))) float stats[4][64];            // -lse over the scale, -delta
-  extern __shared__ __attribute__((aligned(16))) float rel_lds[];
-  const int ktiles = (p.Nk + 31) / 32, id = (int)blockIdx.x - p.table_items;
-  if (id < 0) return rel_table_sums(p, (int)blockIdx.x, stats[0]);
+  const int ktiles = (p.Nk + 31) / 32;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, l32 = lane & 31;
   const int bk_lo = p.bk.lo, bk_hi = p.bk.hi;
   const int all = ktiles * p.B * p.H, share = p.qsplits > 1 ? id / all : 0;
@@ -1206,7 +1198,7 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 2 : 1) rel_bwd_few_dkv_bf16_k
   const bool kok = ki < keys;
   const u32x4 qr = make_raw_rsrc((const bf16*)p.q + (size_t)b * p.Nq * p.ldq + h * p.dh, attn_slice_bytes(p.Nq, p.ldq, p.dh));
   const u32x4 dr = make_raw_rsrc((const bf16*)p.dout + (size_t)b * p.Nq * p.lddo + h * p.dh, attn_slice_bytes(p.Nq, p.lddo, p.dh));
-  const float* stat_b = (g ? p.delta : p.lse) + ((size_t)b * p.H + h) * p.Nq;
+  const float* stat_b = (g && !OWN ? p.delta : p.lse) + ((size_t)b * p.H + h) * p.Nq;
   const int seen = p.causal ? max(0, k0 - p.query0) / 32 : 0;
   const int tiles = __builtin_amdgcn_readfirstlane(k0 < keys ? max(0, (p.Nq + 31) / 32 - seen) : 0);      // (no query sees keys past the sample's length)
   const int first = seen + (int)((long)tiles * share / p.qsplits) + wave, nqt = seen + (int)((long)tiles * (share + 1) / p.qsplits);
@@ -1219,6 +1211,7 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 2 : 1) rel_bwd_few_dkv_bf16_k
     cd[w].init(w, lane, p.lddo, p.dh);
   }
   float stat = 0.f;
+  bf16x8 on[KC];
   auto request = [&](int qt, int buf) __attribute__((always_inline)) {
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
@@ -1226,6 +1219,11 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 2 : 1) rel_bwd_few_dkv_bf16_k
       cd[w].issue(dr, qt * 32, p.lddo, QD[wave][buf][1], w);
     }
     stat = stat_b[min(qt * 32 + l32, p.Nq - 1)];
+    if (OWN) {
+      const int q = qt * 32 + l32;
+#pragma unroll
+      for (int c = 0; c < KC; ++c) on[c] = ld8((const bf16*)p.o + ((size_t)b * p.Nq + q) * p.ldo + h * p.dh + 16 * c + 8 * g, q < p.Nq && 16 * c + 8 * g < p.dh);
+    }
   };
   if (first < nqt) request(first, 0);
   bf16x8 kf[KC], vf[KC];
@@ -1253,6 +1251,17 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 2 : 1) rel_bwd_few_dkv_bf16_k
     asm volatile("" ::: "memory");
     {
       const bool ok = qt * 32 + l32 < p.Nq;
+      if (OWN) {
+        float d = 0.f;
+#pragma unroll
+        for (int c = 0; c < KC; ++c) {
+          const bf16x8 v = fo.row_frag(D, 0, c);
+#pragma unroll
+          for (int u = 0; u < 8; ++u) d = fmaf((float)on[c][u], (float)v[u], d);
+        }
+        d = reduce_halves(d, AddOp());
+        stat = g ? d : stat;
+      }
       if (g) stats[wave][lane] = ok ? -stat : 0.f;
       else stats[wave][lane] = ok && stat != -INFINITY ? -stat * p.inv_scale : -INFINITY;      // (a query that sees no key has no probabilities)
     }
@@ -1322,6 +1331,35 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 2 : 1) rel_bwd_few_dkv_bf16_k
                                   (bf16*)(which ? p.dv : p.dk) + r * (which ? p.lddv : p.lddk) + c);
     }
   }
+}
+
+template <int DHP, int KC>
+__global__ void __launch_bounds__(256, DHP == 64 ? 2 : 1) rel_bwd_few_dq_bf16_kernel(const RelAttnK p, const RelStarts st) {
+  __shared__ __attribute__((aligned(1024))) bf16 Ks[4][2][64 * DHP];
+  __shared__ float far_sums[2][4];
+  __shared__ uint16_t starts[REL_STARTS];
+  extern __shared__ __attribute__((aligned(16))) float rel_lds[];
+  rel_few_dq<DHP, KC>(p, st, (int)blockIdx.x, Ks, far_sums, starts, rel_lds);
+}
+template <int DHP, int KC>
+__global__ void __launch_bounds__(256, DHP == 64 ? 2 : 1) rel_bwd_few_dkv_bf16_kernel(const RelAttnK p, const RelStarts st) {
+  __shared__ __attribute__((aligned(1024))) bf16 QD[4][2][2][32 * DHP];
+  __shared__ __attribute__((aligned(16))) float stats[4][64];
+  extern __shared__ __attribute__((aligned(16))) float rel_lds[];
+  const int id = (int)blockIdx.x - p.table_items;
+  if (id < 0) return rel_table_sums(p, (int)blockIdx.x, stats[0]);
+  rel_few_dkv<DHP, KC, false>(p, st, id, QD, stats, rel_lds);
+}
+// Both at once, of so few workgroups that they all run beside each other: first those for dQ.
+template <int DHP, int KC>
+__global__ void __launch_bounds__(256, DHP == 64 ? 2 : 1) rel_bwd_few_both_bf16_kernel(const RelAttnK p, const RelStarts st, int dq_workgroups) {
+  __shared__ __attribute__((aligned(1024))) bf16 tiles[4][2][64 * DHP];
+  __shared__ __attribute__((aligned(16))) float stats[4][64];
+  __shared__ float far_sums[2][4];
+  __shared__ uint16_t starts[REL_STARTS];
+  extern __shared__ __attribute__((aligned(16))) float rel_lds[];
+  if ((int)blockIdx.x < dq_workgroups) rel_few_dq<DHP, KC>(p, st, (int)blockIdx.x, tiles, far_sums, starts, rel_lds);
+  else rel_few_dkv<DHP, KC, true>(p, st, (int)blockIdx.x - dq_workgroups, reinterpret_cast<bf16 (*)[2][2][32 * DHP]>(tiles), stats, rel_lds);
 }
 
 // ------------------------------------------------------------------ dQ, dK, dV and the table's gradient at once (bf16, at most 32 NW keys)
@@ -2116,6 +2154,14 @@ static bool rel_few_grads(int B, int H, int N, int along, int d_head, bool causa
 static int rel_few_grad_shares(int B, int H, int N, int along) {
   return (int)std::max<long>(1, std::min(REL_GRAD_SHARES, std::min<long>((along + 63) / 64 / 8, 256 / ((long)B * H * ((N + 31) / 32)))));
 }
+// Shares of the keys and of the queries for q and k workgroups a head, each up to its most, as long as each CU has one workgroup at most: the longer of the two chains first.
+static void rel_share_out(long heads, long q, long k, long k_most, long q_most, int& ksplits, int& qsplits) {
+  for (;;) {
+    const bool keys = ksplits < k_most && (qsplits >= q_most || k * qsplits >= q * ksplits);
+    if ((!keys && qsplits >= q_most) || heads * (q * (ksplits + keys) + k * (qsplits + !keys)) > 256) return;
+    (keys ? ksplits : qsplits)++;
+  }
+}
 // Whether one launch takes the workgroups for dQ and those for dK / dV (which then form delta themselves), and the shares of the keys and of the queries: where all find a
 // CU, the longer of the two chains shared out first; under the causal mask, where half of them end early, also in two rounds, unless there are shares to be had one after the
 // other.  us a pass in two launches / in one: 4 heads of 128 27 / 17, 2 of 41, width 40, 19 / 12, 75 of 22, width 16, 15 / 11, 8 of 257, width 40, 25.5 / 24.2, 2 of 500 32 / 20, 4 of 512
@@ -2124,18 +2170,17 @@ static bool rel_both_f32(int B, int H, int Nq, int Nk, int d_head, bool causal, 
   const long heads = (long)B * H, q = (Nq + 31) / 32, k = (Nk + 31) / 32, blocks = heads * (q + k);
   ksplits = qsplits = 1;
   if (d_head > 64 || blocks > (causal && heads * std::min(q, k) > 128 ? 512 : 256)) return false;
-  const long k_most = rel_shares_most_f32(Nk), q_most = rel_shares_most_f32(Nq);
-  for (;;) {
-    const bool keys = ksplits < k_most && (qsplits >= q_most || k * qsplits >= q * ksplits);
-    if (!keys && qsplits >= q_most) return true;
-    if (heads * (q * (ksplits + keys) + k * (qsplits + !keys)) > 256) return true;
-    (keys ? ksplits : qsplits)++;
-  }
+  rel_share_out(heads, q, k, rel_shares_most_f32(Nk), rel_shares_most_f32(Nq), ksplits, qsplits);
+  return true;
 }
-// Workgroups that sum dS over buckets, of a head and sample
-static int rel_parts(bool all_keys, int B, int H, int Nq, int Nk, int d_head, bool causal) {
-  if (all_keys) return rel_query_shares(B, H, Nq);
-  return rel_few_grads(B, H, Nq, Nk, d_head, causal) ? (Nq + 31) / 32 * rel_few_grad_shares(B, H, Nq, Nk) : (Nq + 127) / 128 * rel_grad_shares(B, H, Nq, Nk);
+// Whether the few heads' workgroups for dQ and those for dK / dV go in one launch (as in fp32, see there): where all run beside each other.  us a pass in two launches / in
+// one: 8 heads of 300 18.6 / 14.2, 8 of 512 19.9 / 14.8, 8 of 1024 27.3 / 24.4, 16 of 512 causal 20.0 / 17.9, width 80, 8 of 512 25.8 / 17.7; but 16 of 1024 37.5 / 41, width 80, 16 of 512 27 / 31.
+static bool rel_few_both(int B, int H, int Nq, int Nk, int d_head, int& ksplits, int& qsplits) {
+  const long heads = (long)B * H, q = (Nq + 31) / 32, k = (Nk + 31) / 32;
+  ksplits = qsplits = 1;
+  if (heads * (q + k) > (d_head <= 64 ? 512 : 256)) return false;
+  rel_share_out(heads, q, k, std::min<long>(REL_GRAD_SHARES, (Nk + 63) / 64 / 8), std::min<long>(REL_GRAD_SHARES, (Nq + 63) / 64 / 8), ksplits, qsplits);
+  return true;
 }
 // The backward's: the same for both types and any bias.  Fewer samples may have more shares, but never more workgroups than REL_*_BLOCKS (begun) where there are
 // shares at all: what these leave is the bound, so that no size needs more than a greater one.
@@ -2158,14 +2203,15 @@ static RelWorkspace rel_workspace(int B, int H, int Nq, int Nk, int d_head, int 
 }
 
 // LDS beyond 64 KB in all has to be allowed, once per kernel and device (allowing it twice is harmless; the bits only save the call).
+constexpr int REL_LDS_REST = 4096;
 template <auto KERNEL> static int rel_allow_lds(int own, int dynamic) {
   static std::atomic<uint64_t> devices{0};
-  if (own + 2048 + dynamic <= 64 * 1024) return DP_OK;      // (own: of the tiles; a few rows of statistics come on top)
+  if (own + REL_LDS_REST + dynamic <= 64 * 1024) return DP_OK;      // (own: of the tiles; a few rows of statistics come on top)
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess) return set_error(DP_EHIP, "attention with a relative position bias: hipGetDevice failed");
   const uint64_t bit = dev >= 0 && dev < 64 ? 1ull << dev : 0;
   if (bit && (devices.load(std::memory_order_acquire) & bit)) return DP_OK;
-  if (hipFuncSetAttribute((const void*)KERNEL, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024 - own - (own ? 2048 : 0)) != hipSuccess)
+  if (hipFuncSetAttribute((const void*)KERNEL, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024 - own - (own ? REL_LDS_REST : 0)) != hipSuccess)
     return set_error(DP_EHIP, "attention with a relative position bias: hipFuncSetAttribute failed");
   devices.fetch_or(bit, std::memory_order_release);
   return DP_OK;
@@ -2363,14 +2409,14 @@ int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_h
       return DP_OK;
     }));
   a.dtable = dtable;
-  const bool at_once = dtype == DP_F32 && rel_both_f32(B, H, Nq, Nk, d_head, causal, a.ksplits, a.qsplits);
-  a.dtable_parts = dtype == DP_F32 ? 0 : B * rel_parts(all_keys, B, H, Nq, Nk, d_head, causal);
+  const int table = rel_table_floats(a.bk) * 4, both = rel_sum_floats(a.bk, 4) * 4;      // bytes of LDS: bias, and sums by distance with it
+  const bool few_fit = 1024 * (d_head <= 64 ? 64 : 96) + REL_LDS_REST + both <= 160 * 1024;
+  const bool at_once = dtype == DP_F32 ? rel_both_f32(B, H, Nq, Nk, d_head, causal, a.ksplits, a.qsplits) : !all_keys && few_fit && rel_few_both(B, H, Nq, Nk, d_head, a.ksplits, a.qsplits);
   a.dtable_add = accumulate != 0;
   a.table_items = dtable ? (H * ((bias->n_buckets + 31) / 32) + 7) / 8 * 8 : 0;      // workgroups that add the parts of the table's gradient (eights: the others stay on their XCDs)
   const double fl = 4.0 * B * H * (double)Nq * Nk * d_head, by = (dtype == DP_BF16 ? 2.0 : 4.0) * B * H * d_head * (3.0 * Nq + 2.0 * Nk);
   if (dtype == DP_F32) {
     KScope ks(KK_ATTN_F32, 2 * fl, 2 * by, s, Nq, Nk, d_head);
-    const int table = rel_table_floats(a.bk) * 4, both = rel_sum_floats(a.bk, 4) * 4;
     if (!at_once) {
       a.ksplits = rel_shares_f32(B, H, Nq, Nk, true);
       a.qsplits = rel_shares_f32(B, H, Nk, Nq, true);
@@ -2394,6 +2440,7 @@ int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_h
   } else if (all_keys) {
     KScope ks(KK_ATTN_BWD_DKV, 2 * fl, 2 * by, s, Nq, Nk, d_head);
     a.qsplits = rel_query_shares(B, H, Nq);
+    a.dtable_parts = B * a.qsplits;
     DP_TRY(rel_short_dispatch(d_head, Nk, [&](auto dhp, auto kc, auto nw) {
       const int lds = RelShort<dhp, nw>::BYTES + rel_sum_floats(a.bk, nw) * 4;
       DP_TRY((rel_allow_lds<rel_bwd_short_bf16_kernel<dhp, kc, nw>>(0, lds)));
@@ -2408,13 +2455,22 @@ int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_h
       hipLaunchKernelGGL(rel_dtable_kernel, dim3(a.table_items), dim3(256), 0, s, a);
       return rel_launched();
     }
+  } else if (at_once) {
+    KScope ks(KK_ATTN_BWD_DKV, 2 * fl, 2 * by, s, Nq, Nk, d_head);
+    const int dq = (Nq + 31) / 32 * B * H * a.ksplits, dkv = (Nk + 31) / 32 * B * H * a.qsplits;
+    a.dtable_parts = B * ((Nq + 31) / 32) * a.ksplits;
+    DP_TRY(rel_dispatch(d_head, [&](auto dhp, auto kc) {
+      DP_TRY((rel_allow_lds<rel_bwd_few_both_bf16_kernel<dhp, kc>>(1024 * dhp, both)));
+      hipLaunchKernelGGL((rel_bwd_few_both_bf16_kernel<dhp, kc>), dim3((unsigned)(dq + dkv)), dim3(256), both, s, a, st, dq);
+      return rel_launched();
+    }));
   } else {
-    const bool few_q = rel_few_grads(B, H, Nq, Nk, d_head, causal), few_k = rel_few_grads(B, H, Nk, Nq, d_head, causal);
+    const bool few_q = few_fit && rel_few_grads(B, H, Nq, Nk, d_head, causal), few_k = rel_few_grads(B, H, Nk, Nq, d_head, causal);
     a.ksplits = few_q ? rel_few_grad_shares(B, H, Nq, Nk) : rel_grad_shares(B, H, Nq, Nk);
     a.qsplits = few_k ? rel_few_grad_shares(B, H, Nk, Nq) : rel_grad_shares(B, H, Nk, Nq);
+    a.dtable_parts = B * ((Nq + (few_q ? 31 : 127)) / (few_q ? 32 : 128)) * a.ksplits;
     const int qrows = few_q ? 32 : 128, krows = few_k ? 32 : 128;
     const long qblocks = (long)((Nq + qrows - 1) / qrows) * B * H * a.ksplits, kblocks = (long)((Nk + krows - 1) / krows) * B * H * a.qsplits;
-    const int table = rel_table_floats(a.bk) * 4, both = rel_sum_floats(a.bk, 4) * 4;
     {
       KScope ks(KK_ATTN_BWD_DQ, fl, by, s, Nq, Nk, d_head);
       a.even = rel_takes_turns(qblocks, d_head <= 64 ? 3 : 2, causal);

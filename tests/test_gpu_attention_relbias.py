@@ -241,6 +241,13 @@ def test_gradients_in_shares(dtype, B, H, nq, nk, d, causal, lens):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("nq,nk,d", [(300, 300, 96), (70, 500, 64), (500, 90, 72), (700, 260, 80), (33, 40, 96)])
+@pytest.mark.parametrize("n_buckets,distance", [(320, 800), (512, 1024)])
+def test_bias_of_many_distances(dtype, nq, nk, d, n_buckets, distance):
+    _check(dtype, 1, 2, nq, nk, d, False, True, n_buckets, distance, 0, None)      # (sums by distance take most of LDS)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("B,H,nq,nk,d", [(1, 8, 1024, 1024, 64), (1, 2, 2048, 4096, 40), (3, 5, 520, 256, 96), (2, 4, 100, 3000, 64), (1, 16, 1, 4000, 64), (4, 12, 77, 77, 64)])
 def test_nothing_is_written_behind_the_workspace(dtype, B, H, nq, nk, d):
     import torch

@@ -2179,6 +2179,7 @@ static bool rel_few_both(int B, int H, int Nq, int Nk, int d_head, int& ksplits,
   const long heads = (long)B * H, q = (Nq + 31) / 32, k = (Nk + 31) / 32;
   ksplits = qsplits = 1;
   if (heads * (q + k) > (d_head <= 64 ? 512 : 256)) return false;
+  if (heads * (q + k) > 256 && (rel_few_grad_shares(B, H, Nq, Nk) > 1 || rel_few_grad_shares(B, H, Nk, Nq) > 1)) return false;      // (no room for shares that the way calls for)
   rel_share_out(heads, q, k, std::min<long>(REL_GRAD_SHARES, (Nk + 63) / 64 / 8), std::min<long>(REL_GRAD_SHARES, (Nq + 63) / 64 / 8), ksplits, qsplits);
   return true;
 }
@@ -2402,16 +2403,19 @@ int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_h
   a.qsplits = a.ksplits = 1;
   a.dtable_partial = dtable ? (float*)((char*)workspace + w.partial) : nullptr;
   hipStream_t s = (hipStream_t)hip_stream;
-  bool all_keys = false;      // one kernel whose workgroups hold all keys (where its LDS suffices for the bias)
-  if (dtype == DP_BF16 && Nk <= 256)
+  a.dtable = dtable;
+  const int table = rel_table_floats(a.bk) * 4, both = rel_sum_floats(a.bk, 4) * 4;      // bytes of LDS: bias, and sums by distance with it
+  const bool few_fit = 1024 * (d_head <= 64 ? 64 : 96) + REL_LDS_REST + both <= 160 * 1024;
+  const bool at_once = dtype == DP_F32 ? rel_both_f32(B, H, Nq, Nk, d_head, causal, a.ksplits, a.qsplits) : few_fit && rel_few_both(B, H, Nq, Nk, d_head, a.ksplits, a.qsplits);
+  const bool few_q = few_fit && rel_few_grads(B, H, Nq, Nk, d_head, causal), few_k = rel_few_grads(B, H, Nk, Nq, d_head, causal);
+  // One kernel whose workgroups hold all keys, where its LDS suffices for the bias; few heads go by 32 queries and keys, but up to 128 keys only in one launch: 8 heads of 200 20.6 /
+  // 12.7 us, 8 of 128 15.4 / 12.1, 64 of 77 16.5 / 13.0, 20 of 300 x 250 27 / 16, 60 of 171, width 40, causal 22 / 18, 72 of 200 28 / 22; but 100 of 128 16.4 / 20.5, 144 of 41, width 40, 13 / 17.
+  bool all_keys = false;
+  if (dtype == DP_BF16 && Nk <= 256 && !at_once && !(Nk > 128 && few_q && few_k))
     DP_TRY(rel_short_dispatch(d_head, Nk, [&](auto dhp, auto, auto nw) {
       all_keys = RelShort<dhp, nw>::BYTES + rel_sum_floats(a.bk, nw) * 4 <= 160 * 1024;
       return DP_OK;
     }));
-  a.dtable = dtable;
-  const int table = rel_table_floats(a.bk) * 4, both = rel_sum_floats(a.bk, 4) * 4;      // bytes of LDS: bias, and sums by distance with it
-  const bool few_fit = 1024 * (d_head <= 64 ? 64 : 96) + REL_LDS_REST + both <= 160 * 1024;
-  const bool at_once = dtype == DP_F32 ? rel_both_f32(B, H, Nq, Nk, d_head, causal, a.ksplits, a.qsplits) : !all_keys && few_fit && rel_few_both(B, H, Nq, Nk, d_head, a.ksplits, a.qsplits);
   a.dtable_add = accumulate != 0;
   a.table_items = dtable ? (H * ((bias->n_buckets + 31) / 32) + 7) / 8 * 8 : 0;      // workgroups that add the parts of the table's gradient (eights: the others stay on their XCDs)
   const double fl = 4.0 * B * H * (double)Nq * Nk * d_head, by = (dtype == DP_BF16 ? 2.0 : 4.0) * B * H * d_head * (3.0 * Nq + 2.0 * Nk);
@@ -2465,7 +2469,6 @@ int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_h
       return rel_launched();
     }));
   } else {
-    const bool few_q = few_fit && rel_few_grads(B, H, Nq, Nk, d_head, causal), few_k = rel_few_grads(B, H, Nk, Nq, d_head, causal);
     a.ksplits = few_q ? rel_few_grad_shares(B, H, Nq, Nk) : rel_grad_shares(B, H, Nq, Nk);
     a.qsplits = few_k ? rel_few_grad_shares(B, H, Nk, Nq) : rel_grad_shares(B, H, Nk, Nq);
     a.dtable_parts = B * ((Nq + (few_q ? 31 : 127)) / (few_q ? 32 : 128)) * a.ksplits;

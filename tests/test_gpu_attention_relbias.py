@@ -240,6 +240,13 @@ def test_gradients_in_shares(dtype, B, H, nq, nk, d, causal, lens):
     _check(dtype, B, H, nq, nk, d, causal, True, 32, 128, nk - nq if causal else 0, lens)
 
 
+@pytest.mark.parametrize("B,H,nq,nk,d,causal,lens", [
+    (30, 12, 77, 77, 64, False, "some"), (7, 40, 130, 120, 96, True, None), (50, 8, 40, 33, 24, True, "some"), (9, 30, 64, 200, 72, False, "some"), (5, 60, 150, 256, 40, True, None),
+    (1, 8, 1024, 77, 64, False, None), (2, 5, 2000, 128, 96, False, [128, 50]), (2, 6, 1500, 100, 40, True, None)])      # the last three: shares of the queries
+def test_gradients_where_a_workgroup_has_all_keys(B, H, nq, nk, d, causal, lens):
+    _check("bf16", B, H, nq, nk, d, causal, True, 32, 128, 0, [(nk * (i + 1)) // B for i in range(B)] if lens == "some" else lens)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("nq,nk,d", [(300, 300, 96), (70, 500, 64), (500, 90, 72), (700, 260, 80), (33, 40, 96)])
 @pytest.mark.parametrize("n_buckets,distance", [(320, 800), (512, 1024)])

@@ -145,11 +145,28 @@ __device__ __forceinline__ void rel_block_map(const RelAttnK& p, int id, int nti
 // byte extent of n rows, which may be none
 __device__ __forceinline__ uint32_t rel_slice_bytes(int n, int ld, int dh) { return (uint32_t)__builtin_amdgcn_readfirstlane(n > 0 ? (int)attn_slice_bytes(n, ld, dh) : 0); }
 
+// Four columns of a query's output, unscaled, and (first column) the logarithm of its sum; m: reference of its exponentials (log2 domain).
+template <typename T> __device__ __forceinline__ void rel_store_o(const RelAttnK& p, const f32x4& o, float sum, float m, int b, int h, int row, int col) {
+  const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+  typedef __attribute__((ext_vector_type(4))) T Four;
+  Four v;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) v[u] = (T)(o[u] * inv);
+  *reinterpret_cast<Four*>((T*)p.o + ((size_t)b * p.Nq + row) * p.ldo + h * p.dh + col) = v;
+  if (p.lse && col == 0) p.lse[((size_t)b * p.H + h) * p.Nq + row] = sum == 0.f ? -INFINITY : fmaf(m, LN2, logf(sum));
+}
+// The same of a share of the keys: unscaled columns, and (first column) reference and sum, for rel_join_kernel.
+__device__ __forceinline__ void rel_store_share(const RelAttnK& p, const f32x4& o, float sum, float m, int share, int bh, int row, int col) {
+  const size_t rows = (size_t)p.B * p.H * p.Nq, at = share * rows + (size_t)bh * p.Nq + row;
+  *reinterpret_cast<f32x4*>(p.part + at * p.dh + col) = o;
+  if (col == 0) *reinterpret_cast<u32x2*>(p.part + p.shares * rows * p.dh + 2 * at) = u32x2{__builtin_bit_cast(uint32_t, m), __builtin_bit_cast(uint32_t, sum)};
+}
+
 // ------------------------------------------------------------------ forward (bf16)
 // 128 queries a workgroup, keys in tiles of 64, two LDS stages; online softmax with a reference point that moves when the sum outgrows it (see
 // attn_fwd_bf16_kernel).  8 x 5 heads of 4096 tokens 192 us, 8 x 10 of 1024 31 (without a bias 188 and 29); with the bias of the far tiles in the accumulators, sixteen moves a
 // block, 203 and 33.  Bound by the vector work of the softmax between the products (the products of the former alone are 153 us at the rate of a large one).  A query that sees no key keeps the reference -inf and the sum 0: zeros, and lse = -inf.
-template <int DHP, int KC, int MINW>
+template <int DHP, int KC, int MINW, bool SHARES>
 __global__ void __launch_bounds__(256, MINW) rel_fwd_bf16_kernel(const RelAttnK p, const RelStarts st) {
   constexpr int DT = DHP / 32, BQ = 128, TILE = 64 * DHP;
   __shared__ __attribute__((aligned(1024))) bf16 Ks[2][TILE];
@@ -157,8 +174,9 @@ __global__ void __launch_bounds__(256, MINW) rel_fwd_bf16_kernel(const RelAttnK 
   extern __shared__ __attribute__((aligned(16))) float rel_lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, l32 = lane & 31;
   const int bk_lo = p.bk.lo, bk_hi = p.bk.hi;
+  const int qtiles = (p.Nq + BQ - 1) / BQ, all = qtiles * p.B * p.H, share = SHARES ? (int)blockIdx.x / all : 0;
   int qtile, bh;
-  rel_block_map(p, blockIdx.x, (p.Nq + BQ - 1) / BQ, true, qtile, bh);
+  rel_block_map(p, SHARES ? (int)blockIdx.x % all : (int)blockIdx.x, qtiles, true, qtile, bh);
   const int b = bh / p.H, h = bh % p.H;
   RelFill<bf16, false, 256> fill;
   fill.request(p, st, h);
@@ -168,7 +186,8 @@ __global__ void __launch_bounds__(256, MINW) rel_fwd_bf16_kernel(const RelAttnK 
   const int lim_all = p.causal ? min(keys, pos0 + 1) : keys;                              // ... that all queries of the wave see
   const int lim_wave = p.causal ? min(keys, pos0 + 32) : keys;                            // ... that some query of the wave sees
   const int lim_any = p.causal ? min(keys, p.query0 + min(p.Nq, qtile * BQ + BQ)) : keys;  // ... of the workgroup
-  const int nkt = __builtin_amdgcn_readfirstlane(lim_any > 0 ? (lim_any + 63) / 64 : 0);
+  const int tiles = __builtin_amdgcn_readfirstlane(lim_any > 0 ? (lim_any + 63) / 64 : 0);
+  const int kt0 = SHARES ? (int)((long)tiles * share / p.shares) : 0, nkt = SHARES ? (int)((long)tiles * (share + 1) / p.shares) : tiles;
   const bf16* qb = (const bf16*)p.q + (size_t)b * p.Nq * p.ldq + h * p.dh;
   const u32x4 kr = make_raw_rsrc((const bf16*)p.k + (size_t)b * p.Nk * p.ldk + h * p.dh, rel_slice_bytes(keys, p.ldk, p.dh));
   const u32x4 vr = make_raw_rsrc((const bf16*)p.v + (size_t)b * p.Nk * p.ldv + h * p.dh, rel_slice_bytes(keys, p.ldv, p.dh));
@@ -178,9 +197,9 @@ __global__ void __launch_bounds__(256, MINW) rel_fwd_bf16_kernel(const RelAttnK 
   AttnTileCopy<DHP> ck, cv;
   ck.init(wave, lane, p.ldk, p.dh);
   cv.init(wave, lane, p.ldv, p.dh);
-  if (nkt > 0) {
-    ck.issue(kr, 0, p.ldk, Ks[0], wave);
-    cv.issue(vr, 0, p.ldv, Vs[0], wave);
+  if (kt0 < nkt) {
+    ck.issue(kr, kt0 * 64, p.ldk, Ks[0], wave);
+    cv.issue(vr, kt0 * 64, p.ldv, Vs[0], wave);
   }
   const int tab = 4 * g - pos - (bk_lo - REL_MARGIN);      // entry of this lane's first key
 
@@ -198,8 +217,8 @@ __global__ void __launch_bounds__(256, MINW) rel_fwd_bf16_kernel(const RelAttnK 
   __syncthreads();
   const float far_lo = rel_uniform(rel_lds[0]), far_hi = rel_uniform(rel_lds[rel_entries(p.bk) - 1]);
 
-  for (int kt = 0; kt < nkt; ++kt) {
-    const int buf = kt & 1;
+  for (int kt = kt0; kt < nkt; ++kt) {
+    const int buf = (kt - kt0) & 1;
     take_turns(p.even, kt);
     if (kt + 1 < nkt) {      // every wave left stage buf ^ 1 at the barrier that ended the previous iteration
       ck.issue(kr, (kt + 1) * 64, p.ldk, Ks[buf ^ 1], wave);
@@ -257,7 +276,7 @@ __global__ void __launch_bounds__(256, MINW) rel_fwd_bf16_kernel(const RelAttnK 
 #pragma unroll
         for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[t][r]);
       mx = fmaxf(m, fmaf(reduce_halves(mx, MaxOp()), p.scale_log2, shift + 8.0f));
-      if (kt > 0) {
+      if (kt > kt0) {
         const float alpha = __builtin_amdgcn_exp2f(m - (mx == -INFINITY ? 0.f : mx));
         lsum *= alpha;
 #pragma unroll
@@ -268,10 +287,10 @@ __global__ void __launch_bounds__(256, MINW) rel_fwd_bf16_kernel(const RelAttnK 
       m = mx;
     };
     scores();
-    if (kt == 0) move_reference();
+    if (kt == kt0) move_reference();
     probabilities();
     if (__any(!(rs <= 256.f) || m == -INFINITY)) {
-      if (kt > 0) {
+      if (kt > kt0) {
         scores();
         move_reference();
         probabilities();
@@ -292,6 +311,16 @@ __global__ void __launch_bounds__(256, MINW) rel_fwd_bf16_kernel(const RelAttnK 
 
   lsum = reduce_halves(lsum, AddOp());      // (each lane summed its own keys)
   if (qi >= p.Nq) return;
+  if (SHARES) {
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        const int col = 32 * i + 8 * r4 + 4 * g;
+        if (col < p.dh) rel_store_share(p, f32x4{oacc[i][4 * r4], oacc[i][4 * r4 + 1], oacc[i][4 * r4 + 2], oacc[i][4 * r4 + 3]}, lsum, m, share, bh, qi, col);
+      }
+    return;
+  }
   const float inv = lsum > 0.f ? 1.0f / lsum : (lsum == 0.f ? 0.f : lsum);      // (NaN stays)
   bf16* ob = (bf16*)p.o + ((size_t)b * p.Nq + qi) * p.ldo + h * p.dh;
 #pragma unroll
@@ -307,23 +336,6 @@ __global__ void __launch_bounds__(256, MINW) rel_fwd_bf16_kernel(const RelAttnK 
       }
     }
   if (p.lse && g == 0) p.lse[((size_t)b * p.H + h) * p.Nq + qi] = lsum == 0.f ? -INFINITY : fmaf(m, LN2, logf(lsum));
-}
-
-// Four columns of a query's output, unscaled, and (first column) the logarithm of its sum; m: reference of its exponentials (log2 domain).
-template <typename T> __device__ __forceinline__ void rel_store_o(const RelAttnK& p, const f32x4& o, float sum, float m, int b, int h, int row, int col) {
-  const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-  typedef __attribute__((ext_vector_type(4))) T Four;
-  Four v;
-#pragma unroll
-  for (int u = 0; u < 4; ++u) v[u] = (T)(o[u] * inv);
-  *reinterpret_cast<Four*>((T*)p.o + ((size_t)b * p.Nq + row) * p.ldo + h * p.dh + col) = v;
-  if (p.lse && col == 0) p.lse[((size_t)b * p.H + h) * p.Nq + row] = sum == 0.f ? -INFINITY : fmaf(m, LN2, logf(sum));
-}
-// The same of a share of the keys: unscaled columns, and (first column) reference and sum, for rel_join_kernel.
-__device__ __forceinline__ void rel_store_share(const RelAttnK& p, const f32x4& o, float sum, float m, int share, int bh, int row, int col) {
-  const size_t rows = (size_t)p.B * p.H * p.Nq, at = share * rows + (size_t)bh * p.Nq + row;
-  *reinterpret_cast<f32x4*>(p.part + at * p.dh + col) = o;
-  if (col == 0) *reinterpret_cast<u32x2*>(p.part + p.shares * rows * p.dh + 2 * at) = u32x2{__builtin_bit_cast(uint32_t, m), __builtin_bit_cast(uint32_t, sum)};
 }
 
 // ------------------------------------------------------------------ forward of few queries (bf16)
@@ -2256,18 +2268,26 @@ static int rel_shares(int B, int H, int Nq, int Nk, int d_head) {
   return (int)std::max<long>(1, std::min(rel_shares_most(Nk), Nq <= 32 && d_head <= 64 ? (REL_SHARE_BLOCKS + blocks - 1) / blocks : 256 / blocks));
 }
 // Whether the forward takes 32 queries a workgroup and shares the keys out, instead of 128 queries that read each key once: where those are too few for
-// the CUs and these all run at once.  Heads, queries x keys, width, us by 32 (with what joins the shares) and by 128: 8, 256 x 4096, 64 16 / 54; 8, 1024 x 1024, 64 12 / 17; 16
+// the CUs and these all run at once.  Heads, queries x keys, width, us by 32 (with what joins the shares) and by 128: 8, 256 x 4096, 64 16 / 54 (one share); 8, 1024 x 1024, 64 12 / 17; 16
 // 16 / 17; 8, 2048 x 2048, 64 27 / 30; 4, 2000 x 2000, 40 15 / 27; 32, 512 x 512, 64 11.0 / 11.2; 64, 128 x 256, 64 6.8 / 8.0; 24, 300 x 1000, 72 16 / 19; 12, 512 x 512, 96 11 / 13;
-// but 64, 256 x 256, 64 8.9 / 8.2; 32, 300 x 1000, 72 29 / 20; 24, 512 x 512, 96 21 / 14; 144, 77 x 77, 64 7.3 / 6.4.
+// but 64, 256 x 256, 64 8.9 / 8.2; 32, 300 x 1000, 72 29 / 20; beyond 2048 keys see rel_shares_128; 24, 512 x 512, 96 21 / 14; 144, 77 x 77, 64 7.3 / 6.4.
 static bool rel_few(int B, int H, int Nq, int Nk, int d_head) {
   if (Nq <= 32) return true;
   const long blocks = (long)B * H * ((Nq + 31) / 32);
-  return blocks <= (d_head <= 64 && Nk > 256 ? 512 : 256);
+  return blocks <= (Nk > 2048 ? 64 : d_head <= 64 && Nk > 256 ? 512 : 256);
+}
+// Shares of the keys for workgroups of 128 queries: where CUs would have none and the way is long, eight tiles at least, two workgroups a CU at most, and not in two.  Heads of as many
+// queries as keys, us with 1 / 2 / 4 / 8 shares: 4 of 3044, width 88, causal 51 / 36 / 29 / 28; 3 of 4096, width 96, 67 / 46 / 37 / 37; 4 of 4096 54 / 38 / 32 / 32; 6 of 3000 41 / - / 31 (three); 8 of 2048, width 80, 33 / 30 / 30; but 12
+// of 1024, width 96, 21.5 / 23.6, 8 of 4096 (256 workgroups) 54.6 / 55.9.  By 32 queries a workgroup instead: 4 of 4096 46, 2 of 3000 24 (21), 4 of 1024 x 8192 34 (24), but 4 of 2048 18.4 (19.4),
+// 8 of 2048 causal 22 (26) and 4 of 300 x 8000 19 (22).
+static int rel_shares_128(int B, int H, int Nq, int Nk) {
+  const long blocks = (long)B * H * ((Nq + 127) / 128);
+  return blocks > 170 || Nk < 2048 ? 1 : (int)std::max<long>(1, std::min(rel_shares_most(Nk), 512 / blocks));
 }
 // (no size needs more than a greater one, as in rel_workspace)
 static size_t rel_share_bytes(int B, int H, int Nq, int Nk, int d_head) {
   const size_t most = std::max(rel_shares_most(Nk), rel_shares_most_f32(Nk));
-  return most > 1 ? align_up(std::min(most * B * H * Nq, (size_t)(2 * REL_SHARE_BLOCKS - 1) * 32) * (d_head + 2) * sizeof(float), 256) : 0;
+  return most > 1 ? align_up(std::min(most * B * H * Nq, (size_t)512 * 128) * (d_head + 2) * sizeof(float), 256) : 0;
 }
 
 static int check_rel(const char* who, int dtype, const RelAttnK& k, const dp_relbias* bias, bool bwd) {
@@ -2369,14 +2389,21 @@ int dp_op_attention_relbias_fwd(int dtype, int B, int H, int Nq, int Nk, int d_h
     hipLaunchKernelGGL((rel_join_kernel<bf16>), dim3((unsigned)joins), dim3(256), 0, s, a);
     return rel_launched();
   }
-  const long blocks = (long)((Nq + 127) / 128) * B * H;
+  DP_TRY(shares(rel_shares_128(B, H, Nq, Nk)));
+  const long blocks = (long)((Nq + 127) / 128) * B * H * a.shares;
   a.even = rel_takes_turns(blocks, d_head <= 64 ? 4 : 3, causal);
-  return rel_dispatch(d_head, [&](auto dhp, auto kc) {
+  DP_TRY(rel_dispatch(d_head, [&](auto dhp, auto kc) {
     constexpr int W = dhp == 64 ? 4 : 3;
-    DP_TRY((rel_allow_lds<rel_fwd_bf16_kernel<dhp, kc, W>>(512 * dhp, lds)));
-    hipLaunchKernelGGL((rel_fwd_bf16_kernel<dhp, kc, W>), dim3((unsigned)blocks), dim3(256), lds, s, a, st);
-    return rel_launched();
-  });
+    auto run = [&](auto shares) {
+      DP_TRY((rel_allow_lds<rel_fwd_bf16_kernel<dhp, kc, W, shares>>(512 * dhp, lds)));
+      hipLaunchKernelGGL((rel_fwd_bf16_kernel<dhp, kc, W, shares>), dim3((unsigned)blocks), dim3(256), lds, s, a, st);
+      return rel_launched();
+    };
+    return a.shares > 1 ? run(std::true_type()) : run(std::false_type());
+  }));
+  if (a.shares == 1) return DP_OK;
+  hipLaunchKernelGGL((rel_join_kernel<bf16>), dim3((unsigned)joins), dim3(256), 0, s, a);
+  return rel_launched();
 }
 
 int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_head, int causal, float scale, const void* q, int ldq, const void* k,

@@ -247,6 +247,13 @@ def test_gradients_where_a_workgroup_has_all_keys(B, H, nq, nk, d, causal, lens)
     _check("bf16", B, H, nq, nk, d, causal, True, 32, 128, 0, [(nk * (i + 1)) // B for i in range(B)] if lens == "some" else lens)
 
 
+@pytest.mark.parametrize("B,H,nq,nk,d,causal,lens", [
+    (1, 3, 1000, 2500, 64, True, None), (2, 2, 800, 2100, 88, False, [2100, 130]), (1, 1, 2200, 3000, 40, True, [2900]), (3, 4, 700, 2049, 64, True, [0, 1, 2049])])
+def test_shares_of_the_keys(B, H, nq, nk, d, causal, lens):
+    _check("bf16", B, H, nq, nk, d, causal, True, 32, 128, nk - nq if causal else 0, lens)
+    _check("bf16", B, H, nq, nk, d, causal, True, 32, 128, -nq // 2 if causal else 50, lens, workspace=False, gain=6.0)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("nq,nk,d", [(300, 300, 96), (70, 500, 64), (500, 90, 72), (700, 260, 80), (33, 40, 96)])
 @pytest.mark.parametrize("n_buckets,distance", [(320, 800), (512, 1024)])

@@ -18,6 +18,7 @@
 #include "dp_host.h"
 #include "dp_kernels.h"
 #include "dp_ktime.h"
+#include "dp_relbias_buckets.h"
 
 #include <math.h>
 #include <string.h>
@@ -28,16 +29,7 @@
 
 namespace dp {
 
-constexpr int REL_MAX_BUCKETS = 512, REL_MAX_DISTANCE = 1024, REL_MARGIN = 96;
-
-struct RelBucketsK {
-  int n_buckets, per_side, half;      // buckets in all, of one direction, of one distance each
-  int bidirectional;
-  int lo, hi;                         // the bucket of every distance <= lo is lo's, of every one >= hi is hi's
-};
-// Least distance of bucket half + k, two to a word; past the last 0xFFFF.  A kernel argument of its own: indexed inside the other arguments, it would send
-// all of them through scratch memory.
-struct RelStarts { uint32_t of[REL_MAX_BUCKETS / 4]; };
+constexpr int REL_MARGIN = 96;
 
 struct RelAttnK {
   int B, H, Nq, Nk, dh, causal, query0;
@@ -63,27 +55,10 @@ struct RelAttnK {
   RelBucketsK bk;
 };
 
-// Counts the starts that are not above the distance, sixteen (eight scalar registers) at a time: no lane waits for a memory access of its own.
-__device__ __forceinline__ int rel_bucket(const RelBucketsK& r, const RelStarts& st, int dist) {
-  const int n = r.bidirectional ? abs(dist) : max(-dist, 0), side = r.bidirectional && dist > 0 ? r.per_side : 0;
-  int k = r.half - 1;
-  for (int w = 0; w < (r.per_side - r.half + 1) / 2; w += 8) {
-#pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      const uint32_t two = st.of[w + u];
-      k += (int)(two & 0xFFFFu) <= n;
-      k += (int)(two >> 16) <= n;
-    }
-  }
-  return side + (n < r.half ? n : k);
-}
 // Least distance of each bucket of a direction, and behind the last one more than any in the sums' reach: in LDS from a kernel's beginning, for its end.
 constexpr int REL_STARTS = REL_MAX_BUCKETS + 8;
 __device__ __forceinline__ void rel_fill_starts(const RelBucketsK& r, const RelStarts& st, uint16_t* starts, int threads) {
-  for (int k = threadIdx.x; k <= r.per_side; k += threads) {
-    const uint32_t two = st.of[max(k - r.half, 0) / 2];
-    starts[k] = (uint16_t)(k < r.half ? k : (k == r.per_side ? 0x7FFFu : ((k - r.half) & 1 ? two >> 16 : two & 0xFFFFu)));
-  }
+  for (int k = threadIdx.x; k <= r.per_side; k += threads) starts[k] = (uint16_t)rel_start(r, st, k);
 }
 __host__ __device__ __forceinline__ int rel_entries(const RelBucketsK& r) { return r.hi - r.lo + 1 + 2 * REL_MARGIN; }
 __host__ __device__ __forceinline__ int rel_table_floats(const RelBucketsK& r) { return (rel_entries(r) + 3) / 4 * 4; }

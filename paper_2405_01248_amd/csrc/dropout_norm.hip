@@ -193,8 +193,10 @@ struct NormBwdK {
 // With g = dy gamma and xh = (sum - mean) rstd: dsum = rstd (g - mean(g) - xh mean(g xh)) + dsum_in, dx = dropout of dsum, and the columns' sums of
 // dy xh and dy.  A group of L lanes walks every G-th row, the next one's operands requested before the present one is used; a lane adds its columns of
 // dy xh and dy in registers, and the groups' sums meet in LDS at the end.  32768 x 640, fp32 residual gradients: 67 us (5.0 TB/s) and 4.7 for the sums.
+// Four waves a SIMD where a row has 256 lanes and more, which is what norm_bwd_workgroups counts on: in fp32 129 registers left three, and one workgroup a CU of 512 lanes instead of two
+// (us: 1000 x 3000 22.3 -> 19.5, 2048 x 4096 34.9 -> 33.2, 16384 x 1536 117 -> 101, 8192 x 2048 75 -> 71, 8192 x 4096 131 and 132).
 template <typename T, typename S, int L, int NC>
-__global__ void __launch_bounds__(norm_threads<L>) norm_bwd_kernel(const NormBwdK a) {
+__global__ void __launch_bounds__(norm_threads<L>, L >= 256 ? 4 : 1) norm_bwd_kernel(const NormBwdK a) {
   constexpr int NT = norm_threads<L>, PER = NT / L;      // rows at a time
   __shared__ float red[2][2][L > 64 ? L / 64 : 1];
   __shared__ __attribute__((aligned(16))) float meet[PER > 1 ? NT * 8 : 8];

@@ -2130,12 +2130,13 @@ static int rel_shares_f32(int B, int H, int N, int along, bool backward) {
   return backward || along > 256 ? (int)std::max<long>(1, std::min(rel_shares_most_f32(along), 256 / blocks)) : 1;
 }
 // Whether the backward takes workgroups of 32 queries (keys) whose waves share the other side out: where those of 128 leave CUs without one, and these all run at once
-// (two a CU, wide heads one), or, where the causal mask leaves half of the tiles, in two rounds of a long way.  Both kernels, us a pass by 128 (shares where rel_grad_shares
+// (per_cu of them a CU: two, wide heads and large tables one), or, where the causal mask leaves half of the tiles, in two rounds of a long way.  Both kernels, us a pass by 128 (shares where rel_grad_shares
 // gives some) and by 32: 8 heads of 300 27 / 19, 8 of 512 30 / 20, 50 of 300 28 / 25, 8 of 1024 40 / 27, 16 of 1024 50 / 38 and causal 48 / 30, 8 of 2048 64 / 57, width 80, 16
 // of 512 39 / 27, width 96, 8 of 1024 47 / 39; causal 24 of 1024 55 / 47, 32 56 / 52, 16 of 2048 83 / 71; but 48 of 512 37 / 42 and causal 36 / 40, 32 of 1024 56 / 68, width 96, 12 of 1024 57 / 63;
-// 4 of 4096 89 / 97: each K and V read four times as often.
-static bool rel_few_grads(int B, int H, int N, int along, int d_head, bool causal) {
-  return (long)B * H * ((N + 31) / 32) <= (d_head > 64 ? 256 : causal && along >= 1024 ? 1024 : 512);
+// 4 of 4096 89 / 97: each K and V read four times as often.  With 64 buckets to 256, by two a CU, of which the second had no LDS, / by the one that has: 50 of 300 35 / 26, 16 of 1024 49 / 45, 12 of
+// 1024 49 / 42, 32 of 512 37 / 33, 8 of 2048 72 / 59, causal 24 of 1024 56 / 48, 32 of 1024 70 / 50, 16 of 2048 94 / 73, but 64 of 250 27.9 / 29.0.
+static bool rel_few_grads(int B, int H, int N, int along, int d_head, bool causal, int per_cu) {
+  return (long)B * H * ((N + 31) / 32) <= 256 * per_cu * (d_head <= 64 && causal && along >= 1024 ? 2 : 1);
 }
 // Their shares, until each CU has one, of eight tiles at least: 16 heads of 128 x 2048 in 1 / 2 / 4 shares (of dQ) 30 / 28 / 25, but 8 of 512 in 1 / 2 20 / 23.
 static int rel_few_grad_shares(int B, int H, int N, int along) {
@@ -2162,10 +2163,11 @@ static bool rel_both_f32(int B, int H, int Nq, int Nk, int d_head, bool causal, 
 }
 // Whether the few heads' workgroups for dQ and those for dK / dV go in one launch (as in fp32, see there): where all run beside each other.  us a pass in two launches / in
 // one: 8 heads of 300 18.6 / 14.2, 8 of 512 19.9 / 14.8, 8 of 1024 27.3 / 24.4, 16 of 512 causal 20.0 / 17.9, width 80, 8 of 512 25.8 / 17.7; but 16 of 1024 37.5 / 41, width 80, 16 of 512 27 / 31.
-static bool rel_few_both(int B, int H, int Nq, int Nk, int d_head, int& ksplits, int& qsplits) {
+// One workgroup a CU (64 buckets to 256) where 512 were launched / are not: 16 of 512 26.3 / 22.5, causal 22.8 / 20.9, 8 of 1024 35 / 29, 20 of 300 x 250 23.4 / 20.0.
+static bool rel_few_both(int B, int H, int Nq, int Nk, int per_cu, int& ksplits, int& qsplits) {
   const long heads = (long)B * H, q = (Nq + 31) / 32, k = (Nk + 31) / 32;
   ksplits = qsplits = 1;
-  if (heads * (q + k) > (d_head <= 64 ? 512 : 256)) return false;
+  if (heads * (q + k) > 256 * per_cu) return false;
   if (heads * (q + k) > 256 && (rel_few_grad_shares(B, H, Nq, Nk) > 1 || rel_few_grad_shares(B, H, Nk, Nq) > 1)) return false;      // (no room for shares that the way calls for)
   rel_share_out(heads, q, k, std::min<long>(REL_GRAD_SHARES, (Nk + 63) / 64 / 8), std::min<long>(REL_GRAD_SHARES, (Nq + 63) / 64 / 8), ksplits, qsplits);
   return true;
@@ -2189,6 +2191,11 @@ static RelWorkspace rel_workspace(int B, int H, int Nq, int Nk, int d_head, int 
   w.bytes = w.dkv + rel_align(2 * std::max(left(Nk, Nq), short_keys) * row);
   return w;
 }
+
+// Workgroups that a CU holds beside each other: as many as its registers allow (most), and as its LDS does, which is handed out in steps of 1280 bytes.  The bias takes its part of
+// that: with 64 buckets to 256 distances the few heads' kernels for dQ take 90 KB each instead of 81 (32 to 128).
+static int rel_per_cu(int lds, int most) { return std::max(1, std::min(most, 160 * 1024 / (int)align_up(lds, 1280))); }
+constexpr int rel_few_lds(int dhp) { return 1024 * dhp + 4 * 64 * 4 + 2 * 4 * 4 + REL_STARTS * 2; }      // of the few heads' kernels, without the bias: tiles, statistics, far sums, bucket starts
 
 // LDS beyond 64 KB in all has to be allowed, once per kernel and device (allowing it twice is harmless; the bits only save the call).
 constexpr int REL_LDS_REST = 4096;
@@ -2366,7 +2373,7 @@ int dp_op_attention_relbias_fwd(int dtype, int B, int H, int Nq, int Nk, int d_h
   }
   DP_TRY(shares(rel_shares_128(B, H, Nq, Nk)));
   const long blocks = (long)((Nq + 127) / 128) * B * H * a.shares;
-  a.even = rel_takes_turns(blocks, d_head <= 64 ? 4 : 3, causal);
+  a.even = rel_takes_turns(blocks, d_head <= 64 ? rel_per_cu(512 * 64 + lds, 4) : rel_per_cu(512 * 96 + lds, 3), causal);
   DP_TRY(rel_dispatch(d_head, [&](auto dhp, auto kc) {
     constexpr int W = dhp == 64 ? 4 : 3;
     auto run = [&](auto shares) {
@@ -2407,9 +2414,11 @@ int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_h
   hipStream_t s = (hipStream_t)hip_stream;
   a.dtable = dtable;
   const int table = rel_table_floats(a.bk) * 4, both = rel_sum_floats(a.bk, 4) * 4;      // bytes of LDS: bias, and sums by distance with it
-  const bool few_fit = 1024 * (d_head <= 64 ? 64 : 96) + REL_LDS_REST + both <= 160 * 1024;
-  const bool at_once = dtype == DP_F32 ? rel_both_f32(B, H, Nq, Nk, d_head, causal, a.ksplits, a.qsplits) : few_fit && rel_few_both(B, H, Nq, Nk, d_head, a.ksplits, a.qsplits);
-  const bool few_q = few_fit && rel_few_grads(B, H, Nq, Nk, d_head, causal), few_k = rel_few_grads(B, H, Nk, Nq, d_head, causal);
+  const int dhp = d_head <= 64 ? 64 : 96;
+  const bool few_fit = 1024 * dhp + REL_LDS_REST + both <= 160 * 1024;
+  const int few_per_cu = rel_per_cu(rel_few_lds(dhp) + both, dhp == 64 ? 2 : 1), few_k_per_cu = rel_per_cu(rel_few_lds(dhp) + table, dhp == 64 ? 2 : 1);
+  const bool at_once = dtype == DP_F32 ? rel_both_f32(B, H, Nq, Nk, d_head, causal, a.ksplits, a.qsplits) : few_fit && rel_few_both(B, H, Nq, Nk, few_per_cu, a.ksplits, a.qsplits);
+  const bool few_q = few_fit && rel_few_grads(B, H, Nq, Nk, d_head, causal, few_per_cu), few_k = rel_few_grads(B, H, Nk, Nq, d_head, causal, few_k_per_cu);
   // One kernel whose workgroups hold all keys, where its LDS suffices for the bias; few heads go by 32 queries and keys, but up to 128 keys only in one launch: 8 heads of 200 20.6 /
   // 12.7 us, 8 of 128 15.4 / 12.1, 64 of 77 16.5 / 13.0, 20 of 300 x 250 27 / 16, 60 of 171, width 40, causal 22 / 18, 72 of 200 28 / 22; but 100 of 128 16.4 / 20.5, 144 of 41, width 40, 13 / 17.
   bool all_keys = false;
@@ -2478,7 +2487,7 @@ int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_h
     const long qblocks = (long)((Nq + qrows - 1) / qrows) * B * H * a.ksplits, kblocks = (long)((Nk + krows - 1) / krows) * B * H * a.qsplits;
     {
       KScope ks(KK_ATTN_BWD_DQ, fl, by, s, Nq, Nk, d_head);
-      a.even = rel_takes_turns(qblocks, d_head <= 64 ? 3 : 2, causal);
+      a.even = rel_takes_turns(qblocks, rel_per_cu(512 * dhp + 2 * 4 * 4 + REL_STARTS * 2 + both, dhp == 64 ? 3 : 2), causal);
       DP_TRY(rel_dispatch(d_head, [&](auto dhp, auto kc) {
         if (few_q) {
           DP_TRY((rel_allow_lds<rel_bwd_few_dq_bf16_kernel<dhp, kc>>(1024 * dhp, both)));
@@ -2496,7 +2505,7 @@ int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_h
     KScope ks(KK_ATTN_BWD_DKV, fl, by, s, Nq, Nk, d_head);
     // Three waves per SIMD where two would begin a second round; under the causal mask tiles end at different times anyway, and its selects have no registers
     // left (8 x 10 heads of 1024 40 and 46 us)
-    const bool many = d_head <= 64 && !causal && kblocks > 2 * 256;
+    const bool many = d_head <= 64 && !causal && kblocks > 2 * 256 && rel_per_cu(768 * dhp + 4 * 64 * 4 + table, 3) == 3;      // (with 512 buckets to 1024 LDS holds two: 263 -> 241 us)
     a.even = rel_takes_turns(kblocks, many ? 3 : 2, causal);
     DP_TRY(rel_dispatch(d_head, [&](auto dhp, auto kc) {
       if (few_k) {

@@ -1,0 +1,45 @@
+"""The backward of the attention with a relative position bias by the size of its table: the launches that it takes, and results against the definition."""
+import pytest
+
+from test_gpu_attention_relbias import _check
+
+pytestmark = pytest.mark.gpu
+
+DQ, DKV = "attn_bwd_dq", "attn_bwd_dkv"
+
+
+def _kinds(B, H, nq, nk, d, causal, n_buckets, distance, both):
+    """Kinds of the launches of a bf16 backward."""
+    import torch
+    from paper_2405_01248_amd import binding as K
+    ld = H * d
+    q, do, o, dq = (torch.randn((B, nq, ld), device="cuda").bfloat16() for _ in range(4))
+    k, v, dk, dv = (torch.randn((B, nk, ld), device="cuda").bfloat16() for _ in range(4))
+    table, lse, dtable = torch.randn((n_buckets, H), device="cuda").bfloat16(), torch.zeros((B, H, nq), device="cuda"), torch.empty((n_buckets, H), device="cuda")
+    ws = torch.empty(K.op_attention_relbias_workspace_bytes(B, H, nq, nk, d, n_buckets, True), dtype=torch.uint8, device="cuda")
+    K.ktime_begin(64)
+    K.op_attention_relbias_bwd(K.DP_BF16, B, H, nq, nk, d, causal, 0.125, q, ld, k, ld, v, ld, K.RelBias(table, n_buckets, distance, both, 0), None, o, ld, lse, do, ld,
+                               dq, ld, dk, ld, dv, ld, dtable, False, ws)
+    return [r["kind"] for r in K.ktime_end(64)]
+
+
+# One launch for all gradients where its workgroups all run at once: 512 with a table of 32 buckets to 128 distances (two a CU), 256 with one that leaves LDS for one.
+@pytest.mark.parametrize("H,n,causal,small,large", [(16, 512, False, [DKV], [DQ, DKV]), (16, 512, True, [DKV], [DQ, DKV]), (8, 512, False, [DKV], [DKV]), (32, 512, False, [DQ, DKV], [DQ, DKV])])
+def test_one_launch_where_its_workgroups_run_at_once(H, n, causal, small, large):
+    for (n_buckets, distance), want in (((32, 128), small), ((64, 256), large)):
+        kinds = _kinds(1, H, n, n, 64, causal, n_buckets, distance, not causal)
+        assert [k for k in kinds if k in (DQ, DKV)] == want, (n_buckets, kinds)
+
+
+@pytest.mark.parametrize("both", [True, False])
+@pytest.mark.parametrize("B,H,nq,nk,d,causal", [(1, 16, 512, 512, 64, False), (1, 16, 512, 512, 64, True), (1, 12, 1000, 1000, 40, False), (1, 50, 300, 300, 64, False), (2, 10, 300, 250, 64, True),
+                                                (3, 8, 1024, 1024, 64, True), (1, 8, 2048, 2048, 64, False), (4, 18, 200, 200, 64, False), (3, 4, 520, 520, 88, False)])
+def test_large_tables(B, H, nq, nk, d, causal, both):
+    lens = [nk - i * nk // (B + 1) for i in range(B)]
+    _check("bf16", B, H, nq, nk, d, causal, both, 64, 256, nk - nq, lens)
+
+
+@pytest.mark.parametrize("both", [True, False])
+@pytest.mark.parametrize("B,H,n", [(8, 10, 700), (9, 14, 300)])
+def test_tables_that_leave_room_for_two_workgroups_a_cu(B, H, n, both):
+    _check("bf16", B, H, n, n, 64, False, both, 512, 1024, 0, None)

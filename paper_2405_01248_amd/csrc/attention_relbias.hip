@@ -2453,23 +2453,15 @@ int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_h
       return rel_launched();
     }));
   } else if (all_keys) {
-    KScope ks(KK_ATTN_BWD_DKV, 2 * fl, 2 * by, s, Nq, Nk, d_head);
     a.qsplits = rel_query_shares(B, H, Nq);
     a.dtable_parts = B * a.qsplits;
+    KScope ks(KK_ATTN_BWD_DKV, 2 * fl, 2 * by, s, Nq, Nk, d_head);
     DP_TRY(rel_short_dispatch(d_head, Nk, [&](auto dhp, auto kc, auto nw) {
       const int lds = RelShort<dhp, nw>::BYTES + rel_sum_floats(a.bk, nw) * 4;
       DP_TRY((rel_allow_lds<rel_bwd_short_bf16_kernel<dhp, kc, nw>>(0, lds)));
       hipLaunchKernelGGL((rel_bwd_short_bf16_kernel<dhp, kc, nw>), dim3((unsigned)(B * H * a.qsplits)), dim3(64 * nw), lds, s, a, st);
       return rel_launched();
     }));
-    if (a.qsplits > 1) {
-      hipLaunchKernelGGL((rel_join_grads_kernel<bf16>), dim3((unsigned)(rel_join_workgroups(B, Nk, H, d_head) + a.table_items)), dim3(256), 0, s, a, 0u);
-      return rel_launched();
-    }
-    if (dtable) {
-      hipLaunchKernelGGL(rel_dtable_kernel, dim3(a.table_items), dim3(256), 0, s, a);
-      return rel_launched();
-    }
   } else if (at_once) {
     KScope ks(KK_ATTN_BWD_DKV, 2 * fl, 2 * by, s, Nq, Nk, d_head);
     const int dq = (Nq + 31) / 32 * B * H * a.ksplits, dkv = (Nk + 31) / 32 * B * H * a.qsplits;
@@ -2523,10 +2515,12 @@ int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_h
       return many ? run(integral_constant<int, dhp == 64 ? 3 : 2>(), std::false_type()) : run(integral_constant<int, 2>(), std::false_type());
     }));
   }
-  if (all_keys) return DP_OK;
-  if (!at_once) a.table_items = 0;      // (they were there already)
+  if (!at_once && !all_keys) a.table_items = 0;      // (they were there already)
+  if (a.ksplits == 1 && a.qsplits == 1 && a.table_items == 0) return DP_OK;
+  const double parts = 4.0 * a.dtable_parts * H * bias->n_buckets, es = dtype == DP_BF16 ? 2.0 : 4.0, hd = (double)H * d_head;
+  KScope ks(KK_REDUCE, 0.0, (a.table_items ? parts : 0.0) + (a.ksplits > 1 ? (4.0 * a.ksplits + es) * B * Nq * hd : 0.0) + (a.qsplits > 1 ? 2 * (4.0 * a.qsplits + es) * B * Nk * hd : 0.0), s,
+            H * d_head, a.ksplits, a.qsplits);
   if (a.ksplits == 1 && a.qsplits == 1) {
-    if (a.table_items == 0) return DP_OK;
     hipLaunchKernelGGL(rel_dtable_kernel, dim3(a.table_items), dim3(256), 0, s, a);
     return rel_launched();
   }

@@ -2102,12 +2102,14 @@ static int rel_buckets(const char* who, int n_buckets, int max_distance, int bid
 }
 
 static size_t rel_align(size_t n) { return align_up(n, 256); }
-// Shares of the queries where a workgroup has all keys of a head: as many as run beside each other, of two tiles at least.
+// Shares of the queries where a workgroup has all keys of a head: as many as run beside each other (per_cu of them a CU: two of up to 128 keys and width 64 beside a small table, else one),
+// of two tiles at least.  us a pass with as many as 512 workgroups, rounded up, / with what runs at once: 8 x 30 heads of 1024 x 77 63 / 46, 8 x 10 of 4096 x 77, width 40, 71 / 54, 4 x 20
+// of 2048 x 77 48 / 38, width 96, 109 / 89, 8 x 20 of 1024 x 256 88 / 65, 4 x 20 of 1024 x 250, width 72, 68 / 54.
 constexpr long REL_QUERY_SHARES = 16, REL_QUERY_BLOCKS = 512;
-static int rel_query_shares(int B, int H, int Nq) {
+static int rel_query_shares(int B, int H, int Nq, int per_cu) {
   const long blocks = (long)B * H, tiles = (Nq + 63) / 64;
   if (blocks >= 256) return 1;
-  const long shares = std::max<long>(1, std::min(std::min(REL_QUERY_SHARES, tiles / 2), (REL_QUERY_BLOCKS + blocks - 1) / blocks)), each = (tiles + shares - 1) / shares;
+  const long shares = std::max<long>(1, std::min(std::min(REL_QUERY_SHARES, tiles / 2), std::min(REL_QUERY_BLOCKS, 256l * per_cu) / blocks)), each = (tiles + shares - 1) / shares;
   return (int)((tiles + each - 1) / each);
 }
 // Shares of the keys (dQ), or of the queries (dK / dV), where workgroups of 128 of the others are too few for the CUs: four tiles at least, two workgroups a CU at most,
@@ -2172,13 +2174,13 @@ static bool rel_few_both(int B, int H, int Nq, int Nk, int per_cu, int& ksplits,
   rel_share_out(heads, q, k, std::min<long>(REL_GRAD_SHARES, (Nk + 63) / 64 / 8), std::min<long>(REL_GRAD_SHARES, (Nq + 63) / 64 / 8), ksplits, qsplits);
   return true;
 }
-// The backward's: the same for both types and any bias.  Fewer samples may have more shares, but never more workgroups than REL_*_BLOCKS (begun) where there are
+// The backward's: the same for both types and any bias.  Fewer samples may have more shares, but never more workgroups than REL_*_BLOCKS where there are
 // shares at all: what these leave is the bound, so that no size needs more than a greater one.
 struct RelWorkspace { size_t delta, partial, dq, dkv, bytes; };
 static RelWorkspace rel_workspace(int B, int H, int Nq, int Nk, int d_head, int n_buckets) {
   RelWorkspace w;
   const size_t heads = (size_t)B * H, row = d_head * sizeof(float);
-  const size_t few_keys = REL_QUERY_BLOCKS + 255, parts = std::max(heads * ((Nq + 31) / 32), std::min(heads * ((Nq + 31) / 32) * REL_QUERY_SHARES, few_keys));
+  const size_t few_keys = REL_QUERY_BLOCKS, parts = std::max(heads * ((Nq + 31) / 32), std::min(heads * ((Nq + 31) / 32) * REL_QUERY_SHARES, few_keys));
   auto left = [&](int N, int along) {
     const long most = rel_shares_most_f32(along);      // (no less than the other type's)
     return most > 1 ? std::min(most * heads * N, (size_t)REL_GRAD_BLOCKS * 128) : 0;
@@ -2422,9 +2424,12 @@ int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_h
   // One kernel whose workgroups hold all keys, where its LDS suffices for the bias; few heads go by 32 queries and keys, but up to 128 keys only in one launch: 8 heads of 200 20.6 /
   // 12.7 us, 8 of 128 15.4 / 12.1, 64 of 77 16.5 / 13.0, 20 of 300 x 250 27 / 16, 60 of 171, width 40, causal 22 / 18, 72 of 200 28 / 22; but 100 of 128 16.4 / 20.5, 144 of 41, width 40, 13 / 17.
   bool all_keys = false;
+  int short_per_cu = 1;
   if (dtype == DP_BF16 && Nk <= 256 && !at_once && !(Nk > 128 && few_q && few_k))
     DP_TRY(rel_short_dispatch(d_head, Nk, [&](auto dhp, auto, auto nw) {
-      all_keys = RelShort<dhp, nw>::BYTES + rel_sum_floats(a.bk, nw) * 4 <= 160 * 1024;
+      const int lds = RelShort<dhp, nw>::BYTES + rel_sum_floats(a.bk, nw) * 4;
+      all_keys = lds <= 160 * 1024;
+      short_per_cu = rel_per_cu(lds, nw == 4 ? 2 : 1);
       return DP_OK;
     }));
   a.dtable_add = accumulate != 0;
@@ -2453,7 +2458,7 @@ int dp_op_attention_relbias_bwd(int dtype, int B, int H, int Nq, int Nk, int d_h
       return rel_launched();
     }));
   } else if (all_keys) {
-    a.qsplits = rel_query_shares(B, H, Nq);
+    a.qsplits = rel_query_shares(B, H, Nq, short_per_cu);
     a.dtable_parts = B * a.qsplits;
     KScope ks(KK_ATTN_BWD_DKV, 2 * fl, 2 * by, s, Nq, Nk, d_head);
     DP_TRY(rel_short_dispatch(d_head, Nk, [&](auto dhp, auto kc, auto nw) {

@@ -45,8 +45,19 @@ def test_every_launch_is_recorded(dtype, B, H, nq, nk, want):
     assert _kinds(B, H, nq, nk, 64, False, 32, 128, True, dtype=dtype) == want
 
 
+# Shares of the queries where a workgroup has all keys: no more workgroups than run at once, of which a CU holds two of up to 128 keys and width 64 with a table of 32 buckets to 128.
+@pytest.mark.parametrize("H,nq,nk,d,n_buckets,distance,at_once", [(80, 2048, 77, 64, 32, 128, 512), (80, 2048, 77, 96, 32, 128, 256), (80, 2048, 77, 64, 64, 256, 256), (80, 1024, 200, 64, 32, 128, 256),
+                                                                  (160, 1024, 250, 40, 32, 128, 256), (40, 4096, 77, 64, 32, 128, 512), (255, 1024, 77, 64, 32, 128, 512)])
+def test_shares_of_the_queries_run_at_once(H, nq, nk, d, n_buckets, distance, at_once):
+    main, join = _records(1, H, nq, nk, d, False, n_buckets, distance, True)
+    assert main["kind"] == DKV and join["kind"] == REDUCE and join["n"] == 1
+    shares, tiles = join["k"], (nq + 63) // 64
+    each = -(-tiles // max(1, min(16, tiles // 2, at_once // H)))
+    assert H * shares <= at_once and shares == -(-tiles // each), (shares, each)
+
+
 @pytest.mark.parametrize("both", [True, False])
-@pytest.mark.parametrize("B,H,nq,nk,d,causal", [(1, 16, 512, 512, 64, False), (1, 16, 512, 512, 64, True), (1, 12, 1000, 1000, 40, False), (1, 50, 300, 300, 64, False), (2, 10, 300, 250, 64, True),
+@pytest.mark.parametrize("B,H,nq,nk,d,causal", [(1, 16, 512, 512, 64, False), (1, 16, 512, 512, 64, True), (1, 12, 1000, 1000, 40, False), (1, 50, 300, 300, 64, False), (2, 10, 300, 250, 64, True), (4, 20, 700, 77, 64, False),
                                                 (3, 8, 1024, 1024, 64, True), (1, 8, 2048, 2048, 64, False), (4, 18, 200, 200, 64, False), (3, 4, 520, 520, 88, False)])
 def test_large_tables(B, H, nq, nk, d, causal, both):
     lens = [nk - i * nk // (B + 1) for i in range(B)]

@@ -478,8 +478,8 @@ int dp_op_attention_bwd(int dtype, int B, int H, int Nq, int Nk, int d_head, flo
  * A query that sees no key has the output zero and lse = -infinity, and contributes nothing to the gradients.  Layout of q, k, v, o, lse as in
  * dp_op_attention_fwd; lse may be NULL in the forward.  The backward takes o and lse of the forward and writes dq, dk, dv and, unless NULL, the
  * table's gradient dtable, fp32 [n_buckets, H], overwritten or added to with accumulate.  Sums are in a fixed order: equal calls give equal bits.
- * d_head at most 96; d_head and row strides multiples of 8 (bf16) or 4 (fp32); scale within [1e-6, 1e6]; each operand's rows of one sample
- * below 2 GiB; pointers 16-byte aligned (key_len 4).  Outputs may not overlap inputs.
+ * d_head at most 96; d_head and row strides multiples of 8 (bf16, strides below 2^24) or 4 (fp32); scale within [1e-6, 1e6]; each operand's rows of one
+ * sample below 2 GiB; pointers 16-byte aligned (key_len 4).  Outputs may not overlap inputs.
  * workspace: dp_op_attention_relbias_workspace_bytes bytes, 256-byte aligned, needed by the backward; the forward uses it where it splits the keys of few
  * queries, and runs without it (NULL) unsplit.  Fewer samples, queries or keys (heads, width and buckets being the same) need no more.  Calls that may overlap
  * need workspaces of their own. */

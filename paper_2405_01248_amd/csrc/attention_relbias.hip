@@ -2293,6 +2293,8 @@ static int check_rel(const char* who, int dtype, const RelAttnK& k, const dp_rel
     DP_TRY(check_ptr(ops[i].p, ops[i].name));
     if (ops[i].ld < span) return set_errorf(DP_EINVAL, "%s: the row stride of %s is less than heads * d_head", who, ops[i].name);
     if (ops[i].ld % grid) return set_errorf(DP_EUNSUPPORTED, "%s: the row stride of %s must be a multiple of %d", who, ops[i].name, grid);
+    // (a tile's copies count up to 128 rows, whether they exist or not, by 32-bit byte offsets: beyond 2^32 those of missing rows would come round to others)
+    if (dtype == DP_BF16 && ops[i].ld >= 1 << 24) return set_errorf(DP_EUNSUPPORTED, "%s: the row stride of %s must be below 2^24 elements", who, ops[i].name);
     // one (sample, head) is addressed with 32-bit byte offsets, of which bit 31 means "no data"
     if ((size_t)ops[i].n * ops[i].ld * es >= (1ull << 31)) return set_errorf(DP_EUNSUPPORTED, "%s: the rows of one sample of %s must span less than 2 GiB", who, ops[i].name);
   }

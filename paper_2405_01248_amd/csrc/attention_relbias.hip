@@ -827,7 +827,7 @@ __device__ __forceinline__ void rel_store_dkv(const RelAttnK& p, const f32x16 (&
 // ------------------------------------------------------------------ dK, dV (bf16)
 // Each wave owns 32 keys and walks the queries in tiles of 64, from the first that sees one of the workgroup's keys (see attn_bwd_dkv_bf16_kernel).  The
 // bias is the addend of the exponent here, and lse what the scores begin with.  MINW: waves per SIMD, exactly; three have no registers for K, which they read from
-// LDS again for every tile, nor for the causal mask: 8 x 10 heads of 1024 72 -> 55 us, 8 x 5 of 4096 372 -> 343, 16 x 16 of 300 33 -> 27.  Four products a block bound
+// LDS again for every tile, nor for the causal mask, and leave 5 of width 64 (2 of 48) in scratch, of which 3 (none) are read again every second tile: 8 x 10 heads of 1024 72 -> 55 us, 8 x 5 of 4096 372 -> 343, 16 x 16 of 300 33 -> 27.  Four products a block bound
 // it: 8 x 5 of 4096 are 344 GF, 305 us at a large product's rate.  SHARES: one of qsplits shares of the query tiles, as above.
 template <int DHP, int KC, int MINW, bool SHARES>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(MINW, MINW))) rel_bwd_dkv_bf16_kernel(const RelAttnK p, const RelStarts st) {
@@ -1354,7 +1354,7 @@ __global__ void __launch_bounds__(256, DHP == 64 ? 2 : 1) rel_bwd_few_both_bf16_
 // exponentials once instead of twice.  Per tile every wave adds to its keys' dK and dV, adds its dS along the diagonals and leaves it in LDS; behind a barrier the
 // dQ of the tile is formed from it and the keys, while the next tile's delta is.  64 x 12 heads of 77 tokens 31 us (42 by the two kernels above), 32 x 16 of 256 and
 // width 72 75 (101); the chain of a tile, two barriers long, bounds it.  The second sixteen keys of a wave work with -V, hence -delta and
-// -dS (see rel_bwd_dq_bf16_kernel).
+// -dS (see rel_bwd_dq_bf16_kernel).  Wide heads leave 11 to 23 registers in scratch, fragments and offsets that every tile reads again.
 template <int DHP, int NW> struct RelShort {
   static constexpr int TILE = 64 * DHP, K = 32 * NW * DHP, DS = 32 * NW * 64;                            // elements
   static_assert(K <= 2 * TILE + DS, "V passes through the second stage and dS");

@@ -66,3 +66,16 @@ def test_relbias_workgroups_a_cu(kernels):
     small, large = 9 * 4 * 376, 9 * 4 * 628
     assert _lds_a_cu(1024 * 64 + 2096 + small) == 2 and _lds_a_cu(1024 * 64 + 2096 + large) == 1
     assert _lds_a_cu(512 * 64 + 1072 + small) == 3 and _lds_a_cu(512 * 64 + 1072 + large) == 2
+
+
+def test_what_the_relative_bias_leaves_in_scratch(kernels):
+    """Nothing, but for the three waves a SIMD of dK / dV and the wide heads of the kernel that has all keys: no more than their comments say."""
+    known = {r"rel_bwd_dkv_bf16_kernelILi64ELi4ELi3E": (5, 24), r"rel_bwd_dkv_bf16_kernelILi64ELi3ELi3E": (2, 12), r"rel_bwd_short_bf16_kernelILi96E": (23, 96)}
+    seen = 0
+    for name, r in kernels.items():
+        if not re.search(r"rel_(fwd|bwd|join|dtable)", name):
+            continue
+        seen += 1
+        registers, scratch = next((v for k, v in known.items() if re.search(k, name)), (0, 0))
+        assert r["vgpr_spill_count"] <= registers and r["private_segment_fixed_size"] <= scratch, (name, r)
+    assert seen > 50, seen

@@ -68,3 +68,101 @@ def test_large_tables(B, H, nq, nk, d, causal, both):
 @pytest.mark.parametrize("B,H,n", [(8, 10, 700), (9, 14, 300)])
 def test_tables_that_leave_room_for_two_workgroups_a_cu(B, H, n, both):
     _check("bf16", B, H, n, n, 64, False, both, 512, 1024, 0, None)
+
+
+# Every split of the backward and of the forward with tables whose end buckets, far sums and LDS differ from those of 32 buckets to 128 distances, queries without a key among them.
+TABLES = [(64, 256, True), (64, 256, False), (512, 1024, False)]
+TYPES = [("bf16", *table) for table in TABLES] + [("f32", 64, 256, False)]
+
+
+def _offset(nq, nk, causal):
+    return -(nq // 3) if causal else nk // 2 - 37      # (under the causal mask the first third sees nothing)
+
+
+@pytest.mark.parametrize("dtype,n_buckets,distance,both", TYPES)
+@pytest.mark.parametrize("B,H,nq,nk,d,causal,lens", [
+    (1, 3, 513, 513, 64, False, None), (1, 3, 513, 513, 64, True, None), (1, 2, 70, 2100, 40, False, [1500]), (2, 1, 2050, 300, 96, True, [300, 7]), (1, 4, 1024, 1024, 80, True, [700]),
+    (1, 10, 900, 1000, 88, False, [777]), (2, 8, 1030, 1030, 72, True, [1030, 640]), (1, 6, 1500, 1500, 64, False, [1499]), (3, 6, 1100, 1100, 64, False, [1100, 1, 600]),
+    (1, 2, 30, 3000, 64, False, [2999]), (1, 2, 3000, 30, 40, False, None), (2, 3, 330, 300, 8, True, [0, 290])])
+def test_gradients_in_shares(dtype, n_buckets, distance, both, B, H, nq, nk, d, causal, lens):
+    _check(dtype, B, H, nq, nk, d, causal, both, n_buckets, distance, _offset(nq, nk, causal), lens)
+
+
+@pytest.mark.parametrize("n_buckets,distance,both", TABLES)
+@pytest.mark.parametrize("B,H,nq,nk,d,causal,lens", [
+    (30, 12, 77, 77, 64, False, "some"), (7, 40, 130, 120, 96, True, None), (50, 8, 40, 33, 24, True, "some"), (9, 30, 64, 200, 72, False, "some"), (5, 60, 150, 256, 40, True, None),
+    (2, 6, 1500, 100, 40, True, None), (2, 40, 1000, 250, 64, False, [250, 129])])
+def test_gradients_where_a_workgroup_has_all_keys(n_buckets, distance, both, B, H, nq, nk, d, causal, lens):
+    _check("bf16", B, H, nq, nk, d, causal, both, n_buckets, distance, _offset(nq, nk, causal), [(nk * (i + 1)) // B for i in range(B)] if lens == "some" else lens)
+
+
+@pytest.mark.parametrize("n_buckets,distance,both", TABLES)
+@pytest.mark.parametrize("B,H,nq,nk,d,causal,lens", [(1, 3, 1000, 2500, 64, True, None), (2, 2, 800, 2100, 88, False, [2100, 130]), (3, 4, 700, 2049, 64, True, [0, 1, 2049]), (2, 8, 1, 4000, 64, False, [4000, 77])])
+def test_shares_of_the_keys(n_buckets, distance, both, B, H, nq, nk, d, causal, lens):
+    _check("bf16", B, H, nq, nk, d, causal, both, n_buckets, distance, _offset(nq, nk, causal), lens)
+
+
+@pytest.mark.parametrize("dtype,n_buckets,distance,both", TYPES + [("bf16", 511, 1000, False)])
+@pytest.mark.parametrize("B,H,nq,nk,d", [(1, 8, 1024, 1024, 64), (1, 2, 2048, 2500, 40), (3, 5, 520, 256, 96), (2, 40, 1000, 77, 64), (4, 12, 77, 77, 64)])
+def test_nothing_is_written_behind_the_workspace(dtype, n_buckets, distance, both, B, H, nq, nk, d):
+    import torch
+    from paper_2405_01248_amd import binding as K
+    ld, t = H * d, torch.float32 if dtype == "f32" else torch.bfloat16
+    q, do, o, dq = (torch.randn((B, nq, ld), device="cuda").to(t) for _ in range(4))
+    k, v, dk, dv = (torch.randn((B, nk, ld), device="cuda").to(t) for _ in range(4))
+    table, lse, whole = torch.randn((n_buckets, H), device="cuda").to(t), torch.empty((B, H, nq), device="cuda"), torch.full((n_buckets * H + 4096,), 9.0, device="cuda")
+    dtable = whole[:n_buckets * H].view(n_buckets, H)
+    for backward in (False, True):
+        n = K.op_attention_relbias_workspace_bytes(B, H, nq, nk, d, n_buckets, backward)
+        ws = torch.full((n + 65536,), 0x5A, dtype=torch.uint8, device="cuda")
+        args = (K.DP_F32 if dtype == "f32" else K.DP_BF16, B, H, nq, nk, d, False, 0.125, q, ld, k, ld, v, ld, K.RelBias(table, n_buckets, distance, both, 0), None, o, ld, lse)
+        if backward:
+            K.op_attention_relbias_bwd(*args, do, ld, dq, ld, dk, ld, dv, ld, dtable, False, ws[:n])
+        else:
+            K.op_attention_relbias_fwd(*args, ws[:n] if n else None)
+        assert (ws[n:] == 0x5A).all() and (whole[n_buckets * H:] == 9.0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,H,nq,nk", [(1, 6, 1500, 1500), (2, 20, 900, 77), (1, 4, 3, 3000)])
+def test_captured_passes_and_another_stream(dtype, B, H, nq, nk):
+    """Split passes with a table of one direction, replayed and beside the others on a second stream, each with buffers of its own."""
+    import torch
+    from paper_2405_01248_amd import binding as K
+    d, nb, t, dt = 64, 64, torch.float32 if dtype == "f32" else torch.bfloat16, K.DP_F32 if dtype == "f32" else K.DP_BF16
+    ld = H * d
+    q, do = (torch.randn((B, nq, ld), device="cuda").to(t) for _ in range(2))
+    kv, table = torch.randn((B, nk, 2 * ld), device="cuda").to(t), torch.randn((nb, H), device="cuda").to(t)
+    key_len = torch.full((B,), nk, dtype=torch.int32, device="cuda")
+    bias = K.RelBias(table, nb, 256, False, nk - nq - 20)
+
+    def buffers():
+        ws = [K.op_attention_relbias_workspace_bytes(B, H, nq, nk, d, nb, backward) for backward in (False, True)]
+        return {"o": torch.empty_like(q), "lse": torch.empty((B, H, nq), device="cuda"), "dq": torch.empty_like(q), "dkv": torch.empty_like(kv), "dt": torch.empty((nb, H), device="cuda"),
+                "ws": [torch.empty(n, dtype=torch.uint8, device="cuda") if n else None for n in ws]}
+
+    def step(b):
+        args = (dt, B, H, nq, nk, d, True, 0.125, q, ld, kv, 2 * ld, kv[:, :, ld:], 2 * ld, bias, key_len, b["o"], ld, b["lse"])
+        K.op_attention_relbias_fwd(*args, b["ws"][0])
+        K.op_attention_relbias_bwd(*args, do, ld, b["dq"], ld, b["dkv"], 2 * ld, b["dkv"][:, :, ld:], 2 * ld, b["dt"], False, b["ws"][1])
+
+    cap, eager, other = buffers(), buffers(), buffers()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(cap)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(cap)
+    for i in range(3):
+        kv.normal_()
+        key_len[0] = nk - 500 * i if nk > 1000 else nk - 5 * i
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            step(other)
+        graph.replay()
+        step(eager)
+        torch.cuda.synchronize()
+        for name in ("o", "lse", "dq", "dkv", "dt"):
+            assert torch.equal(cap[name], eager[name]) and torch.equal(other[name], eager[name]), name

@@ -72,11 +72,13 @@ __device__ __forceinline__ int rel_keys(const RelAttnK& p, int b) {
 __device__ __forceinline__ float rel_entry(float v, float factor) { return v <= -65536.f ? -INFINITY : v * factor; }
 
 // Bias of head h by distance, times a factor.  Entry e is distance lo - margin + e, or, REVERSED, hi + margin - e.  In two steps, so that the table's
-// loads are on their way beside the first tiles': what a thread has of the first two rounds is requested first and stored behind the tiles' copies.
+// loads are on their way beside the first tiles': what a thread has of the first two rounds is requested first and stored behind the tiles' copies.  Distances less than any of
+// the call's have the bias of the least: only queries of the last tile that do not exist meet them, whose probabilities (0 times the bias's exponential) would be NaN if the
+// table held NaN or infinity there.
 template <typename T, bool REVERSED, int THREADS> struct RelFill {
   T v[2];
   __device__ __forceinline__ T entry(const RelAttnK& p, const RelStarts& st, int h, int e) const {
-    const int dist = REVERSED ? p.bk.hi + REL_MARGIN - e : p.bk.lo - REL_MARGIN + e;
+    const int dist = max(REVERSED ? p.bk.hi + REL_MARGIN - e : p.bk.lo - REL_MARGIN + e, 1 - p.Nq - p.query0);
     return ((const T*)p.table)[(size_t)rel_bucket(p.bk, st, dist) * p.H + h];
   }
   __device__ __forceinline__ void request(const RelAttnK& p, const RelStarts& st, int h) {

@@ -166,3 +166,17 @@ def test_captured_passes_and_another_stream(dtype, B, H, nq, nk):
         torch.cuda.synchronize()
         for name in ("o", "lse", "dq", "dkv", "dt"):
             assert torch.equal(cap[name], eager[name]) and torch.equal(other[name], eager[name]), name
+
+
+# Buckets of distances that no query and key of the call have: rows of the last tile that do not exist meet them.
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,H,nq,nk,d,causal,both,query0,unused", [
+    (1, 2, 33, 33, 64, False, True, 0, [13, 14, 15, 29, 30, 31]), (2, 3, 33, 33, 40, True, False, 0, range(23, 32)), (30, 12, 33, 33, 64, False, True, 0, [13, 14, 15, 29, 30, 31]),
+    (1, 1, 1, 700, 64, False, False, 0, range(1, 32)), (1, 3, 70, 70, 96, True, True, 0, [15, *range(17, 32)]), (4, 12, 77, 300, 64, False, True, 0, [15]),
+    (8, 10, 70, 70, 64, False, True, 0, [15, 31]), (4, 20, 70, 300, 64, False, True, 0, [15]), (1, 2, 40, 2000, 64, True, False, 0, range(24, 32)), (1, 8, 33, 300, 96, False, False, 0, range(23, 32)), (3, 40, 33, 520, 64, False, False, 0, range(23, 32))])
+def test_anything_in_buckets_of_distances_that_do_not_occur(dtype, B, H, nq, nk, d, causal, both, query0, unused):
+    from oracle import training_ops as T
+    visible = [[not causal or k <= q + query0 for k in range(nk)] for q in range(nq)]
+    assert not set(T.buckets(nq, nk, query0, 32, 128, both)[visible].tolist()) & set(unused)
+    for x in (float("nan"), float("inf"), -float("inf")):
+        _check(dtype, B, H, nq, nk, d, causal, both, 32, 128, query0, None, garbage={k: x for k in unused})

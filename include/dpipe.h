@@ -470,11 +470,12 @@ int dp_op_attention_bwd(int dtype, int B, int H, int Nq, int Nk, int d_head, flo
  * each direction has half of n_buckets, keys behind the query the second half; else all are for keys up to the query, and keys behind it
  * share bucket 0.  dp_relative_bucket (host) returns the bucket of distance = key position - query position, or an error code.
  *   table    [device] [n_buckets, H] in the storage dtype; n_buckets 2 .. 512 (even, at least 4, if bidirectional), max_distance above half, at most 1024.
- *            The pairs of an entry of -65536 or less are masked, as those of -infinity are.
+ *            The pairs of an entry of -65536 or less are masked, as those of -infinity are (also where these are all that a query sees).
+ *            Entries that no visible pair has are read but count for nothing, whatever they hold.
  *   key_len  [device] int32 [B] or NULL: sample b has keys 0 .. key_len[b] - 1 (taken as at least 0 and at most Nk)
  *   causal   query i sees keys j <= query0 + i only
  * Keys and values that no query of the call sees, behind the sample's length or behind the last query, are not read; the backward writes zeros for
- * their gradients.
+ * their gradients.  All other rows of q, k, v, o and d_o take part in products, with a weight of zero where a pair is masked: they should be finite.
  * A query that sees no key has the output zero and lse = -infinity, and contributes nothing to the gradients.  Layout of q, k, v, o, lse as in
  * dp_op_attention_fwd; lse may be NULL in the forward.  The backward takes o and lse of the forward and writes dq, dk, dv and, unless NULL, the
  * table's gradient dtable, fp32 [n_buckets, H], overwritten or added to with accumulate.  Sums are in a fixed order: equal calls give equal bits.

@@ -3,6 +3,8 @@
 //
 // bf16: the tiles, operand layouts and splits of the kernels without a bias (dp_attention_tile.h): a wave owns 32 queries (forward, dQ) or 32 keys
 // (dK / dV), scores come out of the matrix instruction with one query (key) a lane, and the other side streams through LDS in tiles of 64.
+// P and dS are rounded to bf16 as operands of the second products (the instruction for fp32 has a sixteenth of the rate): each is off by up to 2^-8 of itself, at random, so that outputs are some 0.0022 of their size
+// from 64 bits, of which their own rounding is 0.0017; sums, references, lse and the table's gradient are fp32.
 // The bias costs these loops no vector instruction.  What the accumulators of the scores are cleared with otherwise is the bias over the scale:
 //   - bias over distance lies in LDS (fp32) from the last distance at which the bucket still changes to the other one, and 96 distances
 //     of the end buckets beyond either, as far as a tile that touches the middle reaches; four neighbouring accumulator registers are four neighbouring entries;

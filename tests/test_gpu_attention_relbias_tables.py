@@ -180,3 +180,16 @@ def test_anything_in_buckets_of_distances_that_do_not_occur(dtype, B, H, nq, nk,
     assert not set(T.buckets(nq, nk, query0, 32, 128, both)[visible].tolist()) & set(unused)
     for x in (float("nan"), float("inf"), -float("inf")):
         _check(dtype, B, H, nq, nk, d, causal, both, 32, 128, query0, None, garbage={k: x for k in unused})
+
+
+# Buckets that only keys behind a sample's length meet.
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,H,nq,nk,d,query0,length", [(1, 2, 300, 300, 64, 0, 20), (1, 8, 70, 500, 40, -5, 15), (40, 10, 77, 77, 64, 0, 19), (3, 40, 130, 300, 64, 0, 17), (8, 12, 300, 400, 96, 0, 12),
+                                                       (4, 3, 1, 2000, 64, 0, 20), (1, 3, 400, 2300, 64, 0, 18), (2, 40, 513, 90, 64, 0, 16)])
+def test_anything_in_buckets_behind_the_key_lengths(dtype, B, H, nq, nk, d, query0, length):
+    from oracle import training_ops as T
+    bk = T.buckets(nq, nk, query0, 32, 128, True)
+    hidden = sorted(set(bk[:, length:].ravel().tolist()) - set(bk[:, :length].ravel().tolist()))
+    assert len(hidden) >= 4
+    for x in (float("nan"), float("inf")):
+        _check(dtype, B, H, nq, nk, d, False, True, 32, 128, query0, [length] * (B - 1) + [length - 1], garbage={k: x for k in hidden})

@@ -2217,6 +2217,8 @@ template <auto KERNEL> static int rel_allow_lds(int own, int dynamic) {
   devices.fetch_or(bit, std::memory_order_release);
   return DP_OK;
 }
+// Width of the tiles and steps of 16 over the head.  us with the steps of the next line instead: width 40, 8 x 5 heads of 4096 forward 170 / 181, 8 x 10 of 1024 forward and backward 28.9 + 86.9 / 30.0 + 92.6; width 72
+// and 80, 8 x 10 of 1024 39.3 + 148 / 40.4 + 154, 32 x 16 of 256 backward 76 / 85.
 template <class F> static int rel_dispatch(int d_head, F f) {
   using std::integral_constant;
   if (d_head <= 48) return f(integral_constant<int, 64>(), integral_constant<int, 3>());
@@ -2224,7 +2226,8 @@ template <class F> static int rel_dispatch(int d_head, F f) {
   if (d_head <= 80) return f(integral_constant<int, 96>(), integral_constant<int, 5>());
   return f(integral_constant<int, 96>(), integral_constant<int, 6>());
 }
-// Blocks of 32 columns and steps of 8 over the head
+// Blocks of 32 columns and steps of 8 over the head.  us with the line behind instead: width 16, 8 x 16 heads of 1000 forward 153 / 185, backward 546 / 668, 4 x 8 of 300 11.5 / 12.9 and 37 / 42; width 40, 8 x 8 of 1000
+// 161 / 184 and 598 / 699.
 template <class F> static int rel_dispatch_f32(int d_head, F f) {
   using std::integral_constant;
   if (d_head <= 16) return f(integral_constant<int, 1>(), integral_constant<int, 2>());
@@ -2259,8 +2262,11 @@ static int rel_shares(int B, int H, int Nq, int Nk, int d_head) {
 // the CUs and these all run at once.  Heads, queries x keys, width, us by 32 (with what joins the shares) and by 128: 8, 256 x 4096, 64 16 / 54 (one share); 8, 1024 x 1024, 64 12 / 17; 16
 // 16 / 17; 8, 2048 x 2048, 64 27 / 30; 4, 2000 x 2000, 40 15 / 27; 32, 512 x 512, 64 11.0 / 11.2; 64, 128 x 256, 64 6.8 / 8.0; 24, 300 x 1000, 72 16 / 19; 12, 512 x 512, 96 11 / 13;
 // but 64, 256 x 256, 64 8.9 / 8.2; 32, 300 x 1000, 72 29 / 20; beyond 2048 keys see rel_shares_128; 24, 512 x 512, 96 21 / 14; 144, 77 x 77, 64 7.3 / 6.4.
-static bool rel_few(int B, int H, int Nq, int Nk, int d_head) {
-  if (Nq <= 32) return true;
+// Up to 32 queries either has a workgroup a head, this one more of them in flight (for shares) and that one four a CU: 512 heads of one query, width 64, 256 keys 7.7 / 9.2, 500 15.4 / 15.0, 1000 30 / 24, 320 of
+// 500 13.4 / 13.6, 1000 24 / 22, 256 of 1000 18.5 / 17.3, 2000 29 / 30, 4000 51 / 56; keys of different lengths 512 of 1000 21 / 20, 384 of 4000 42 / 53, 800 of 4000 101 / 88; 600 of 32 x 32 10.9 / 6.5; width 96, 256 of
+// 200 7.7 / 8.8, 1000 24 / 23, 288 of 200 13.5 / 10.8, 1000 38 / 29, 2040 of 32 x 500 119 / 85.
+static bool rel_few(int B, int H, int Nq, int Nk, int d_head, bool lengths) {
+  if (Nq <= 32) return (long)B * H <= (d_head <= 64 && (Nk <= 512 || lengths) ? 512 : 256);
   const long blocks = (long)B * H * ((Nq + 31) / 32);
   return blocks <= (Nk > 2048 ? 64 : d_head <= 64 && Nk > 256 ? 512 : 256);
 }
@@ -2368,7 +2374,7 @@ int dp_op_attention_relbias_fwd(int dtype, int B, int H, int Nq, int Nk, int d_h
     return rel_launched();
   }
   const int lds = rel_table_floats(a.bk) * 4;
-  if (rel_few(B, H, Nq, Nk, d_head)) {
+  if (rel_few(B, H, Nq, Nk, d_head, key_len != nullptr)) {
     DP_TRY(shares(rel_shares(B, H, Nq, Nk, d_head)));
     DP_TRY(rel_dispatch(d_head, [&](auto dhp, auto kc) {
       DP_TRY((rel_allow_lds<rel_fwd_few_bf16_kernel<dhp, kc>>(1024 * dhp, lds)));

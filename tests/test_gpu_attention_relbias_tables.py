@@ -193,3 +193,9 @@ def test_anything_in_buckets_behind_the_key_lengths(dtype, B, H, nq, nk, d, quer
     assert len(hidden) >= 4
     for x in (float("nan"), float("inf")):
         _check(dtype, B, H, nq, nk, d, False, True, 32, 128, query0, [length] * (B - 1) + [length - 1], garbage={k: x for k in hidden})
+
+
+# Up to 32 queries of so many heads that each gets a workgroup of the kernel for many queries.
+@pytest.mark.parametrize("B,H,nq,nk,d,causal,lens", [(75, 8, 1, 600, 64, True, None), (70, 10, 32, 77, 64, False, "some"), (40, 8, 17, 300, 96, True, "some"), (40, 16, 5, 700, 40, False, "some")])
+def test_few_queries_of_many_heads(B, H, nq, nk, d, causal, lens):
+    _check("bf16", B, H, nq, nk, d, causal, not causal, 32, 128, nk - nq, [(nk * (i + 1)) // B for i in range(B)] if lens else None)
